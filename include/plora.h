@@ -441,6 +441,122 @@ PLORA_API plora_status plora_attn_status(void *workspace_dev, void *stream, int3
  * 0 < cycles <= PLORA_HOOK_MAX_CYCLES.  Synchronises `stream`. */
 PLORA_API plora_status plora_attn_set_debug(void *workspace_dev, int64_t cycles, int32_t hook, void *stream);
 
+/* ---- Serving over a paged KV cache ----------------------------------------------------------------------
+ * (No counterpart in the paper, whose attention takes one contiguous cache per request; these calls are what
+ * stands between the deltas of q, k, v and the delta of o in a serving step.)
+ *
+ * The cache is [n_pages][n_kv_heads][page_size][head_dim] of 16-bit values, one buffer for K and one for V (page_stride
+ * elements between pages; 0 = packed).  Row r of block_table lists the pages of request r in order: token i of the
+ * request lies in slot block_table[r][i / page_size] * page_size + i % page_size, a slot being counted
+ * through all pages (n_pages * page_size must stay below 2^31).
+ *
+ * plora_kv_plan: block tables and slot maps of a step, from the requests' lengths, on the device.
+ *   kv_len, new_len   int32 [n_req]: tokens cached, tokens this step adds (negative values count as 0)
+ *   free_pages        int32 [n_free]: pages to hand out, from index *cursor_in on (nullptr: from 0)
+ *   block_table       int32 [n_req][max_blocks]: entries [ceil(kv_len / page_size), ceil((kv_len + new_len) / page_size))
+ *                     of row r are written, in the order of (request, block); the others are left as they are
+ *   tok_start         int32 [n_req + 1]: first new token of every request, then their number
+ *   positions, tok_req, slots  int32 [max_tokens]: per new token; -1 beyond the last one
+ *   kv_len_out        int32 [n_req]: kv_len + new_len;   cursor_out: int32, *cursor_in + pages taken
+ * A page beyond the free list's end, or a block beyond max_blocks, gives a slot of -1 (and a table entry of -1): a caller
+ * that may run out compares *cursor_out with n_free.  kv_len_out and cursor_out may not be the inputs' buffers.
+ * page_size must be a power of two.  All pointers device.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+PLORA_API plora_status plora_kv_plan(const int32_t *kv_len_dev, const int32_t *new_len_dev, int32_t n_req, int32_t page_size,
+                                     const int32_t *free_pages_dev, int32_t n_free, const int32_t *cursor_in_dev,
+                                     int32_t *block_table_dev, int32_t max_blocks, int32_t max_tokens, int32_t *tok_start_dev,
+                                     int32_t *positions_dev, int32_t *tok_req_dev, int32_t *slots_dev, int32_t *kv_len_out_dev,
+                                     int32_t *cursor_out_dev, void *stream);
+
+/* Rotary positions.  plora_rope_table fills table[pos][i] = {cos, sin} (fp32, times `magnitude`) of pos * f_i for
+ * pos < max_pos, i < rot_dim / 2, computed in 64 bits; 16-byte aligned, max_pos * rot_dim floats.  The frequencies
+ * are f_i = base^(-2 i / rot_dim), scaled for contexts longer than the trained orig_len:
+ *   NONE    f_i
+ *   LINEAR  f_i / factor (positions interpolated)
+ *   NTK     base * factor^(rot_dim / (rot_dim - 2)) in place of base
+ *   BANDS   by the number of turns n_i = orig_len f_i / 2 pi: f_i above `high`, f_i / factor below `low`,
+ *           interpolated linearly in n_i between
+ *   RAMP    f_i up to the pair that turns `high` times over orig_len, f_i / factor from the one that turns `low` times
+ *           on, interpolated linearly in i between (pairs rounded outwards) */
+#define PLORA_ROPE_NONE 0
+#define PLORA_ROPE_LINEAR 1
+#define PLORA_ROPE_NTK 2
+#define PLORA_ROPE_BANDS 3
+#define PLORA_ROPE_RAMP 4
+#define PLORA_ROPE_MAX_DIM 512
+typedef struct {
+    int32_t rot_dim, scaling;
+    double base, factor, orig_len, low, high, magnitude;
+} plora_rope_desc;
+PLORA_API plora_status plora_rope_table(const plora_rope_desc *desc, int32_t max_pos, float *table_dev, void *stream);
+
+/* Rotates q and k to their positions, writes q to q_out, and k and v to their cache slots, in one pass: the fp32 y of the
+ * deltas (or 16-bit projections) goes in, what plora_attn_paged reads comes out, rounded once.
+ * The first rot_dim of the head's dims turn (0: none do), the rest pass through.  HALF pairs dims (i, i + rot_dim / 2),
+ * INTERLEAVED (2 i, 2 i + 1):  (a, b) -> (a cos - b sin, b cos + a sin).
+ * q, k, v    [n_tok][heads][head_dim], q_stride / k_stride / v_stride elements between tokens (0: packed), so that they
+ *            may be parts of one fused row; in_type: PLORA_INPUT_FP32, or the same as out_type
+ * q_out      [n_tok][n_q_heads][head_dim], packed; may be q itself if in_type == out_type and q is packed
+ * positions  int32 [n_tok]; below 0: a padding token, its q_out row is zeroed and nothing goes to the cache
+ * slots      int32 [n_tok]; below 0: nothing goes to the cache.  Slots of a call must be distinct.
+ * status     device int32 or NULL: a sticky word that gets PLORA_ERR_INVALID_ARG if a position was >= max_pos (the token
+ *            is then treated as padding) or a slot lay beyond the cache (it is not written)
+ * n_q_heads = 0 or n_kv_heads = 0 leaves out q or k and v.  Any strides and alignments of whole elements work; the
+ * 16-byte ones are fast. */
+#define PLORA_INPUT_FP32 2
+#define PLORA_ROPE_HALF 0
+#define PLORA_ROPE_INTERLEAVED 1
+typedef struct {
+    int32_t in_type, out_type, layout;
+    int32_t n_tok, n_q_heads, n_kv_heads, head_dim, rot_dim, max_pos, page_size, n_pages;
+    int64_t q_stride, k_stride, v_stride, page_stride;
+    const void *q, *k, *v;
+    const int32_t *positions, *slots;
+    const float *table;
+    void *q_out, *k_cache, *v_cache;
+    int32_t *status;
+} plora_rope_cache_args;
+PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args *args, void *stream);
+
+/* Attention of new tokens over the paged cache, O = softmax(score) V per query head, with
+ *     score = scale * q k,  then  softcap * tanh(score / softcap)  if softcap > 0,
+ *     then  score - slopes[query head] * |position - key index|    if slopes is given,
+ * over the keys lo <= j < hi of the token's own request.  A token whose interval is empty gets a zero row.
+ *
+ * tok_start  int32 [n_req + 1]: query tokens of request r are [tok_start[r], tok_start[r + 1]); the last one stands at
+ *            position kv_len[r] - 1.  NULL: one token per request (n_tok == n_req).
+ * kv_len     int32 [n_req], the step's own tokens included (clamped to min(max_blocks, n_pages) * page_size).
+ * key_lo     int32 [n_tok] or NULL (0): where a token's document, or its sliding window, begins
+ * key_hi     int32 [n_tok] or NULL (its position + 1): where its keys end, e.g. the end of a prefix that sees itself both
+ *            ways; clamped to kv_len
+ * groups     group_start int32 [n_groups + 1] (requests [group_start[g], group_start[g + 1])) and prefix_len int32
+ *            [n_groups]: the first prefix_len[g] tokens of the group's requests are the same; where every request of a
+ *            group has one token they are read once, for all, through the first request's block table.  (With LoRA on
+ *            k and v, requests share a prefix if they share their adapter: groups are then the bucket's segments.)
+ *            The result does not depend on the grouping beyond rounding.  n_groups = 0: none.
+ * type       PLORA_INPUT_BF16 / FP16 of q, K, V and out; products and sums in fp32, weights rounded to the type for the
+ *            second product.
+ * q [n_tok][n_q_heads][head_dim] (q_stride elements between tokens, 0: packed), out packed; query head h reads KV
+ * head h / (n_q_heads / n_kv_heads).  head_dim 64 or 128; page_size 16, 32, 64 or 128; at most 16 query heads per KV
+ * head.  q, K, V and out 16-byte aligned, strides multiples of 8.  Cache slots at or beyond kv_len may hold anything.
+ * A block table entry outside [0, n_pages) that is needed reads as zeros and sets PLORA_ERR_INVALID_ARG in the status word.
+ * workspace  256-byte aligned, at least plora_attn_paged_workspace_bytes(...) bytes (max_blocks there: min(max_blocks,
+ *            n_pages)); first 256 bytes zero before the first call, scratch between calls, one stream at a time; the
+ *            status word and diagnostics are those of plora_attn_decode (plora_attn_status, plora_attn_set_debug). */
+typedef struct {
+    int32_t type;
+    int32_t n_tok, n_req, n_groups, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_blocks;
+    int64_t q_stride, page_stride;
+    const void *q, *k_cache, *v_cache;
+    const int32_t *block_table, *kv_len, *tok_start, *group_start, *prefix_len, *key_lo, *key_hi;
+    const float *slopes;
+    float scale, softcap;
+    void *out, *workspace;
+    size_t workspace_bytes;
+} plora_paged_attn;
+PLORA_API size_t plora_attn_paged_workspace_bytes(int32_t n_tok, int32_t n_req, int32_t n_q_heads, int32_t n_kv_heads,
+                                                  int32_t head_dim, int32_t page_size, int32_t max_blocks);
+PLORA_API plora_status plora_attn_paged(const plora_paged_attn *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

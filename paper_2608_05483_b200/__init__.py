@@ -11,4 +11,7 @@ from .binding import (  # noqa: F401
     plora_register_pool, plora_set_path, plora_shrink, plora_shrink_m16, status_string,
     attn_decode, plora_attn_decode, plora_attn_set_debug, plora_attn_status, plora_attn_workspace_bytes,
     plora_set_test_hook, plora_set_wait_limit, plora_set_inputs_resident, plora_stream_read, HOOK_NONE, HOOK_WITHHOLD_RELEASE, HOOK_MAX_CYCLES,
+    INPUT_BF16, INPUT_FP16, INPUT_FP32, ROPE_BANDS, ROPE_HALF, ROPE_INTERLEAVED, ROPE_LINEAR, ROPE_NONE, ROPE_NTK, ROPE_RAMP,
+    KvPlan, PagedAttn, RopeCacheArgs, RopeDesc, attn_paged, attn_paged_workspace, kv_plan, plora_attn_paged,
+    plora_attn_paged_workspace_bytes, plora_kv_plan, plora_rope_cache, plora_rope_table, rope_cache, rope_table,
 )

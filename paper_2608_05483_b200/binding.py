@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 from pathlib import Path
+from typing import Any, NamedTuple
 
 import numpy as np
 
@@ -35,7 +36,12 @@ EXPORTS = (
     "plora_lora_delta_host", "plora_lora_delta_host_async", "plora_host_sync", "plora_lora_delta_noalloc", "plora_set_path", "plora_device_status", "plora_launch_count", "plora_status_string",
     "plora_cost_model", "plora_attn_workspace_bytes", "plora_attn_decode", "plora_attn_status", "plora_attn_set_debug",
     "plora_set_wait_limit", "plora_set_test_hook", "plora_set_inputs_resident", "plora_stream_read",
+    "plora_kv_plan", "plora_rope_table", "plora_rope_cache", "plora_attn_paged_workspace_bytes", "plora_attn_paged",
 )
+
+INPUT_BF16, INPUT_FP16, INPUT_FP32 = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
 
 HOOK_NONE, HOOK_WITHHOLD_RELEASE, HOOK_MAX_CYCLES = 0, 1, 1 << 24
 
@@ -57,6 +63,29 @@ class CostHw(ctypes.Structure):
 class CostTerms(ctypes.Structure):
     _fields_ = [("t_gpu", ctypes.c_double * 4), ("t_dev_cpt", ctypes.c_double * 4), ("t_dev_trs", ctypes.c_double * 4),
                 ("t_lora_gpu", ctypes.c_double), ("t_lora_dev", ctypes.c_double), ("t_lora", ctypes.c_double)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32)] + [
+        (n, ctypes.c_double) for n in ("base", "factor", "orig_len", "low", "high", "magnitude")]
+
+
+class RopeCacheArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("in_type", "out_type", "layout", "n_tok", "n_q_heads", "n_kv_heads", "head_dim",
+                                               "rot_dim", "max_pos", "page_size", "n_pages")]
+                + [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "page_stride")]
+                + [(n, ctypes.c_void_p) for n in ("q", "k", "v", "positions", "slots", "table", "q_out", "k_cache", "v_cache",
+                                                  "status")])
+
+
+class PagedAttn(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("type", "n_tok", "n_req", "n_groups", "n_q_heads", "n_kv_heads", "head_dim",
+                                               "page_size", "n_pages", "max_blocks")]
+                + [(n, ctypes.c_int64) for n in ("q_stride", "page_stride")]
+                + [(n, ctypes.c_void_p) for n in ("q", "k_cache", "v_cache", "block_table", "kv_len", "tok_start", "group_start",
+                                                  "prefix_len", "key_lo", "key_hi", "slopes")]
+                + [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("out", ctypes.c_void_p),
+                   ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)])
 
 
 class PloraError(RuntimeError):
@@ -124,6 +153,11 @@ def load(build_if_missing: bool = True):
         "plora_stream_read": (i32, [vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp]),
         "plora_cost_model": (i32, [ctypes.POINTER(CostHw), i32, vp, vp, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                    ctypes.POINTER(CostTerms)]),
+        "plora_kv_plan": (i32, [vp, vp, i32, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
+        "plora_rope_table": (i32, [ctypes.POINTER(RopeDesc), i32, vp, vp]),
+        "plora_rope_cache": (i32, [ctypes.POINTER(RopeCacheArgs), vp]),
+        "plora_attn_paged_workspace_bytes": (ctypes.c_size_t, [i32] * 7),
+        "plora_attn_paged": (i32, [ctypes.POINTER(PagedAttn), vp]),
     }
     for name in EXPORTS:
         fn = getattr(lib, name)  # AttributeError here = the library does not export what the header declares
@@ -212,6 +246,188 @@ def attn_decode(q, k_cache, v_cache, kv_len, scale, out=None, workspace=None, st
     _check(plora_attn_decode(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), kv_len.data_ptr(), B, Lmax, Hkv, Hq // Hkv,
                              d, scale, out.data_ptr(), workspace.data_ptr(), int(workspace.numel()), _stream_handle(stream)),
            "plora_attn_decode")
+    return out, workspace
+
+
+# ---- serving over a paged KV cache ------------------------------------------------------
+def plora_kv_plan(kv_len_ptr, new_len_ptr, n_req, page_size, free_ptr, n_free, cursor_in_ptr, table_ptr, max_blocks, max_tokens,
+                  tok_start_ptr, positions_ptr, tok_req_ptr, slots_ptr, kv_len_out_ptr, cursor_out_ptr, stream=0):
+    return load().plora_kv_plan(kv_len_ptr, new_len_ptr, n_req, page_size, free_ptr, n_free, cursor_in_ptr, table_ptr, max_blocks,
+                                max_tokens, tok_start_ptr, positions_ptr, tok_req_ptr, slots_ptr, kv_len_out_ptr, cursor_out_ptr,
+                                stream)
+
+
+def plora_rope_table(desc: RopeDesc, max_pos: int, table_ptr: int, stream=0):
+    return load().plora_rope_table(ctypes.byref(desc), max_pos, table_ptr, stream)
+
+
+def plora_rope_cache(args: RopeCacheArgs, stream=0):
+    return load().plora_rope_cache(ctypes.byref(args), stream)
+
+
+def plora_attn_paged_workspace_bytes(n_tok, n_req, n_q_heads, n_kv_heads, head_dim, page_size, max_blocks) -> int:
+    return int(load().plora_attn_paged_workspace_bytes(n_tok, n_req, n_q_heads, n_kv_heads, head_dim, page_size, max_blocks))
+
+
+def plora_attn_paged(args: PagedAttn, stream=0):
+    return load().plora_attn_paged(ctypes.byref(args), stream)
+
+
+class KvPlan(NamedTuple):
+    """What kv_plan writes (int32 device tensors): tok_start [n_req + 1], positions / tok_req / slots [max_tokens],
+    kv_len [n_req] and cursor [1] after the step."""
+    tok_start: Any
+    positions: Any
+    tok_req: Any
+    slots: Any
+    kv_len: Any
+    cursor: Any
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(name, t, shape):
+    """An int32 CUDA tensor, packed, of this shape (None in the shape: any size)."""
+    import torch
+    _need(t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.dim() == len(shape)
+          and all(w is None or w == n for w, n in zip(shape, t.shape)),
+          f"{name}: int32 CUDA tensor {list(shape)} expected, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _type16(t):
+    import torch
+    _need(t.dtype in (torch.bfloat16, torch.float16), f"bfloat16 or float16 expected, got {t.dtype}")
+    return INPUT_BF16 if t.dtype is torch.bfloat16 else INPUT_FP16
+
+
+def _heads(name, t):
+    """Strides of a [n_tok, heads, head_dim] tensor whose heads are packed: elements between tokens."""
+    _need(t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] <= 1 or t.stride(1) == t.shape[2]),
+          f"{name}: CUDA tensor [n_tok, heads, head_dim] with packed heads expected")
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1] * t.shape[2])
+
+
+def _cache(k_cache, v_cache):
+    """Elements between pages of a cache pair [n_pages, n_kv_heads, page_size, head_dim] whose pages are packed."""
+    _need(k_cache.is_cuda and v_cache.is_cuda and k_cache.dim() == 4 and k_cache.shape == v_cache.shape
+          and k_cache.dtype == v_cache.dtype and k_cache.stride() == v_cache.stride(),
+          "k_cache, v_cache: alike CUDA tensors [n_pages, n_kv_heads, page_size, head_dim] expected")
+    n, h, s, d = k_cache.shape
+    _need(k_cache[0].is_contiguous(), "k_cache, v_cache: a page's values must be packed")
+    return int(k_cache.stride(0)) if n > 1 else h * s * d
+
+
+def kv_plan(kv_len, new_len, page_size: int, free_pages, block_table, max_tokens: int, cursor=None, out=None, stream=None) -> KvPlan:
+    """Pages, slots and positions of a step (plora_kv_plan): kv_len, new_len int32 [n_req], free_pages int32 [n_free],
+    block_table int32 [n_req, max_blocks] (updated in place), cursor int32 [1] or None (the free list's first unused
+    entry; the result's cursor is the next step's).  out: a KvPlan of an earlier step, to be overwritten."""
+    import torch
+    n = int(kv_len.shape[0])
+    if out is None:
+        buf = torch.empty(2 * n + 2 + 3 * max_tokens, dtype=torch.int32, device=kv_len.device)
+        at, parts = 0, []
+        for size in (n + 1, max_tokens, max_tokens, max_tokens, n, 1):
+            parts.append(buf[at:at + size])
+            at += size
+        out = KvPlan(*parts)
+    _check(plora_kv_plan(_ints("kv_len", kv_len, (n,)), _ints("new_len", new_len, (n,)), n, int(page_size),
+                         _ints("free_pages", free_pages, (None,)), int(free_pages.shape[0]),
+                         _ints("cursor", cursor, (1,)) if cursor is not None else None,
+                         _ints("block_table", block_table, (n, None)), int(block_table.shape[1]), int(max_tokens),
+                         _ints("tok_start", out.tok_start, (n + 1,)), _ints("positions", out.positions, (max_tokens,)),
+                         _ints("tok_req", out.tok_req, (max_tokens,)), _ints("slots", out.slots, (max_tokens,)),
+                         _ints("kv_len", out.kv_len, (n,)), _ints("cursor", out.cursor, (1,)), _stream_handle(stream)),
+           "plora_kv_plan")
+    return out
+
+
+_SCALINGS = {"none": ROPE_NONE, "linear": ROPE_LINEAR, "ntk": ROPE_NTK, "bands": ROPE_BANDS, "ramp": ROPE_RAMP}
+
+
+def rope_table(rot_dim: int, max_pos: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+               orig_len: float = 0.0, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0, device="cuda", stream=None):
+    """The fp32 table [max_pos, rot_dim // 2, 2] of cosines and sines (plora_rope_table)."""
+    import torch
+    _need(scaling in _SCALINGS, f"scaling: one of {sorted(_SCALINGS)} expected, got {scaling!r}")
+    table = torch.empty((max(0, int(max_pos)), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
+    d = RopeDesc(int(rot_dim), _SCALINGS[scaling], base, factor, orig_len, low, high, magnitude)
+    _check(plora_rope_table(d, int(max_pos), table.data_ptr(), _stream_handle(stream)), "plora_rope_table")
+    return table
+
+
+def rope_cache(q, k, v, positions, slots, table, k_cache, v_cache, q_out=None, interleaved: bool = False, status=None, stream=None):
+    """Rotates q and k, writes k and v to their cache slots and returns the rotated q (plora_rope_cache).  q, k, v:
+    [n_tok, heads, head_dim], fp32 or the cache's type, rows of any stride; table: rope_table's (None: nothing turns)."""
+    import torch
+    n, hq, d = q.shape
+    hk = int(k.shape[1])
+    out_type = _type16(k_cache)
+    page_stride = _cache(k_cache, v_cache)
+    _need(k.dtype == q.dtype and v.dtype == q.dtype and q.dtype in (torch.float32, k_cache.dtype),
+          "q, k, v: one type, float32 or the cache's, expected")
+    _need(k.shape == (n, hk, d) and v.shape == k.shape and k_cache.shape[1] == hk and k_cache.shape[3] == d,
+          "q, k, v and the caches: shapes do not agree")
+    if q_out is None:
+        q_out = torch.empty((n, hq, d), dtype=k_cache.dtype, device=q.device)
+    _need(q_out.dtype == k_cache.dtype and q_out.shape == q.shape and q_out.is_contiguous(), "q_out: packed, of the cache's type, expected")
+    if table is not None:
+        _need(table.dtype is torch.float32 and table.is_cuda and table.is_contiguous() and table.dim() == 3 and table.shape[2] == 2,
+              "table: float32 [max_pos, rot_dim // 2, 2] expected")
+    a = RopeCacheArgs(INPUT_FP32 if q.dtype is torch.float32 else out_type, out_type, ROPE_INTERLEAVED if interleaved else ROPE_HALF,
+                      n, hq, hk, d, 0 if table is None else 2 * int(table.shape[1]), 0 if table is None else int(table.shape[0]),
+                      int(k_cache.shape[2]), int(k_cache.shape[0]), _heads("q", q), _heads("k", k), _heads("v", v), page_stride,
+                      q.data_ptr(), k.data_ptr(), v.data_ptr(), _ints("positions", positions, (n,)), _ints("slots", slots, (n,)),
+                      None if table is None else table.data_ptr(), q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                      None if status is None else _ints("status", status, (1,)))
+    _check(plora_rope_cache(a, _stream_handle(stream)), "plora_rope_cache")
+    return q_out
+
+
+def attn_paged_workspace(q, k_cache, n_req: int, max_blocks=None):
+    """A zeroed workspace for attn_paged on batches of q's size over this cache (max_blocks: the block table's width, None:
+    any)."""
+    import torch
+    n_pages, hk, page, d = k_cache.shape
+    need = plora_attn_paged_workspace_bytes(max(1, int(q.shape[0])), int(n_req), int(q.shape[1]), hk, d, page,
+                                            n_pages if max_blocks is None else min(n_pages, int(max_blocks)))
+    if need == 0:
+        raise PloraError(ERR_UNSUPPORTED, "plora_attn_paged_workspace_bytes")
+    return torch.zeros(need, dtype=torch.uint8, device=q.device)
+
+
+def attn_paged(q, k_cache, v_cache, block_table, kv_len, scale: float, tok_start=None, group_start=None, prefix_len=None,
+               softcap: float = 0.0, slopes=None, key_lo=None, key_hi=None, out=None, workspace=None, stream=None):
+    """Attention of the new tokens q [n_tok, n_q_heads, head_dim] over the paged cache (plora_attn_paged); returns
+    (out, workspace).  tok_start None: one token per request.  Pass the returned workspace back in to reuse it."""
+    import torch
+    n, hq, d = q.shape
+    n_pages, hk, page, _ = k_cache.shape
+    n_req = int(kv_len.shape[0])
+    page_stride = _cache(k_cache, v_cache)
+    _need(q.dtype == k_cache.dtype and k_cache.shape[3] == d and hk > 0 and hq % hk == 0, "q and the caches do not agree")
+    table_ptr = _ints("block_table", block_table, (n_req, None))
+    if out is None:
+        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+    _need(out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous() and out.is_cuda, "out: packed, of q's shape and type, expected")
+    if workspace is None:
+        workspace = attn_paged_workspace(q, k_cache, n_req, block_table.shape[1])
+    n_groups = 0 if group_start is None else int(group_start.shape[0]) - 1
+    _need(n_groups >= 0 and (group_start is None) == (prefix_len is None), "group_start and prefix_len go together")
+    if slopes is not None:
+        _need(slopes.dtype is torch.float32 and slopes.is_cuda and slopes.is_contiguous() and slopes.shape == (hq,),
+              "slopes: float32 CUDA tensor [n_q_heads] expected")
+    opt = lambda name, t, shape: None if t is None else _ints(name, t, shape)
+    a = PagedAttn(_type16(q), n, n_req, n_groups, hq, hk, d, page, n_pages, int(block_table.shape[1]), _heads("q", q), page_stride,
+                  q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table_ptr, _ints("kv_len", kv_len, (n_req,)),
+                  opt("tok_start", tok_start, (n_req + 1,)), opt("group_start", group_start, (None,)),
+                  opt("prefix_len", prefix_len, (n_groups,)), opt("key_lo", key_lo, (n,)), opt("key_hi", key_hi, (n,)),
+                  None if slopes is None else slopes.data_ptr(), scale, softcap, out.data_ptr(), workspace.data_ptr(),
+                  int(workspace.numel()))
+    _check(plora_attn_paged(a, _stream_handle(stream)), "plora_attn_paged")
     return out, workspace
 
 

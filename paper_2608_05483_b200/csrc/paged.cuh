@@ -1,0 +1,197 @@
+// Attention over a paged KV cache: what the kernels of plora_attn_paged share.
+//
+// The batch is cut into units.  A unit is a run of consecutive query tokens (all query heads of one KV
+// head: ntok * G rows) against a range of keys of one block table; a work item is a unit and a KV head.
+// A request's tokens against the keys that are its own make units, and so do the tokens of a group of
+// requests against the keys of their common prefix, which are then read once for the whole group.
+// Where a token's keys are dealt out to more than one unit, each leaves a partial result (maximum m,
+// sum l, unnormalised output o, in the base-2 domain), and the merge kernel combines them:
+//     O = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i,   m = max_i m_i.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "plora.h"
+
+namespace plora {
+namespace paged {
+
+struct Unit {       // 32 bytes
+    int32_t tok0, ntok;   // query tokens
+    int32_t req;          // row of the block table
+    int32_t k0, k1;       // keys [k0, k1)
+    int32_t part;         // first partial (counted in tokens), -1: the unit writes the output itself
+    int32_t pad_[2];
+};
+static_assert(sizeof(Unit) == 32, "a unit is two 16-byte words");
+
+struct TokInfo {    // 16 bytes: keys [lo, hi) are visible to the token, which stands at pos
+    int32_t lo, hi, pos, pad_;
+};
+
+// How the partial results of a token lie: n[i] of them from number base[i] on, stride[i] apart; i = 0 the
+// token's own keys, i = 1 its group's prefix.  n[0] < 0: its unit writes the output itself.
+struct TokMerge {   // 32 bytes
+    int32_t base[2], n[2], stride[2], pad_[2];
+};
+
+// Workspace header (256 bytes, zero before the first call): word 0 the sticky status word; words 8 and
+// 10 the test hook and the wait limit of plora_attn_set_debug; the rest is rewritten by every call.
+constexpr int kSmallUnitsWord = 1, kBigUnitsWord = 2, kSmallNextWord = 3, kBigNextWord = 4;
+constexpr int kHookWord = 8, kLimitWord = 10;
+constexpr long long kWaitCycles = 4000000000ll;   // default limit of a wait: about two seconds of SM clock
+
+struct Params {
+    int32_t* header;
+    Unit* small_units;
+    Unit* big_units;
+    TokInfo* tok_info;
+    TokMerge* tok_merge;
+    float2* part_ml;          // [partial token][query head] {m, l}
+    float* part_o;            // [partial token][query head][D]
+    int32_t cap_small, cap_big, cap_part;
+
+    const uint16_t* q;
+    uint16_t* out;
+    long long q_stride;       // elements between tokens
+    const int32_t* block_table;
+    const int32_t* kv_len;
+    const int32_t* tok_start;     // nullptr: one token per request
+    const int32_t* group_start;   // nullptr: no groups
+    const int32_t* prefix_len;
+    const int32_t* key_lo;
+    const int32_t* key_hi;
+    const float* slopes;
+    int32_t n_tok, n_req, n_groups, n_q_heads, n_kv_heads, G;
+    int32_t page_size, page_shift, n_pages, max_blocks;
+    int32_t max_kv;           // min(max_blocks, n_pages) * page_size
+    float scale_log2e;        // softmax scale times log2(e): scores live in the base-2 domain
+    float cap_in, cap_log2e;  // capped scores: cap_log2e * tanh(cap_in * qk), cap_in already times 2 log2(e)
+};
+
+constexpr int kSmallRows = 16;     // rows of a unit the mma.sync kernel takes
+
+// ---- PTX wrappers ---------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void mbar_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Every wait is bounded.  When one runs out, the CTA's abort flag goes up, the status word gets
+// PLORA_ERR_TIMEOUT, and every role leaves its loop.
+struct WaitCtl {
+    volatile int* abort_flag;
+    int32_t* header;
+};
+__device__ __forceinline__ long long wait_limit(const int32_t* header) {
+    const long long v = *reinterpret_cast<const volatile long long*>(header + kLimitWord);
+    return v > 0 ? v : kWaitCycles;
+}
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, WaitCtl w) {
+    const long long t0 = clock64();
+    long long limit = 0;
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+        if (*w.abort_flag) return false;
+        if (limit == 0) limit = wait_limit(w.header);
+        if (clock64() - t0 > limit) break;
+    }
+    *w.abort_flag = 1;
+    __threadfence_block();
+    atomicCAS(w.header, 0, PLORA_ERR_TIMEOUT);
+    return false;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const WaitCtl& w) {
+    if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait_slow(bar, parity, w);
+}
+// A last look at a barrier before a CTA leaves, whatever the abort flag says: copies in flight must land first.
+__device__ __forceinline__ bool mbar_drain(uint32_t bar, uint32_t parity, long long limit) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity))
+        if (clock64() - t0 > limit) return false;
+    return true;
+}
+__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+// Box of the 4-D cache tensor [page][KV head][slot][dim]: 64 dims of consecutive slots, 128-byte rows, swizzled.
+__device__ __forceinline__ void tma_box4(uint32_t dst, const CUtensorMap* tm, int dim, int slot, int head, int page,
+                                         uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tm)), "r"(dim), "r"(slot), "r"(head), "r"(page), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// two floats -> one word of two 16-bit values, round to nearest even (lo in the lower half)
+template <bool FP16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    uint32_t r;
+    if (FP16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Score in the base-2 domain from the raw product: scale, cap, bias by distance.  tanh(x) is taken as
+// 1 - 2 / (1 + e^2x): the fast tanh instruction's 2^-11 would be multiplied by the cap before it reaches an exponential.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float score(const Params& p, float qk, float slope, int dist) {
+    float s;
+    if (CAP) s = fmaf(-2.f * p.cap_log2e, rcp(1.f + ex2(qk * p.cap_in)), p.cap_log2e);
+    else s = qk * p.scale_log2e;
+    if (BIAS) s = fmaf(-slope, fabsf((float)dist), s);
+    return s;
+}
+
+// ---- launches -----------------------------------------------------------------------------------------
+cudaError_t launch_small(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim, bool fp16,
+                         int sm_count, cudaStream_t st);
+cudaError_t launch_pdl(const void* kern, dim3 grid, dim3 block, size_t smem, cudaStream_t st, void** args);
+
+}  // namespace paged
+}  // namespace plora

@@ -1,0 +1,481 @@
+// Attention over a paged KV cache: the plan (which units a batch is cut into), the merge, and the C entry.
+//
+// The plan is made on the device, from lengths that only the device knows, so a step needs no copy to the
+// host and can be captured in a graph.  Its first CTA writes the units; the others write what every token may see.
+#include <limits.h>
+
+#include "paged.cuh"
+
+namespace plora {
+namespace paged {
+
+cudaError_t launch_pdl(const void* kern, dim3 grid, dim3 block, size_t smem, cudaStream_t st, void** args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelExC(&cfg, kern, args);
+}
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatever the device has: it sizes the workspace
+constexpr int kSmallItems = kPlanSms * 2 * 8;   // aimed-at items of the small kernel (two CTAs per SM)
+constexpr int kSmallMinKeys = 128;     // no split shorter than this
+constexpr int kGroupCache = 2048;      // group starts held in shared memory
+
+struct Sums {        // counts that the scan carries along
+    int small, part;
+};
+
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+
+// What the plan knows of a request: its tokens, its keys, and how many of them belong to its group's prefix.
+struct Req {
+    int tok0, n, kv, pre;
+};
+
+__device__ __forceinline__ void token_range(const Params& p, int r, int& tok0, int& n) {
+    if (p.tok_start) {
+        tok0 = clampi(p.tok_start[r], 0, p.n_tok);
+        n = clampi(p.tok_start[r + 1], tok0, p.n_tok) - tok0;
+    } else {
+        tok0 = r;
+        n = 1;
+    }
+}
+__device__ __forceinline__ int kv_of(const Params& p, int r) { return clampi(p.kv_len[r], 0, p.max_kv); }
+
+// The group's common prefix if its tokens read it together: more than one request, one token each.
+__device__ __forceinline__ int group_prefix(const Params& p, int s, int e) {
+    if (e - s < 2) return 0;
+    int t0, t1, n;
+    token_range(p, s, t0, n);
+    token_range(p, e - 1, t1, n);
+    return t1 + n - t0 == e - s ? 1 : 0;
+}
+
+// Keys [lo, hi) visible to the token at position pos of a cache of kv tokens.
+__device__ __forceinline__ TokInfo visible(const Params& p, int t, int pos, int kv) {
+    TokInfo ti;
+    ti.pos = pos;
+    ti.lo = p.key_lo ? max(p.key_lo[t], 0) : 0;
+    ti.hi = p.key_hi ? min(p.key_hi[t], kv) : min(pos + 1, kv);
+    ti.pad_ = 0;
+    return ti;
+}
+
+__device__ __forceinline__ Sums scan_exclusive(Sums v, Sums& total, Sums* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Sums in = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int a = __shfl_up_sync(0xffffffffu, in.small, d), b = __shfl_up_sync(0xffffffffu, in.part, d);
+        if (lane >= d) {
+            in.small += a;
+            in.part += b;
+        }
+    }
+    __syncthreads();
+    if (lane == 31) warp_sums[warp] = in;
+    __syncthreads();
+    Sums before{0, 0}, all{0, 0};
+    for (int w = 0; w < kPlanThreads / 32; ++w) {
+        const Sums x = warp_sums[w];
+        if (w < warp) {
+            before.small += x.small;
+            before.part += x.part;
+        }
+        all.small += x.small;
+        all.part += x.part;
+    }
+    total = all;
+    return Sums{before.small + in.small - v.small, before.part + in.part - v.part};
+}
+
+__device__ __forceinline__ long long sum_all(long long v, long long* red) {
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    long long s = 0;
+    for (int w = 0; w < kPlanThreads / 32; ++w) s += red[w];
+    return s;
+}
+
+__device__ void write_token_info(const Params& p) {
+    const int t = (blockIdx.x - 1) * kPlanThreads + threadIdx.x;
+    if (t >= p.n_tok) return;
+    int r = t, pos, kv;
+    if (p.tok_start) {
+        int lo = 0, hi = p.n_req;        // the last request whose first token is not behind t
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (p.tok_start[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        r = lo;
+        const int end = p.tok_start[r + 1];
+        kv = kv_of(p, r);
+        if (t >= end || t < p.tok_start[r]) {        // a token of no request: nothing to see
+            p.tok_info[t] = TokInfo{0, 0, 0, 0};
+            p.tok_merge[t] = TokMerge{{0, 0}, {0, 0}, {0, 0}, {0, 0}};   // a zero row
+            return;
+        }
+        pos = kv - (end - t);
+    } else {
+        kv = kv_of(p, r);
+        pos = kv - 1;
+    }
+    p.tok_info[t] = visible(p, t, pos, kv);
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
+    grid_launch_dependents();
+    if (blockIdx.x > 0) {
+        write_token_info(p);
+        return;
+    }
+    __shared__ Sums warp_sums[kPlanThreads / 32];
+    __shared__ long long red[kPlanThreads / 32];
+    __shared__ int s_group[kGroupCache + 1];
+    const int tid = threadIdx.x;
+    const int TB = max(1, kSmallRows / p.G);      // tokens of a unit
+    const bool cached = p.n_groups <= kGroupCache;
+    for (int g = tid; p.n_groups > 0 && cached && g <= p.n_groups; g += kPlanThreads) s_group[g] = clampi(p.group_start[g], 0, p.n_req);
+    __syncthreads();
+    auto gstart = [&](int g) { return cached ? s_group[g] : clampi(p.group_start[g], 0, p.n_req); };
+    auto prefix_of = [&](int g) {                  // tokens of the prefix that group g reads together, 0: none
+        const int s = gstart(g), e = gstart(g + 1);
+        if (!group_prefix(p, s, e)) return 0;
+        return clampi(p.prefix_len[g], 0, kv_of(p, s));
+    };
+    auto request = [&](int r) {
+        Req q;
+        token_range(p, r, q.tok0, q.n);
+        q.kv = kv_of(p, r);
+        q.pre = 0;
+        if (p.n_groups > 0) {
+            int lo = 0, hi = p.n_groups;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (gstart(mid) <= r) lo = mid;
+                else hi = mid;
+            }
+            if (gstart(lo) <= r && r < gstart(lo + 1)) q.pre = prefix_of(lo);
+        }
+        return q;
+    };
+    // keys of block b of a request: from the first that one of its tokens sees (behind the shared prefix) to the last
+    auto block_keys = [&](const Req& q, int b, int& k0, int& k1) {
+        k0 = INT_MAX;
+        k1 = 0;
+        for (int t = q.tok0 + b * TB; t < q.tok0 + min(q.n, (b + 1) * TB); ++t) {
+            const TokInfo ti = visible(p, t, q.kv - (q.tok0 + q.n - t), q.kv);
+            if (ti.lo < ti.hi) {
+                k0 = min(k0, ti.lo);
+                k1 = max(k1, ti.hi);
+            }
+        }
+        k0 = max(k0, q.pre);
+        k1 = max(k0, k1);
+        if (k0 == INT_MAX) k0 = k1 = 0;
+    };
+
+    // how many keys there are to read in all, over the units: the split length follows from it
+    long long keys = 0;
+    for (int r = tid; r < p.n_req; r += kPlanThreads) {
+        const Req q = request(r);
+        for (int b = 0; b * TB < q.n; ++b) {
+            int k0, k1;
+            block_keys(q, b, k0, k1);
+            keys += k1 - k0;
+        }
+    }
+    for (int g = tid; g < p.n_groups; g += kPlanThreads) {
+        const int s = gstart(g), e = gstart(g + 1);
+        keys += (long long)prefix_of(g) * ((e - s + TB - 1) / TB);
+    }
+    keys = sum_all(keys, red);
+    const long long per = (keys * p.n_kv_heads + kSmallItems - 1) / kSmallItems;
+    const int chunk = (int)max((long long)kSmallMinKeys, (per + 63) / 64 * 64);
+
+    Sums carry{0, 0};
+    // the groups' prefixes: always partial results
+    for (int g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
+        const int g = g0 + tid;
+        int pre = 0, s = 0, n = 0, tok0 = 0, nn;
+        if (g < p.n_groups) {
+            s = gstart(g);
+            n = gstart(g + 1) - s;
+            pre = prefix_of(g);
+            if (pre > 0) token_range(p, s, tok0, nn);
+        }
+        const int splits = (pre + chunk - 1) / chunk, blocks = pre > 0 ? (n + TB - 1) / TB : 0;
+        Sums total;
+        Sums at = scan_exclusive(Sums{splits * blocks, splits * (pre > 0 ? n : 0)}, total, warp_sums);
+        at.small += carry.small;
+        at.part += carry.part;
+        if (pre > 0 && (at.small + splits * blocks > p.cap_small || at.part + splits * n > p.cap_part)) {
+            atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
+            for (int t = 0; t < n; ++t) p.tok_merge[tok0 + t].n[1] = 0;
+        } else if (pre > 0) {
+            for (int b = 0; b < blocks; ++b) {
+                const int nt = min(TB, n - b * TB);
+                for (int i = 0; i < splits; ++i)
+                    p.small_units[at.small + b * splits + i] =
+                        Unit{tok0 + b * TB, nt, s, i * chunk, min(pre, (i + 1) * chunk), at.part + i * n + b * TB, {0, 0}};
+                for (int t = 0; t < nt; ++t) {
+                    TokMerge& m = p.tok_merge[tok0 + b * TB + t];
+                    m.base[1] = at.part + b * TB + t;
+                    m.n[1] = splits;
+                    m.stride[1] = n;
+                }
+            }
+        }
+        carry.small += total.small;
+        carry.part += total.part;
+    }
+    __syncthreads();
+    // the requests' own keys
+    for (int r0 = 0; r0 < p.n_req; r0 += kPlanThreads) {
+        const int r = r0 + tid;
+        Req q{0, 0, 0, 0};
+        if (r < p.n_req) q = request(r);
+        Sums want{0, 0};
+        for (int b = 0; b * TB < q.n; ++b) {
+            int k0, k1;
+            block_keys(q, b, k0, k1);
+            const int splits = (k1 - k0 + chunk - 1) / chunk;
+            want.small += splits;
+            if (splits > 1 || q.pre > 0) want.part += splits * min(TB, q.n - b * TB);
+        }
+        Sums total;
+        Sums at = scan_exclusive(want, total, warp_sums);
+        at.small += carry.small;
+        at.part += carry.part;
+        if (at.small + want.small > p.cap_small || at.part + want.part > p.cap_part) {
+            atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
+            for (int t = 0; t < q.n; ++t) p.tok_merge[q.tok0 + t] = TokMerge{{0, 0}, {0, 0}, {0, 0}, {0, 0}};
+            q.n = 0;
+        }
+        for (int b = 0; b * TB < q.n; ++b) {
+            int k0, k1;
+            block_keys(q, b, k0, k1);
+            const int splits = (k1 - k0 + chunk - 1) / chunk, nt = min(TB, q.n - b * TB);
+            const bool partial = splits > 1 || q.pre > 0;
+            for (int i = 0; i < splits; ++i)
+                p.small_units[at.small + i] = Unit{q.tok0 + b * TB, nt, r, k0 + i * chunk, min(k1, k0 + (i + 1) * chunk),
+                                                   partial ? at.part + i * nt : -1, {0, 0}};
+            for (int t = 0; t < nt; ++t) {
+                TokMerge& m = p.tok_merge[q.tok0 + b * TB + t];
+                m.base[0] = at.part + t;
+                m.n[0] = splits == 1 && !partial ? -1 : splits;
+                m.stride[0] = nt;
+                if (q.pre == 0) m.n[1] = 0;
+            }
+            at.small += splits;
+            if (partial) at.part += splits * nt;
+        }
+        carry.small += total.small;
+        carry.part += total.part;
+    }
+    if (tid == 0) {
+        p.header[kSmallUnitsWord] = min(carry.small, p.cap_small);
+        p.header[kBigUnitsWord] = 0;
+        p.header[kSmallNextWord] = 0;
+        p.header[kBigNextWord] = 0;
+    }
+}
+
+// One warp per (token, query head): the token's partial results, rescaled by their maxima.
+template <int D, bool FP16>
+__global__ void __launch_bounds__(128) merge_kernel(const Params p) {
+    grid_wait();
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= (long long)p.n_tok * p.n_q_heads) return;
+    const int lane = threadIdx.x & 31;
+    const int t = (int)(row / p.n_q_heads), hq = (int)(row - (long long)t * p.n_q_heads);
+    const TokMerge tm = p.tok_merge[t];
+    if (tm.n[0] < 0) return;
+    constexpr int V = D / 32;
+    float o[V], M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) o[v] = 0.f;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+        for (int i = 0; i < tm.n[s]; ++i) M = fmaxf(M, p.part_ml[(size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq].x);
+    const float Me = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+        for (int i = 0; i < tm.n[s]; ++i) {
+            const size_t at = (size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq;
+            const float2 ml = p.part_ml[at];
+            const float f = ex2(ml.x - Me);
+            L = fmaf(f, ml.y, L);
+            const float* src = p.part_o + at * D + lane * V;
+#pragma unroll
+            for (int v = 0; v < V; v += 2) {
+                const float2 x = *reinterpret_cast<const float2*>(src + v);
+                o[v] = fmaf(f, x.x, o[v]);
+                o[v + 1] = fmaf(f, x.y, o[v + 1]);
+            }
+        }
+    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);    // nothing visible: a zero row
+    uint16_t* dst = p.out + (size_t)row * D + lane * V;
+#pragma unroll
+    for (int v = 0; v < V; v += 2) *reinterpret_cast<uint32_t*>(dst + v) = pack16<FP16>(o[v] * inv, o[v + 1] * inv);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled() {
+    static EncodeTiledFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess) f = nullptr;
+        return reinterpret_cast<EncodeTiledFn>(f);
+    }();
+    return fn;
+}
+
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+struct Caps {
+    long long small, part;
+};
+// Upper bounds of what the plan can write.  The split length is at least 1 / kSmallItems of all keys, so the splits
+// are at most one per block plus kSmallItems / heads; a block that is split makes at most twice that many.
+Caps caps(long long n_tok, long long n_req, long long max_kv, int n_kv_heads, int G) {
+    const long long TB = kSmallRows / G > 0 ? kSmallRows / G : 1;
+    const long long extra = (kSmallItems + n_kv_heads - 1) / n_kv_heads;
+    Caps c;
+    c.small = n_tok / TB + 2 * n_req + extra + 1;
+    const long long by_items = 2 * n_req + 4 * extra * TB;
+    const long long by_len = n_tok * (2 * ((max_kv + kSmallMinKeys - 1) / kSmallMinKeys) + 2);
+    c.part = by_items < by_len ? by_items : by_len;
+    return c;
+}
+
+struct Layout {
+    size_t small, info, merge, ml, o, total;
+};
+Layout layout(const Caps& c, long long n_tok, int n_q_heads, int head_dim) {
+    Layout l;
+    size_t at = 256;
+    l.small = at; at += up256((size_t)c.small * sizeof(Unit));
+    l.info = at; at += up256((size_t)n_tok * sizeof(TokInfo));
+    l.merge = at; at += up256((size_t)n_tok * sizeof(TokMerge));
+    l.ml = at; at += up256((size_t)c.part * n_q_heads * sizeof(float2));
+    l.o = at; at += up256((size_t)c.part * n_q_heads * head_dim * sizeof(float));
+    l.total = at;
+    return l;
+}
+
+bool supported(int n_q_heads, int n_kv_heads, int head_dim, int page_size) {
+    if (head_dim != 64 && head_dim != 128) return false;
+    if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128) return false;
+    return n_q_heads % n_kv_heads == 0 && n_q_heads / n_kv_heads <= kSmallRows;
+}
+
+}  // namespace
+}  // namespace paged
+}  // namespace plora
+
+using namespace plora::paged;
+
+extern "C" PLORA_API size_t plora_attn_paged_workspace_bytes(int32_t n_tok, int32_t n_req, int32_t n_q_heads, int32_t n_kv_heads,
+                                                             int32_t head_dim, int32_t page_size, int32_t max_blocks) {
+    if (n_tok < 1 || n_req < 1 || n_q_heads < 1 || n_kv_heads < 1 || max_blocks < 1 || page_size < 1) return 0;
+    if (!supported(n_q_heads, n_kv_heads, head_dim, page_size)) return 0;
+    const Caps c = caps(n_tok, n_req, (long long)max_blocks * page_size, n_kv_heads, n_q_heads / n_kv_heads);
+    return layout(c, n_tok, n_q_heads, head_dim).total;
+}
+
+extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, void* stream) {
+    if (!a || a->n_tok < 0 || a->n_req < 0 || a->n_groups < 0) return PLORA_ERR_INVALID_ARG;
+    if (a->n_tok == 0) return PLORA_OK;
+    if (!a->q || !a->k_cache || !a->v_cache || !a->block_table || !a->kv_len || !a->out || !a->workspace || a->n_req < 1 ||
+        a->n_q_heads < 1 || a->n_kv_heads < 1 || a->n_pages < 1 || a->max_blocks < 1 || a->page_size < 1 || a->head_dim < 1)
+        return PLORA_ERR_INVALID_ARG;
+    if (a->type != PLORA_INPUT_BF16 && a->type != PLORA_INPUT_FP16) return PLORA_ERR_INVALID_ARG;
+    if (!supported(a->n_q_heads, a->n_kv_heads, a->head_dim, a->page_size)) return PLORA_ERR_UNSUPPORTED;
+    if (!a->tok_start && a->n_tok != a->n_req) return PLORA_ERR_INVALID_ARG;
+    if (a->n_groups > 0 && (!a->group_start || !a->prefix_len || a->n_groups > a->n_req)) return PLORA_ERR_INVALID_ARG;
+    if (!(a->softcap >= 0.f) || a->softcap > 3.0e38f || !(a->scale == a->scale)) return PLORA_ERR_INVALID_ARG;
+    const long long head_row = a->head_dim, page_elems = (long long)a->n_kv_heads * a->page_size * a->head_dim;
+    const long long page_stride = a->page_stride ? a->page_stride : page_elems;
+    const long long q_stride = a->q_stride ? a->q_stride : (long long)a->n_q_heads * head_row;
+    if (page_stride < page_elems || (page_stride & 7) || q_stride < (long long)a->n_q_heads * head_row || (q_stride & 7))
+        return PLORA_ERR_INVALID_ARG;
+    if (((uintptr_t)a->q & 15) || ((uintptr_t)a->k_cache & 15) || ((uintptr_t)a->v_cache & 15) || ((uintptr_t)a->out & 15) ||
+        ((uintptr_t)a->workspace & 255))
+        return PLORA_ERR_INVALID_ARG;
+    if ((long long)a->max_blocks * a->page_size > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
+    Params p{};
+    p.n_tok = a->n_tok; p.n_req = a->n_req; p.n_groups = a->n_groups;
+    p.n_q_heads = a->n_q_heads; p.n_kv_heads = a->n_kv_heads; p.G = a->n_q_heads / a->n_kv_heads;
+    p.page_size = a->page_size; p.n_pages = a->n_pages; p.max_blocks = a->max_blocks;
+    for (p.page_shift = 0; (1 << p.page_shift) < p.page_size; ++p.page_shift) {}
+    p.max_kv = (a->max_blocks < a->n_pages ? a->max_blocks : a->n_pages) * a->page_size;
+    const Caps c = caps(p.n_tok, p.n_req, p.max_kv, p.n_kv_heads, p.G);
+    const Layout l = layout(c, p.n_tok, p.n_q_heads, a->head_dim);
+    if (a->workspace_bytes < l.total) return PLORA_ERR_WORKSPACE;
+    if (c.small * p.n_kv_heads > INT32_MAX || c.part > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
+    uint8_t* ws = static_cast<uint8_t*>(a->workspace);
+    p.header = reinterpret_cast<int32_t*>(ws);
+    p.small_units = reinterpret_cast<Unit*>(ws + l.small);
+    p.tok_info = reinterpret_cast<TokInfo*>(ws + l.info);
+    p.tok_merge = reinterpret_cast<TokMerge*>(ws + l.merge);
+    p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
+    p.part_o = reinterpret_cast<float*>(ws + l.o);
+    p.cap_small = (int32_t)c.small; p.cap_part = (int32_t)c.part;
+    p.q = static_cast<const uint16_t*>(a->q);
+    p.out = static_cast<uint16_t*>(a->out);
+    p.q_stride = q_stride;
+    p.block_table = a->block_table; p.kv_len = a->kv_len; p.tok_start = a->tok_start;
+    p.group_start = a->group_start; p.prefix_len = a->prefix_len;
+    p.key_lo = a->key_lo; p.key_hi = a->key_hi; p.slopes = a->slopes;
+    const float log2e = 1.4426950408889634f;
+    p.scale_log2e = a->scale * log2e;
+    if (a->softcap > 0.f) {
+        p.cap_in = 2.f * log2e * a->scale / a->softcap;
+        p.cap_log2e = a->softcap * log2e;
+    }
+    if (!encode_tiled()) return PLORA_ERR_UNSUPPORTED;
+    const bool fp16 = a->type == PLORA_INPUT_FP16;
+    // K and V as 4-D tensors [page][KV head][slot][dim]; a box is 64 dims of the slots of a page piece, 128-byte swizzled
+    CUtensorMap tm[2];
+    const cuuint64_t dims[4] = {(cuuint64_t)a->head_dim, (cuuint64_t)p.page_size, (cuuint64_t)p.n_kv_heads, (cuuint64_t)p.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)a->head_dim * 2, (cuuint64_t)p.page_size * a->head_dim * 2, (cuuint64_t)page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(p.page_size < 64 ? p.page_size : 64), 1, 1};
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    const void* bases[2] = {a->k_cache, a->v_cache};
+    for (int i = 0; i < 2; ++i)
+        if (encode_tiled()(&tm[i], fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                           const_cast<void*>(bases[i]), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return PLORA_ERR_INVALID_ARG;
+    int dev = 0, sm_count = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return PLORA_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    plan_kernel<<<1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads, kPlanThreads, 0, st>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return PLORA_ERR_CUDA;
+    if (launch_small(tm[0], tm[1], p, a->head_dim, fp16, sm_count, st) != cudaSuccess) return PLORA_ERR_CUDA;
+    void* args[] = {&p};
+    const void* mk = a->head_dim == 128 ? (fp16 ? (const void*)merge_kernel<128, true> : (const void*)merge_kernel<128, false>)
+                                        : (fp16 ? (const void*)merge_kernel<64, true> : (const void*)merge_kernel<64, false>);
+    const long long rows = (long long)p.n_tok * p.n_q_heads;
+    if (launch_pdl(mk, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, args) != cudaSuccess) return PLORA_ERR_CUDA;
+    return PLORA_OK;
+}
