@@ -536,7 +536,7 @@ PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args *args, void 
  * type       PLORA_INPUT_BF16 / FP16 of q, K, V and out; products and sums in fp32, weights rounded to the type for the
  *            second product.
  * q [n_tok][n_q_heads][head_dim] (q_stride elements between tokens, 0: packed), out packed; query head h reads KV
- * head h / (n_q_heads / n_kv_heads).  head_dim 64 or 128; page_size 16, 32, 64 or 128; at most 16 query heads per KV
+ * head h / (n_q_heads / n_kv_heads).  head_dim 64 or 128; page_size 16, 32, 64 or 128; at most 128 query heads per KV
  * head.  q, K, V and out 16-byte aligned, strides multiples of 8.  Cache slots at or beyond kv_len may hold anything.
  * A block table entry outside [0, n_pages) that is needed reads as zeros and sets PLORA_ERR_INVALID_ARG in the status word.
  * workspace  256-byte aligned, at least plora_attn_paged_workspace_bytes(...) bytes (max_blocks there: min(max_blocks,

@@ -54,6 +54,7 @@ struct Params {
     float2* part_ml;          // [partial token][query head] {m, l}
     float* part_o;            // [partial token][query head][D]
     int32_t cap_small, cap_big, cap_part;
+    int32_t big_tile_tok;     // query tokens in a 128-row tile of the tensor-core kernel
 
     const uint16_t* q;
     uint16_t* out;
@@ -74,6 +75,7 @@ struct Params {
 };
 
 constexpr int kSmallRows = 16;     // rows of a unit the mma.sync kernel takes
+constexpr int kBigRows = 128;      // rows of a tile of the tensor-core kernel; a unit has up to two tiles
 
 // ---- PTX wrappers ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -108,7 +110,7 @@ __device__ __forceinline__ long long wait_limit(const int32_t* header) {
     const long long v = *reinterpret_cast<const volatile long long*>(header + kLimitWord);
     return v > 0 ? v : kWaitCycles;
 }
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, WaitCtl w) {
+__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, WaitCtl w) {
     const long long t0 = clock64();
     long long limit = 0;
     for (;;) {
@@ -191,6 +193,8 @@ __device__ __forceinline__ float score(const Params& p, float qk, float slope, i
 // ---- launches -----------------------------------------------------------------------------------------
 cudaError_t launch_small(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim, bool fp16,
                          int sm_count, cudaStream_t st);
+cudaError_t launch_big(const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim,
+                       bool fp16, int sm_count, cudaStream_t st);
 cudaError_t launch_pdl(const void* kern, dim3 grid, dim3 block, size_t smem, cudaStream_t st, void** args);
 
 }  // namespace paged

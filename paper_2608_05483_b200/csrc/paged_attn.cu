@@ -29,11 +29,14 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatever the device has: it sizes the workspace
 constexpr int kSmallItems = kPlanSms * 2 * 8;   // aimed-at items of the small kernel (two CTAs per SM)
 constexpr int kSmallMinKeys = 128;     // no split shorter than this
+constexpr int kBigItems = kPlanSms * 2;         // aimed-at items of the tensor-core kernel (one CTA per SM)
+constexpr int kBigMinKeys = 512;
 constexpr int kGroupCache = 2048;      // group starts held in shared memory
 
 struct Sums {        // counts that the scan carries along
-    int small, part;
+    int small, big, part;
 };
+__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) { return Sums{a.small + b.small, a.big + b.big, a.part + b.part}; }
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
 
@@ -72,32 +75,26 @@ __device__ __forceinline__ TokInfo visible(const Params& p, int t, int pos, int 
     return ti;
 }
 
-__device__ __forceinline__ Sums scan_exclusive(Sums v, Sums& total, Sums* warp_sums) {
+__device__ __forceinline__ Sums scan_exclusive(const Sums& v, Sums& total, Sums* warp_sums) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Sums in = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int a = __shfl_up_sync(0xffffffffu, in.small, d), b = __shfl_up_sync(0xffffffffu, in.part, d);
-        if (lane >= d) {
-            in.small += a;
-            in.part += b;
-        }
+        const Sums a{__shfl_up_sync(0xffffffffu, in.small, d), __shfl_up_sync(0xffffffffu, in.big, d),
+                     __shfl_up_sync(0xffffffffu, in.part, d)};
+        if (lane >= d) in = in + a;
     }
     __syncthreads();
     if (lane == 31) warp_sums[warp] = in;
     __syncthreads();
-    Sums before{0, 0}, all{0, 0};
+    Sums before{0, 0, 0}, all{0, 0, 0};
     for (int w = 0; w < kPlanThreads / 32; ++w) {
         const Sums x = warp_sums[w];
-        if (w < warp) {
-            before.small += x.small;
-            before.part += x.part;
-        }
-        all.small += x.small;
-        all.part += x.part;
+        if (w < warp) before = before + x;
+        all = all + x;
     }
     total = all;
-    return Sums{before.small + in.small - v.small, before.part + in.part - v.part};
+    return Sums{before.small + in.small - v.small, before.big + in.big - v.big, before.part + in.part - v.part};
 }
 
 __device__ __forceinline__ long long sum_all(long long v, long long* red) {
@@ -147,7 +144,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     __shared__ long long red[kPlanThreads / 32];
     __shared__ int s_group[kGroupCache + 1];
     const int tid = threadIdx.x;
-    const int TB = max(1, kSmallRows / p.G);      // tokens of a unit
+    // tokens of a unit: the rows of a tile of the small kernel, or two tiles of the big one
+    const int TBs = max(1, kSmallRows / p.G), TBb = 2 * p.big_tile_tok;
+    auto is_small = [&](int n) { return n * p.G <= kSmallRows; };
     const bool cached = p.n_groups <= kGroupCache;
     for (int g = tid; p.n_groups > 0 && cached && g <= p.n_groups; g += kPlanThreads) s_group[g] = clampi(p.group_start[g], 0, p.n_req);
     __syncthreads();
@@ -173,11 +172,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         }
         return q;
     };
-    // keys of block b of a request: from the first that one of its tokens sees (behind the shared prefix) to the last
-    auto block_keys = [&](const Req& q, int b, int& k0, int& k1) {
+    // keys of block b of a request: behind the shared prefix, up to the last that one of its tokens may see (the few tokens
+    // of a small unit are looked at one by one; the big kernel looks for itself)
+    auto block_keys = [&](const Req& q, int b, int TB, int& k0, int& k1) {
+        if (!is_small(q.n)) {
+            k0 = q.pre;
+            k1 = max(k0, p.key_hi ? q.kv : q.kv - q.n + min(q.n, (b + 1) * TB));
+            return;
+        }
         k0 = INT_MAX;
         k1 = 0;
-        for (int t = q.tok0 + b * TB; t < q.tok0 + min(q.n, (b + 1) * TB); ++t) {
+        for (int t = q.tok0; t < q.tok0 + q.n; ++t) {
             const TokInfo ti = visible(p, t, q.kv - (q.tok0 + q.n - t), q.kv);
             if (ti.lo < ti.hi) {
                 k0 = min(k0, ti.lo);
@@ -189,25 +194,38 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         if (k0 == INT_MAX) k0 = k1 = 0;
     };
 
-    // how many keys there are to read in all, over the units: the split length follows from it
-    long long keys = 0;
+    // how many keys there are to read in all, over the units of each kind: the split lengths follow from it
+    long long keys_s = 0, keys_b = 0;
     for (int r = tid; r < p.n_req; r += kPlanThreads) {
         const Req q = request(r);
+        const int TB = is_small(q.n) ? TBs : TBb;
+        long long keys = 0;
         for (int b = 0; b * TB < q.n; ++b) {
             int k0, k1;
-            block_keys(q, b, k0, k1);
+            block_keys(q, b, TB, k0, k1);
             keys += k1 - k0;
         }
+        if (is_small(q.n)) keys_s += keys;
+        else keys_b += keys;
     }
     for (int g = tid; g < p.n_groups; g += kPlanThreads) {
-        const int s = gstart(g), e = gstart(g + 1);
-        keys += (long long)prefix_of(g) * ((e - s + TB - 1) / TB);
+        const int n = gstart(g + 1) - gstart(g), pre = prefix_of(g);
+        if (is_small(n)) keys_s += pre;
+        else keys_b += (long long)pre * ((n + TBb - 1) / TBb);
     }
-    keys = sum_all(keys, red);
-    const long long per = (keys * p.n_kv_heads + kSmallItems - 1) / kSmallItems;
-    const int chunk = (int)max((long long)kSmallMinKeys, (per + 63) / 64 * 64);
+    keys_s = sum_all(keys_s, red);
+    keys_b = sum_all(keys_b, red);
+    const long long per_s = (keys_s * p.n_kv_heads + kSmallItems - 1) / kSmallItems;
+    const long long per_b = (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems;
+    const int chunk_s = (int)min((long long)INT_MAX / 2, max((long long)kSmallMinKeys, (per_s + 63) / 64 * 64));
+    const int chunk_b = (int)min((long long)INT_MAX / 2, max((long long)kBigMinKeys, (per_b + 127) / 128 * 128));
+    auto splits_of = [&](int keys, bool small) { const int c = small ? chunk_s : chunk_b; return (keys + c - 1) / c; };
+    auto fits = [&](const Sums& at, const Sums& want) {
+        return at.small + want.small <= p.cap_small && at.big + want.big <= p.cap_big && at.part + want.part <= p.cap_part;
+    };
+    auto put = [&](bool small, int i, const Unit& u) { (small ? p.small_units : p.big_units)[i] = u; };
 
-    Sums carry{0, 0};
+    Sums carry{0, 0, 0}, total;
     // the groups' prefixes: always partial results
     for (int g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
@@ -218,20 +236,20 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
             pre = prefix_of(g);
             if (pre > 0) token_range(p, s, tok0, nn);
         }
-        const int splits = (pre + chunk - 1) / chunk, blocks = pre > 0 ? (n + TB - 1) / TB : 0;
-        Sums total;
-        Sums at = scan_exclusive(Sums{splits * blocks, splits * (pre > 0 ? n : 0)}, total, warp_sums);
-        at.small += carry.small;
-        at.part += carry.part;
-        if (pre > 0 && (at.small + splits * blocks > p.cap_small || at.part + splits * n > p.cap_part)) {
+        const bool small = is_small(n);
+        const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b;
+        const int splits = splits_of(pre, small), blocks = pre > 0 ? (n + TB - 1) / TB : 0;
+        const Sums want{small ? splits * blocks : 0, small ? 0 : splits * blocks, pre > 0 ? splits * n : 0};
+        const Sums at = carry + scan_exclusive(want, total, warp_sums);
+        if (pre > 0 && !fits(at, want)) {
             atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
             for (int t = 0; t < n; ++t) p.tok_merge[tok0 + t].n[1] = 0;
         } else if (pre > 0) {
             for (int b = 0; b < blocks; ++b) {
                 const int nt = min(TB, n - b * TB);
                 for (int i = 0; i < splits; ++i)
-                    p.small_units[at.small + b * splits + i] =
-                        Unit{tok0 + b * TB, nt, s, i * chunk, min(pre, (i + 1) * chunk), at.part + i * n + b * TB, {0, 0}};
+                    put(small, (small ? at.small : at.big) + b * splits + i,
+                        Unit{tok0 + b * TB, nt, s, i * chunk, min(pre, (i + 1) * chunk), at.part + i * n + b * TB, {0, 0}});
                 for (int t = 0; t < nt; ++t) {
                     TokMerge& m = p.tok_merge[tok0 + b * TB + t];
                     m.base[1] = at.part + b * TB + t;
@@ -240,8 +258,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
                 }
             }
         }
-        carry.small += total.small;
-        carry.part += total.part;
+        carry = carry + total;
     }
     __syncthreads();
     // the requests' own keys
@@ -249,31 +266,32 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         const int r = r0 + tid;
         Req q{0, 0, 0, 0};
         if (r < p.n_req) q = request(r);
-        Sums want{0, 0};
+        const bool small = is_small(q.n);
+        const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b;
+        Sums want{0, 0, 0};
         for (int b = 0; b * TB < q.n; ++b) {
             int k0, k1;
-            block_keys(q, b, k0, k1);
-            const int splits = (k1 - k0 + chunk - 1) / chunk;
-            want.small += splits;
+            block_keys(q, b, TB, k0, k1);
+            const int splits = splits_of(k1 - k0, small);
+            (small ? want.small : want.big) += splits;
             if (splits > 1 || q.pre > 0) want.part += splits * min(TB, q.n - b * TB);
         }
-        Sums total;
-        Sums at = scan_exclusive(want, total, warp_sums);
-        at.small += carry.small;
-        at.part += carry.part;
-        if (at.small + want.small > p.cap_small || at.part + want.part > p.cap_part) {
+        Sums at = carry + scan_exclusive(want, total, warp_sums);
+        if (!fits(at, want)) {
             atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
             for (int t = 0; t < q.n; ++t) p.tok_merge[q.tok0 + t] = TokMerge{{0, 0}, {0, 0}, {0, 0}, {0, 0}};
             q.n = 0;
         }
-        for (int b = 0; b * TB < q.n; ++b) {
+        // (the last block first: it sees the most keys, and the items are taken in this order)
+        int unit = small ? at.small : at.big;
+        for (int b = (q.n + TB - 1) / TB - 1; b >= 0; --b) {
             int k0, k1;
-            block_keys(q, b, k0, k1);
-            const int splits = (k1 - k0 + chunk - 1) / chunk, nt = min(TB, q.n - b * TB);
+            block_keys(q, b, TB, k0, k1);
+            const int splits = splits_of(k1 - k0, small), nt = min(TB, q.n - b * TB);
             const bool partial = splits > 1 || q.pre > 0;
             for (int i = 0; i < splits; ++i)
-                p.small_units[at.small + i] = Unit{q.tok0 + b * TB, nt, r, k0 + i * chunk, min(k1, k0 + (i + 1) * chunk),
-                                                   partial ? at.part + i * nt : -1, {0, 0}};
+                put(small, unit + i, Unit{q.tok0 + b * TB, nt, r, k0 + i * chunk, min(k1, k0 + (i + 1) * chunk),
+                                          partial ? at.part + i * nt : -1, {0, 0}});
             for (int t = 0; t < nt; ++t) {
                 TokMerge& m = p.tok_merge[q.tok0 + b * TB + t];
                 m.base[0] = at.part + t;
@@ -281,15 +299,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
                 m.stride[0] = nt;
                 if (q.pre == 0) m.n[1] = 0;
             }
-            at.small += splits;
+            unit += splits;
             if (partial) at.part += splits * nt;
         }
-        carry.small += total.small;
-        carry.part += total.part;
+        carry = carry + total;
     }
     if (tid == 0) {
         p.header[kSmallUnitsWord] = min(carry.small, p.cap_small);
-        p.header[kBigUnitsWord] = 0;
+        p.header[kBigUnitsWord] = min(carry.big, p.cap_big);
         p.header[kSmallNextWord] = 0;
         p.header[kBigNextWord] = 0;
     }
@@ -350,28 +367,31 @@ EncodeTiledFn encode_tiled() {
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct Caps {
-    long long small, part;
+    long long small, big, part;
 };
-// Upper bounds of what the plan can write.  The split length is at least 1 / kSmallItems of all keys, so the splits
-// are at most one per block plus kSmallItems / heads; a block that is split makes at most twice that many.
+int tile_tokens(int G) { return kBigRows / G; }
+// Upper bounds of what the plan can write.  A split length is at least 1 / kSmallItems (1 / kBigItems) of all keys of its
+// kind, so the units are at most one per block plus that many / heads; blocks that are split make at most twice that many.
 Caps caps(long long n_tok, long long n_req, long long max_kv, int n_kv_heads, int G) {
-    const long long TB = kSmallRows / G > 0 ? kSmallRows / G : 1;
-    const long long extra = (kSmallItems + n_kv_heads - 1) / n_kv_heads;
+    const long long TBs = kSmallRows / G > 0 ? kSmallRows / G : 1, TBb = 2 * tile_tokens(G);
+    const long long extra_s = (kSmallItems + n_kv_heads - 1) / n_kv_heads, extra_b = (kBigItems + n_kv_heads - 1) / n_kv_heads;
     Caps c;
-    c.small = n_tok / TB + 2 * n_req + extra + 1;
-    const long long by_items = 2 * n_req + 4 * extra * TB;
+    c.small = 2 * n_req + extra_s + 1;
+    c.big = n_tok / TBb + 2 * n_req + extra_b + 1;
+    const long long by_items = 2 * n_req + 4 * (extra_s * TBs + extra_b * TBb);
     const long long by_len = n_tok * (2 * ((max_kv + kSmallMinKeys - 1) / kSmallMinKeys) + 2);
     c.part = by_items < by_len ? by_items : by_len;
     return c;
 }
 
 struct Layout {
-    size_t small, info, merge, ml, o, total;
+    size_t small, big, info, merge, ml, o, total;
 };
 Layout layout(const Caps& c, long long n_tok, int n_q_heads, int head_dim) {
     Layout l;
     size_t at = 256;
     l.small = at; at += up256((size_t)c.small * sizeof(Unit));
+    l.big = at; at += up256((size_t)c.big * sizeof(Unit));
     l.info = at; at += up256((size_t)n_tok * sizeof(TokInfo));
     l.merge = at; at += up256((size_t)n_tok * sizeof(TokMerge));
     l.ml = at; at += up256((size_t)c.part * n_q_heads * sizeof(float2));
@@ -383,7 +403,7 @@ Layout layout(const Caps& c, long long n_tok, int n_q_heads, int head_dim) {
 bool supported(int n_q_heads, int n_kv_heads, int head_dim, int page_size) {
     if (head_dim != 64 && head_dim != 128) return false;
     if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128) return false;
-    return n_q_heads % n_kv_heads == 0 && n_q_heads / n_kv_heads <= kSmallRows;
+    return n_q_heads % n_kv_heads == 0 && n_q_heads / n_kv_heads <= kBigRows;
 }
 
 }  // namespace
@@ -423,21 +443,23 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     Params p{};
     p.n_tok = a->n_tok; p.n_req = a->n_req; p.n_groups = a->n_groups;
     p.n_q_heads = a->n_q_heads; p.n_kv_heads = a->n_kv_heads; p.G = a->n_q_heads / a->n_kv_heads;
+    p.big_tile_tok = tile_tokens(p.G);
     p.page_size = a->page_size; p.n_pages = a->n_pages; p.max_blocks = a->max_blocks;
     for (p.page_shift = 0; (1 << p.page_shift) < p.page_size; ++p.page_shift) {}
     p.max_kv = (a->max_blocks < a->n_pages ? a->max_blocks : a->n_pages) * a->page_size;
     const Caps c = caps(p.n_tok, p.n_req, p.max_kv, p.n_kv_heads, p.G);
     const Layout l = layout(c, p.n_tok, p.n_q_heads, a->head_dim);
     if (a->workspace_bytes < l.total) return PLORA_ERR_WORKSPACE;
-    if (c.small * p.n_kv_heads > INT32_MAX || c.part > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
+    if (c.small * p.n_kv_heads > INT32_MAX || c.big * p.n_kv_heads > INT32_MAX || c.part > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
     uint8_t* ws = static_cast<uint8_t*>(a->workspace);
     p.header = reinterpret_cast<int32_t*>(ws);
     p.small_units = reinterpret_cast<Unit*>(ws + l.small);
+    p.big_units = reinterpret_cast<Unit*>(ws + l.big);
     p.tok_info = reinterpret_cast<TokInfo*>(ws + l.info);
     p.tok_merge = reinterpret_cast<TokMerge*>(ws + l.merge);
     p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     p.part_o = reinterpret_cast<float*>(ws + l.o);
-    p.cap_small = (int32_t)c.small; p.cap_part = (int32_t)c.part;
+    p.cap_small = (int32_t)c.small; p.cap_big = (int32_t)c.big; p.cap_part = (int32_t)c.part;
     p.q = static_cast<const uint16_t*>(a->q);
     p.out = static_cast<uint16_t*>(a->out);
     p.q_stride = q_stride;
@@ -465,13 +487,26 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return PLORA_ERR_INVALID_ARG;
+    // the queries as a 3-D tensor [token][head][dim]; a box is 64 dims of a KV head's G heads, of the tokens of a tile
+    CUtensorMap tq;
+    const cuuint64_t qdims[3] = {(cuuint64_t)a->head_dim, (cuuint64_t)p.n_q_heads, (cuuint64_t)p.n_tok};
+    const cuuint64_t qstrides[2] = {(cuuint64_t)a->head_dim * 2, (cuuint64_t)q_stride * 2};
+    const cuuint32_t qbox[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.big_tile_tok};
+    if (encode_tiled()(&tq, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a->q),
+                       qdims, qstrides, qbox, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return PLORA_ERR_INVALID_ARG;
     int dev = 0, sm_count = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return PLORA_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     plan_kernel<<<1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads, kPlanThreads, 0, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return PLORA_ERR_CUDA;
-    if (launch_small(tm[0], tm[1], p, a->head_dim, fp16, sm_count, st) != cudaSuccess) return PLORA_ERR_CUDA;
+    // one token per request, no groups: nothing can be larger than a small unit (and more than 16 heads never make one)
+    if ((p.tok_start || p.n_groups > 0 || p.G > kSmallRows) &&
+        launch_big(tq, tm[0], tm[1], p, a->head_dim, fp16, sm_count, st) != cudaSuccess)
+        return PLORA_ERR_CUDA;
+    if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, sm_count, st) != cudaSuccess) return PLORA_ERR_CUDA;
     void* args[] = {&p};
     const void* mk = a->head_dim == 128 ? (fp16 ? (const void*)merge_kernel<128, true> : (const void*)merge_kernel<128, false>)
                                         : (fp16 ? (const void*)merge_kernel<64, true> : (const void*)merge_kernel<64, false>);

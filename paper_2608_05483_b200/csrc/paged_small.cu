@@ -8,7 +8,7 @@
 // softmax per warp in 32 bits.  (The legacy tensor instruction fits: its operands stay in registers, and at
 // 16 rows the tensor pipe is idle nine tenths of the time anyway.)  At the end of an item the warps' (m, l, o)
 // meet in shared memory.
-// P is rounded to the input type for the second product (2^-9 or 2^-12 of each weight, zero mean; the output
+// P is rounded to the input type for the second product (at most 2^-8 or 2^-11 of each weight, zero mean; the output
 // is rounded to the same type).
 #include "paged.cuh"
 
