@@ -10,10 +10,12 @@ functions fails loudly.
 from __future__ import annotations
 
 import ctypes
+import struct
 from pathlib import Path
 from typing import Any, NamedTuple
 
 import numpy as np
+import torch
 
 from . import _build
 
@@ -155,9 +157,9 @@ def load(build_if_missing: bool = True):
                                    ctypes.POINTER(CostTerms)]),
         "plora_kv_plan": (i32, [vp, vp, i32, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
         "plora_rope_table": (i32, [ctypes.POINTER(RopeDesc), i32, vp, vp]),
-        "plora_rope_cache": (i32, [ctypes.POINTER(RopeCacheArgs), vp]),
+        "plora_rope_cache": (i32, [vp, vp]),
         "plora_attn_paged_workspace_bytes": (ctypes.c_size_t, [i32] * 7),
-        "plora_attn_paged": (i32, [ctypes.POINTER(PagedAttn), vp]),
+        "plora_attn_paged": (i32, [vp, vp]),
     }
     for name in EXPORTS:
         fn = getattr(lib, name)  # AttributeError here = the library does not export what the header declares
@@ -284,64 +286,81 @@ class KvPlan(NamedTuple):
     cursor: Any
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+# These calls are made once per layer or step, at a few microseconds of GPU work each, so the checks are written for
+# speed: plain comparisons, the argument structures packed in one go (laid out as RopeCacheArgs and PagedAttn).
+_ROPE_PACK = struct.Struct("@11i4q10P")
+_PAGED_PACK = struct.Struct("@10i2q11P2f2PN")
 
 
-def _ints(name, t, shape):
-    """An int32 CUDA tensor, packed, of this shape (None in the shape: any size)."""
-    import torch
-    _need(t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.dim() == len(shape)
-          and all(w is None or w == n for w, n in zip(shape, t.shape)),
-          f"{name}: int32 CUDA tensor {list(shape)} expected, got {t.dtype} {list(t.shape)} on {t.device}")
+def _bad(what: str):
+    raise ValueError(what)
+
+
+def _ints(name, t, shape) -> int:
+    """Address of an int32 CUDA tensor, packed, of this shape."""
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        _bad(f"{name}: packed int32 CUDA tensor {list(shape)} expected, got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _type16(t):
-    import torch
-    _need(t.dtype in (torch.bfloat16, torch.float16), f"bfloat16 or float16 expected, got {t.dtype}")
-    return INPUT_BF16 if t.dtype is torch.bfloat16 else INPUT_FP16
+def _opt_ints(name, t, shape) -> int:
+    return 0 if t is None else _ints(name, t, shape)
 
 
-def _heads(name, t):
-    """Strides of a [n_tok, heads, head_dim] tensor whose heads are packed: elements between tokens."""
-    _need(t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] <= 1 or t.stride(1) == t.shape[2]),
-          f"{name}: CUDA tensor [n_tok, heads, head_dim] with packed heads expected")
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1] * t.shape[2])
+def _type16(t) -> int:
+    if t.dtype is torch.bfloat16:
+        return INPUT_BF16
+    if t.dtype is torch.float16:
+        return INPUT_FP16
+    _bad(f"bfloat16 or float16 expected, got {t.dtype}")
 
 
-def _cache(k_cache, v_cache):
-    """Elements between pages of a cache pair [n_pages, n_kv_heads, page_size, head_dim] whose pages are packed."""
-    _need(k_cache.is_cuda and v_cache.is_cuda and k_cache.dim() == 4 and k_cache.shape == v_cache.shape
-          and k_cache.dtype == v_cache.dtype and k_cache.stride() == v_cache.stride(),
-          "k_cache, v_cache: alike CUDA tensors [n_pages, n_kv_heads, page_size, head_dim] expected")
+def _token_stride(name, t) -> int:
+    """Elements between the tokens of a CUDA tensor [n_tok, heads, head_dim] whose heads are packed."""
+    n, h, d = t.shape
+    st, sh, sd = t.stride()
+    if not t.is_cuda or (sd != 1 and d > 1) or (sh != d and h > 1):
+        _bad(f"{name}: CUDA tensor [n_tok, heads, head_dim] with packed heads expected")
+    return st if n > 1 else h * d
+
+
+def _page_stride(k_cache, v_cache) -> int:
+    """Elements between the pages of a cache pair [n_pages, n_kv_heads, page_size, head_dim] whose pages are packed."""
     n, h, s, d = k_cache.shape
-    _need(k_cache[0].is_contiguous(), "k_cache, v_cache: a page's values must be packed")
-    return int(k_cache.stride(0)) if n > 1 else h * s * d
+    st = k_cache.stride()
+    if (v_cache.shape != k_cache.shape or v_cache.dtype is not k_cache.dtype or v_cache.stride() != st or not k_cache.is_cuda
+            or not v_cache.is_cuda or st[3] != 1 or st[2] != d or (st[1] != s * d and h > 1)):
+        _bad("k_cache, v_cache: alike CUDA tensors [n_pages, n_kv_heads, page_size, head_dim] with packed pages expected")
+    return st[0] if n > 1 else h * s * d
+
+
+def _raw_stream(stream, t) -> int:
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def kv_plan(kv_len, new_len, page_size: int, free_pages, block_table, max_tokens: int, cursor=None, out=None, stream=None) -> KvPlan:
     """Pages, slots and positions of a step (plora_kv_plan): kv_len, new_len int32 [n_req], free_pages int32 [n_free],
     block_table int32 [n_req, max_blocks] (updated in place), cursor int32 [1] or None (the free list's first unused
     entry; the result's cursor is the next step's).  out: a KvPlan of an earlier step, to be overwritten."""
-    import torch
-    n = int(kv_len.shape[0])
+    n, = kv_len.shape
+    one, toks = (n,), (max_tokens,)
     if out is None:
         buf = torch.empty(2 * n + 2 + 3 * max_tokens, dtype=torch.int32, device=kv_len.device)
-        at, parts = 0, []
-        for size in (n + 1, max_tokens, max_tokens, max_tokens, n, 1):
-            parts.append(buf[at:at + size])
-            at += size
-        out = KvPlan(*parts)
-    _check(plora_kv_plan(_ints("kv_len", kv_len, (n,)), _ints("new_len", new_len, (n,)), n, int(page_size),
-                         _ints("free_pages", free_pages, (None,)), int(free_pages.shape[0]),
-                         _ints("cursor", cursor, (1,)) if cursor is not None else None,
-                         _ints("block_table", block_table, (n, None)), int(block_table.shape[1]), int(max_tokens),
-                         _ints("tok_start", out.tok_start, (n + 1,)), _ints("positions", out.positions, (max_tokens,)),
-                         _ints("tok_req", out.tok_req, (max_tokens,)), _ints("slots", out.slots, (max_tokens,)),
-                         _ints("kv_len", out.kv_len, (n,)), _ints("cursor", out.cursor, (1,)), _stream_handle(stream)),
-           "plora_kv_plan")
+        out = KvPlan(*buf.split_with_sizes((n + 1, max_tokens, max_tokens, max_tokens, n, 1)))
+        at = buf.data_ptr()
+        ptrs = (at, at + 4 * (n + 1), at + 4 * (n + 1 + max_tokens), at + 4 * (n + 1 + 2 * max_tokens),
+                at + 4 * (n + 1 + 3 * max_tokens), at + 4 * (2 * n + 1 + 3 * max_tokens))
+    else:
+        ptrs = (_ints("tok_start", out.tok_start, (n + 1,)), _ints("positions", out.positions, toks),
+                _ints("tok_req", out.tok_req, toks), _ints("slots", out.slots, toks), _ints("kv_len", out.kv_len, one),
+                _ints("cursor", out.cursor, (1,)))
+    n_free, = free_pages.shape
+    width = block_table.shape[-1]
+    rc = load().plora_kv_plan(_ints("kv_len", kv_len, one), _ints("new_len", new_len, one), n, page_size,
+                              _ints("free_pages", free_pages, (n_free,)), n_free, _opt_ints("cursor", cursor, (1,)),
+                              _ints("block_table", block_table, (n, width)), width, max_tokens, *ptrs, _raw_stream(stream, kv_len))
+    if rc != OK:
+        raise PloraError(rc, "plora_kv_plan")
     return out
 
 
@@ -351,48 +370,57 @@ _SCALINGS = {"none": ROPE_NONE, "linear": ROPE_LINEAR, "ntk": ROPE_NTK, "bands":
 def rope_table(rot_dim: int, max_pos: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
                orig_len: float = 0.0, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0, device="cuda", stream=None):
     """The fp32 table [max_pos, rot_dim // 2, 2] of cosines and sines (plora_rope_table)."""
-    import torch
-    _need(scaling in _SCALINGS, f"scaling: one of {sorted(_SCALINGS)} expected, got {scaling!r}")
+    if scaling not in _SCALINGS:
+        _bad(f"scaling: one of {sorted(_SCALINGS)} expected, got {scaling!r}")
     table = torch.empty((max(0, int(max_pos)), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
     d = RopeDesc(int(rot_dim), _SCALINGS[scaling], base, factor, orig_len, low, high, magnitude)
-    _check(plora_rope_table(d, int(max_pos), table.data_ptr(), _stream_handle(stream)), "plora_rope_table")
+    _check(plora_rope_table(d, int(max_pos), table.data_ptr(), _raw_stream(stream, table)), "plora_rope_table")
     return table
 
 
 def rope_cache(q, k, v, positions, slots, table, k_cache, v_cache, q_out=None, interleaved: bool = False, status=None, stream=None):
     """Rotates q and k, writes k and v to their cache slots and returns the rotated q (plora_rope_cache).  q, k, v:
     [n_tok, heads, head_dim], fp32 or the cache's type, rows of any stride; table: rope_table's (None: nothing turns)."""
-    import torch
     n, hq, d = q.shape
-    hk = int(k.shape[1])
+    hk = k.shape[1]
     out_type = _type16(k_cache)
-    page_stride = _cache(k_cache, v_cache)
-    _need(k.dtype == q.dtype and v.dtype == q.dtype and q.dtype in (torch.float32, k_cache.dtype),
-          "q, k, v: one type, float32 or the cache's, expected")
-    _need(k.shape == (n, hk, d) and v.shape == k.shape and k_cache.shape[1] == hk and k_cache.shape[3] == d,
-          "q, k, v and the caches: shapes do not agree")
+    page_stride = _page_stride(k_cache, v_cache)
+    n_pages, ch, page, cd = k_cache.shape
+    if q.dtype is torch.float32:
+        in_type = INPUT_FP32
+    elif q.dtype is k_cache.dtype:
+        in_type = out_type
+    else:
+        _bad("q, k, v: float32 or the cache's type expected")
+    if k.dtype is not q.dtype or v.dtype is not q.dtype:
+        _bad("q, k, v: one type expected")
+    if k.shape != (n, hk, d) or v.shape != (n, hk, d) or ch != hk or cd != d:
+        _bad("q, k, v and the caches: shapes do not agree")
     if q_out is None:
         q_out = torch.empty((n, hq, d), dtype=k_cache.dtype, device=q.device)
-    _need(q_out.dtype == k_cache.dtype and q_out.shape == q.shape and q_out.is_contiguous(), "q_out: packed, of the cache's type, expected")
+    elif q_out.dtype is not k_cache.dtype or q_out.shape != (n, hq, d) or not q_out.is_cuda or not q_out.is_contiguous():
+        _bad("q_out: packed, of the cache's type and q's shape, expected")
+    rot = max_pos = at = 0
     if table is not None:
-        _need(table.dtype is torch.float32 and table.is_cuda and table.is_contiguous() and table.dim() == 3 and table.shape[2] == 2,
-              "table: float32 [max_pos, rot_dim // 2, 2] expected")
-    a = RopeCacheArgs(INPUT_FP32 if q.dtype is torch.float32 else out_type, out_type, ROPE_INTERLEAVED if interleaved else ROPE_HALF,
-                      n, hq, hk, d, 0 if table is None else 2 * int(table.shape[1]), 0 if table is None else int(table.shape[0]),
-                      int(k_cache.shape[2]), int(k_cache.shape[0]), _heads("q", q), _heads("k", k), _heads("v", v), page_stride,
-                      q.data_ptr(), k.data_ptr(), v.data_ptr(), _ints("positions", positions, (n,)), _ints("slots", slots, (n,)),
-                      None if table is None else table.data_ptr(), q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                      None if status is None else _ints("status", status, (1,)))
-    _check(plora_rope_cache(a, _stream_handle(stream)), "plora_rope_cache")
+        max_pos, half, two = table.shape
+        if two != 2 or table.dtype is not torch.float32 or not table.is_cuda or not table.is_contiguous():
+            _bad("table: float32 [max_pos, rot_dim // 2, 2] expected")
+        rot, at = 2 * half, table.data_ptr()
+    a = _ROPE_PACK.pack(in_type, out_type, ROPE_INTERLEAVED if interleaved else ROPE_HALF, n, hq, hk, d, rot, max_pos, page, n_pages,
+                        _token_stride("q", q), _token_stride("k", k), _token_stride("v", v), page_stride, q.data_ptr(), k.data_ptr(),
+                        v.data_ptr(), _ints("positions", positions, (n,)), _ints("slots", slots, (n,)), at, q_out.data_ptr(),
+                        k_cache.data_ptr(), v_cache.data_ptr(), _opt_ints("status", status, (1,)))
+    rc = load().plora_rope_cache(a, _raw_stream(stream, q))
+    if rc != OK:
+        raise PloraError(rc, "plora_rope_cache")
     return q_out
 
 
 def attn_paged_workspace(q, k_cache, n_req: int, max_blocks=None):
     """A zeroed workspace for attn_paged on batches of q's size over this cache (max_blocks: the block table's width, None:
     any)."""
-    import torch
     n_pages, hk, page, d = k_cache.shape
-    need = plora_attn_paged_workspace_bytes(max(1, int(q.shape[0])), int(n_req), int(q.shape[1]), hk, d, page,
+    need = plora_attn_paged_workspace_bytes(max(1, q.shape[0]), int(n_req), q.shape[1], hk, d, page,
                                             n_pages if max_blocks is None else min(n_pages, int(max_blocks)))
     if need == 0:
         raise PloraError(ERR_UNSUPPORTED, "plora_attn_paged_workspace_bytes")
@@ -403,31 +431,37 @@ def attn_paged(q, k_cache, v_cache, block_table, kv_len, scale: float, tok_start
                softcap: float = 0.0, slopes=None, key_lo=None, key_hi=None, out=None, workspace=None, stream=None):
     """Attention of the new tokens q [n_tok, n_q_heads, head_dim] over the paged cache (plora_attn_paged); returns
     (out, workspace).  tok_start None: one token per request.  Pass the returned workspace back in to reuse it."""
-    import torch
     n, hq, d = q.shape
-    n_pages, hk, page, _ = k_cache.shape
-    n_req = int(kv_len.shape[0])
-    page_stride = _cache(k_cache, v_cache)
-    _need(q.dtype == k_cache.dtype and k_cache.shape[3] == d and hk > 0 and hq % hk == 0, "q and the caches do not agree")
-    table_ptr = _ints("block_table", block_table, (n_req, None))
+    n_pages, hk, page, cd = k_cache.shape
+    n_req, = kv_len.shape
+    width = block_table.shape[-1]
+    page_stride = _page_stride(k_cache, v_cache)
+    if q.dtype is not k_cache.dtype or cd != d or hk == 0 or hq % hk != 0:
+        _bad("q and the caches do not agree")
     if out is None:
         out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
-    _need(out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous() and out.is_cuda, "out: packed, of q's shape and type, expected")
+    elif out.dtype is not q.dtype or out.shape != (n, hq, d) or not out.is_cuda or not out.is_contiguous():
+        _bad("out: packed, of q's shape and type, expected")
     if workspace is None:
-        workspace = attn_paged_workspace(q, k_cache, n_req, block_table.shape[1])
-    n_groups = 0 if group_start is None else int(group_start.shape[0]) - 1
-    _need(n_groups >= 0 and (group_start is None) == (prefix_len is None), "group_start and prefix_len go together")
-    if slopes is not None:
-        _need(slopes.dtype is torch.float32 and slopes.is_cuda and slopes.is_contiguous() and slopes.shape == (hq,),
-              "slopes: float32 CUDA tensor [n_q_heads] expected")
-    opt = lambda name, t, shape: None if t is None else _ints(name, t, shape)
-    a = PagedAttn(_type16(q), n, n_req, n_groups, hq, hk, d, page, n_pages, int(block_table.shape[1]), _heads("q", q), page_stride,
-                  q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table_ptr, _ints("kv_len", kv_len, (n_req,)),
-                  opt("tok_start", tok_start, (n_req + 1,)), opt("group_start", group_start, (None,)),
-                  opt("prefix_len", prefix_len, (n_groups,)), opt("key_lo", key_lo, (n,)), opt("key_hi", key_hi, (n,)),
-                  None if slopes is None else slopes.data_ptr(), scale, softcap, out.data_ptr(), workspace.data_ptr(),
-                  int(workspace.numel()))
-    _check(plora_attn_paged(a, _stream_handle(stream)), "plora_attn_paged")
+        workspace = attn_paged_workspace(q, k_cache, n_req, width)
+    elif workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        _bad("workspace: packed uint8 CUDA tensor expected")
+    if (group_start is None) != (prefix_len is None):
+        _bad("group_start and prefix_len go together")
+    n_groups = 0 if prefix_len is None else prefix_len.shape[0]
+    if slopes is not None and (slopes.dtype is not torch.float32 or not slopes.is_cuda or slopes.shape != (hq,)
+                               or not slopes.is_contiguous()):
+        _bad("slopes: packed float32 CUDA tensor [n_q_heads] expected")
+    a = _PAGED_PACK.pack(_type16(q), n, n_req, n_groups, hq, hk, d, page, n_pages, width, _token_stride("q", q), page_stride,
+                         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ints("block_table", block_table, (n_req, width)),
+                         _ints("kv_len", kv_len, (n_req,)), _opt_ints("tok_start", tok_start, (n_req + 1,)),
+                         _opt_ints("group_start", group_start, (n_groups + 1,)), _opt_ints("prefix_len", prefix_len, (n_groups,)),
+                         _opt_ints("key_lo", key_lo, (n,)), _opt_ints("key_hi", key_hi, (n,)),
+                         0 if slopes is None else slopes.data_ptr(), scale, softcap, out.data_ptr(), workspace.data_ptr(),
+                         workspace.numel())
+    rc = load().plora_attn_paged(a, _raw_stream(stream, q))
+    if rc != OK:
+        raise PloraError(rc, "plora_attn_paged")
     return out, workspace
 
 

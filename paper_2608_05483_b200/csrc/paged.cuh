@@ -15,6 +15,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "plora.h"
 
 namespace plora {
@@ -33,15 +35,16 @@ struct TokInfo {    // 16 bytes: keys [lo, hi) are visible to the token, which s
     int32_t lo, hi, pos, pad_;
 };
 
-// How the partial results of a token lie: n[i] of them from number base[i] on, stride[i] apart; i = 0 the
-// token's own keys, i = 1 its group's prefix.  n[0] < 0: its unit writes the output itself.
+// A token whose result has to be put together: n[i] partial results from number base[i] on, stride[i] apart; i = 0 its
+// own keys, i = 1 its group's prefix.  (None at all: a zero row.)  Tokens whose unit writes the output are not listed.
 struct TokMerge {   // 32 bytes
-    int32_t base[2], n[2], stride[2], pad_[2];
+    int32_t tok, base[2], n[2], stride[2], pad_;
 };
+static_assert(sizeof(TokMerge) == 32, "two 16-byte words");
 
 // Workspace header (256 bytes, zero before the first call): word 0 the sticky status word; words 8 and
 // 10 the test hook and the wait limit of plora_attn_set_debug; the rest is rewritten by every call.
-constexpr int kSmallUnitsWord = 1, kBigUnitsWord = 2, kSmallNextWord = 3, kBigNextWord = 4;
+constexpr int kSmallUnitsWord = 1, kBigUnitsWord = 2, kSmallNextWord = 3, kBigNextWord = 4, kMergeWord = 5;
 constexpr int kHookWord = 8, kLimitWord = 10;
 constexpr long long kWaitCycles = 4000000000ll;   // default limit of a wait: about two seconds of SM clock
 
@@ -50,7 +53,8 @@ struct Params {
     Unit* small_units;
     Unit* big_units;
     TokInfo* tok_info;
-    TokMerge* tok_merge;
+    TokMerge* tok_merge;      // [kMergeWord's count]
+    int4* tok_prefix;         // [token] {base, n, stride}: the partial results of its group's prefix
     float2* part_ml;          // [partial token][query head] {m, l}
     float* part_o;            // [partial token][query head][D]
     int32_t cap_small, cap_big, cap_part;
@@ -67,7 +71,7 @@ struct Params {
     const int32_t* key_lo;
     const int32_t* key_hi;
     const float* slopes;
-    int32_t n_tok, n_req, n_groups, n_q_heads, n_kv_heads, G;
+    int32_t n_tok, n_req, n_groups, n_q_heads, n_kv_heads, G, head_dim;
     int32_t page_size, page_shift, n_pages, max_blocks;
     int32_t max_kv;           // min(max_blocks, n_pages) * page_size
     float scale_log2e;        // softmax scale times log2(e): scores live in the base-2 domain
@@ -190,11 +194,26 @@ __device__ __forceinline__ float score(const Params& p, float qk, float slope, i
     return s;
 }
 
+// The kernel's dynamic shared memory is asked for once per device (a host call of half a microsecond otherwise).
+struct Configured {
+    std::atomic<uint64_t> devices{0};
+    cudaError_t ensure(const void* kern, int bytes, int dev) {
+        const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+        if (devices.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+        return e;
+    }
+};
+struct Device {
+    int id, sms;
+};
+
 // ---- launches -----------------------------------------------------------------------------------------
 cudaError_t launch_small(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim, bool fp16,
-                         int sm_count, cudaStream_t st);
+                         Device dev, cudaStream_t st);
 cudaError_t launch_big(const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim,
-                       bool fp16, int sm_count, cudaStream_t st);
+                       bool fp16, Device dev, cudaStream_t st);
 cudaError_t launch_pdl(const void* kern, dim3 grid, dim3 block, size_t smem, cudaStream_t st, void** args);
 
 }  // namespace paged

@@ -56,13 +56,13 @@ __device__ __forceinline__ void token_range(const Params& p, int r, int& tok0, i
 }
 __device__ __forceinline__ int kv_of(const Params& p, int r) { return clampi(p.kv_len[r], 0, p.max_kv); }
 
-// The group's common prefix if its tokens read it together: more than one request, one token each.
-__device__ __forceinline__ int group_prefix(const Params& p, int s, int e) {
-    if (e - s < 2) return 0;
+// Do requests [s, e) read a common prefix together: more than one, and one token each?
+__device__ __forceinline__ bool one_token_each(const Params& p, int s, int e) {
+    if (e - s < 2) return false;
     int t0, t1, n;
     token_range(p, s, t0, n);
     token_range(p, e - 1, t1, n);
-    return t1 + n - t0 == e - s ? 1 : 0;
+    return t1 + n - t0 == e - s;
 }
 
 // Keys [lo, hi) visible to the token at position pos of a cache of kv tokens.
@@ -87,24 +87,38 @@ __device__ __forceinline__ Sums scan_exclusive(const Sums& v, Sums& total, Sums*
     __syncthreads();
     if (lane == 31) warp_sums[warp] = in;
     __syncthreads();
-    Sums before{0, 0, 0}, all{0, 0, 0};
-    for (int w = 0; w < kPlanThreads / 32; ++w) {
-        const Sums x = warp_sums[w];
-        if (w < warp) before = before + x;
-        all = all + x;
+    Sums all = warp_sums[lane];                   // (every warp scans the 32 warps' sums for itself)
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const Sums a{__shfl_up_sync(0xffffffffu, all.small, d), __shfl_up_sync(0xffffffffu, all.big, d),
+                     __shfl_up_sync(0xffffffffu, all.part, d)};
+        if (lane >= d) all = all + a;
     }
+    Sums before{__shfl_sync(0xffffffffu, all.small, max(warp - 1, 0)), __shfl_sync(0xffffffffu, all.big, max(warp - 1, 0)),
+                __shfl_sync(0xffffffffu, all.part, max(warp - 1, 0))};
+    if (warp == 0) before = Sums{0, 0, 0};
+    all = Sums{__shfl_sync(0xffffffffu, all.small, 31), __shfl_sync(0xffffffffu, all.big, 31), __shfl_sync(0xffffffffu, all.part, 31)};
     total = all;
     return Sums{before.small + in.small - v.small, before.big + in.big - v.big, before.part + in.part - v.part};
 }
 
-__device__ __forceinline__ long long sum_all(long long v, long long* red) {
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+__device__ __forceinline__ void sum_all(long long& a, long long& b, long long (*red)[kPlanThreads / 32]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int d = 16; d > 0; d >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, d);
+        b += __shfl_xor_sync(0xffffffffu, b, d);
+    }
+    if (lane == 0) {
+        red[0][warp] = a;
+        red[1][warp] = b;
+    }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    long long s = 0;
-    for (int w = 0; w < kPlanThreads / 32; ++w) s += red[w];
-    return s;
+    a = red[0][lane];
+    b = red[1][lane];
+    for (int d = 16; d > 0; d >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, d);
+        b += __shfl_xor_sync(0xffffffffu, b, d);
+    }
 }
 
 __device__ void write_token_info(const Params& p) {
@@ -123,7 +137,8 @@ __device__ void write_token_info(const Params& p) {
         kv = kv_of(p, r);
         if (t >= end || t < p.tok_start[r]) {        // a token of no request: nothing to see
             p.tok_info[t] = TokInfo{0, 0, 0, 0};
-            p.tok_merge[t] = TokMerge{{0, 0}, {0, 0}, {0, 0}, {0, 0}};   // a zero row
+            uint4* row = reinterpret_cast<uint4*>(p.out + (size_t)t * p.n_q_heads * p.head_dim);
+            for (int i = 0; i < p.n_q_heads * p.head_dim / 8; ++i) row[i] = make_uint4(0u, 0u, 0u, 0u);
             return;
         }
         pos = kv - (end - t);
@@ -135,32 +150,39 @@ __device__ void write_token_info(const Params& p) {
 }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
+    grid_wait();
     grid_launch_dependents();
     if (blockIdx.x > 0) {
         write_token_info(p);
         return;
     }
     __shared__ Sums warp_sums[kPlanThreads / 32];
-    __shared__ long long red[kPlanThreads / 32];
-    __shared__ int s_group[kGroupCache + 1];
+    __shared__ long long red[2][kPlanThreads / 32];
+    __shared__ int s_group[kGroupCache + 1], s_prefix[kGroupCache];
+    __shared__ int s_merge;
     const int tid = threadIdx.x;
+    if (tid == 0) s_merge = 0;
     // tokens of a unit: the rows of a tile of the small kernel, or two tiles of the big one
     const int TBs = max(1, kSmallRows / p.G), TBb = 2 * p.big_tile_tok;
     auto is_small = [&](int n) { return n * p.G <= kSmallRows; };
     const bool cached = p.n_groups <= kGroupCache;
-    for (int g = tid; p.n_groups > 0 && cached && g <= p.n_groups; g += kPlanThreads) s_group[g] = clampi(p.group_start[g], 0, p.n_req);
-    __syncthreads();
-    auto gstart = [&](int g) { return cached ? s_group[g] : clampi(p.group_start[g], 0, p.n_req); };
-    auto prefix_of = [&](int g) {                  // tokens of the prefix that group g reads together, 0: none
-        const int s = gstart(g), e = gstart(g + 1);
-        if (!group_prefix(p, s, e)) return 0;
-        return clampi(p.prefix_len[g], 0, kv_of(p, s));
+    auto group_at = [&](int g) { return clampi(p.group_start[g], 0, p.n_req); };
+    auto read_prefix = [&](int g) {                // tokens of the prefix that group g reads together, 0: none
+        const int s = group_at(g), e = group_at(g + 1), pre = p.prefix_len[g];
+        return one_token_each(p, s, e) ? clampi(pre, 0, kv_of(p, s)) : 0;
     };
+    if (p.n_groups > 0 && cached) {
+        for (int g = tid; g <= p.n_groups; g += kPlanThreads) s_group[g] = group_at(g);
+        for (int g = tid; g < p.n_groups; g += kPlanThreads) s_prefix[g] = read_prefix(g);
+    }
+    __syncthreads();
+    auto gstart = [&](int g) { return cached ? s_group[g] : group_at(g); };
+    auto prefix_of = [&](int g) { return cached ? s_prefix[g] : read_prefix(g); };
     auto request = [&](int r) {
-        Req q;
+        Req q{0, 0, 0, 0};
+        if (r >= p.n_req) return q;
         token_range(p, r, q.tok0, q.n);
         q.kv = kv_of(p, r);
-        q.pre = 0;
         if (p.n_groups > 0) {
             int lo = 0, hi = p.n_groups;
             while (hi - lo > 1) {
@@ -196,8 +218,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
 
     // how many keys there are to read in all, over the units of each kind: the split lengths follow from it
     long long keys_s = 0, keys_b = 0;
+    const Req first = request(tid);              // (kept: most batches have no more requests than the CTA has threads)
     for (int r = tid; r < p.n_req; r += kPlanThreads) {
-        const Req q = request(r);
+        const Req q = r == tid ? first : request(r);
         const int TB = is_small(q.n) ? TBs : TBb;
         long long keys = 0;
         for (int b = 0; b * TB < q.n; ++b) {
@@ -213,8 +236,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         if (is_small(n)) keys_s += pre;
         else keys_b += (long long)pre * ((n + TBb - 1) / TBb);
     }
-    keys_s = sum_all(keys_s, red);
-    keys_b = sum_all(keys_b, red);
+    sum_all(keys_s, keys_b, red);
     const long long per_s = (keys_s * p.n_kv_heads + kSmallItems - 1) / kSmallItems;
     const long long per_b = (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems;
     const int chunk_s = (int)min((long long)INT_MAX / 2, max((long long)kSmallMinKeys, (per_s + 63) / 64 * 64));
@@ -238,25 +260,22 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         }
         const bool small = is_small(n);
         const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b;
-        const int splits = splits_of(pre, small), blocks = pre > 0 ? (n + TB - 1) / TB : 0;
+        int splits = splits_of(pre, small);
+        const int blocks = pre > 0 ? (n + TB - 1) / TB : 0;
         const Sums want{small ? splits * blocks : 0, small ? 0 : splits * blocks, pre > 0 ? splits * n : 0};
         const Sums at = carry + scan_exclusive(want, total, warp_sums);
-        if (pre > 0 && !fits(at, want)) {
-            atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
-            for (int t = 0; t < n; ++t) p.tok_merge[tok0 + t].n[1] = 0;
-        } else if (pre > 0) {
+        if (pre > 0) {
+            if (!fits(at, want)) {
+                atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
+                splits = 0;
+            }
             for (int b = 0; b < blocks; ++b) {
                 const int nt = min(TB, n - b * TB);
                 for (int i = 0; i < splits; ++i)
                     put(small, (small ? at.small : at.big) + b * splits + i,
                         Unit{tok0 + b * TB, nt, s, i * chunk, min(pre, (i + 1) * chunk), at.part + i * n + b * TB, {0, 0}});
-                for (int t = 0; t < nt; ++t) {
-                    TokMerge& m = p.tok_merge[tok0 + b * TB + t];
-                    m.base[1] = at.part + b * TB + t;
-                    m.n[1] = splits;
-                    m.stride[1] = n;
-                }
             }
+            for (int t = 0; t < n; ++t) p.tok_prefix[tok0 + t] = make_int4(at.part + t, splits, n, 0);
         }
         carry = carry + total;
     }
@@ -264,8 +283,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     // the requests' own keys
     for (int r0 = 0; r0 < p.n_req; r0 += kPlanThreads) {
         const int r = r0 + tid;
-        Req q{0, 0, 0, 0};
-        if (r < p.n_req) q = request(r);
+        const Req q = r0 == 0 ? first : request(r);
         const bool small = is_small(q.n);
         const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b;
         Sums want{0, 0, 0};
@@ -277,78 +295,79 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
             if (splits > 1 || q.pre > 0) want.part += splits * min(TB, q.n - b * TB);
         }
         Sums at = carry + scan_exclusive(want, total, warp_sums);
-        if (!fits(at, want)) {
-            atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
-            for (int t = 0; t < q.n; ++t) p.tok_merge[q.tok0 + t] = TokMerge{{0, 0}, {0, 0}, {0, 0}, {0, 0}};
-            q.n = 0;
-        }
+        const bool room = fits(at, want);
+        if (!room) atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
         // (the last block first: it sees the most keys, and the items are taken in this order)
         int unit = small ? at.small : at.big;
         for (int b = (q.n + TB - 1) / TB - 1; b >= 0; --b) {
             int k0, k1;
             block_keys(q, b, TB, k0, k1);
-            const int splits = splits_of(k1 - k0, small), nt = min(TB, q.n - b * TB);
-            const bool partial = splits > 1 || q.pre > 0;
+            const int splits = room ? splits_of(k1 - k0, small) : 0, nt = min(TB, q.n - b * TB);
+            const bool direct = splits == 1 && q.pre == 0;
             for (int i = 0; i < splits; ++i)
                 put(small, unit + i, Unit{q.tok0 + b * TB, nt, r, k0 + i * chunk, min(k1, k0 + (i + 1) * chunk),
-                                          partial ? at.part + i * nt : -1, {0, 0}});
-            for (int t = 0; t < nt; ++t) {
-                TokMerge& m = p.tok_merge[q.tok0 + b * TB + t];
-                m.base[0] = at.part + t;
-                m.n[0] = splits == 1 && !partial ? -1 : splits;
-                m.stride[0] = nt;
-                if (q.pre == 0) m.n[1] = 0;
+                                          direct ? -1 : at.part + i * nt, {0, 0}});
+            if (!direct) {
+                const int m0 = atomicAdd(&s_merge, nt);      // (in any order: every token's result is its own)
+                for (int t = 0; t < nt; ++t) {
+                    const int tok = q.tok0 + b * TB + t;
+                    const int4 pre = q.pre > 0 ? p.tok_prefix[tok] : make_int4(0, 0, 0, 0);
+                    if (m0 + t < p.n_tok) p.tok_merge[m0 + t] = TokMerge{tok, {at.part + t, pre.x}, {splits, pre.y}, {nt, pre.z}, 0};
+                }
+                at.part += splits * nt;
             }
             unit += splits;
-            if (partial) at.part += splits * nt;
         }
         carry = carry + total;
     }
+    __syncthreads();
     if (tid == 0) {
         p.header[kSmallUnitsWord] = min(carry.small, p.cap_small);
         p.header[kBigUnitsWord] = min(carry.big, p.cap_big);
         p.header[kSmallNextWord] = 0;
         p.header[kBigNextWord] = 0;
+        p.header[kMergeWord] = min(s_merge, p.n_tok);
     }
 }
 
-// One warp per (token, query head): the token's partial results, rescaled by their maxima.
+// One warp per (listed token, query head): the token's partial results, rescaled by their maxima.
 template <int D, bool FP16>
 __global__ void __launch_bounds__(128) merge_kernel(const Params p) {
     grid_wait();
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (row >= (long long)p.n_tok * p.n_q_heads) return;
+    grid_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const int t = (int)(row / p.n_q_heads), hq = (int)(row - (long long)t * p.n_q_heads);
-    const TokMerge tm = p.tok_merge[t];
-    if (tm.n[0] < 0) return;
-    constexpr int V = D / 32;
-    float o[V], M = -INFINITY, L = 0.f;
+    const long long rows = (long long)p.header[kMergeWord] * p.n_q_heads;
+    for (long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); row < rows; row += (long long)gridDim.x * 4) {
+        const int hq = (int)(row % p.n_q_heads);
+        const TokMerge tm = p.tok_merge[row / p.n_q_heads];
+        constexpr int V = D / 32;
+        float o[V], M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) o[v] = 0.f;
+        for (int v = 0; v < V; ++v) o[v] = 0.f;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-        for (int i = 0; i < tm.n[s]; ++i) M = fmaxf(M, p.part_ml[(size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq].x);
-    const float Me = M == -INFINITY ? 0.f : M;
+        for (int s = 0; s < 2; ++s)
+            for (int i = 0; i < tm.n[s]; ++i) M = fmaxf(M, p.part_ml[(size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq].x);
+        const float Me = M == -INFINITY ? 0.f : M;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-        for (int i = 0; i < tm.n[s]; ++i) {
-            const size_t at = (size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq;
-            const float2 ml = p.part_ml[at];
-            const float f = ex2(ml.x - Me);
-            L = fmaf(f, ml.y, L);
-            const float* src = p.part_o + at * D + lane * V;
+        for (int s = 0; s < 2; ++s)
+            for (int i = 0; i < tm.n[s]; ++i) {
+                const size_t at = (size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq;
+                const float2 ml = p.part_ml[at];
+                const float f = ex2(ml.x - Me);
+                L = fmaf(f, ml.y, L);
+                const float* src = p.part_o + at * D + lane * V;
 #pragma unroll
-            for (int v = 0; v < V; v += 2) {
-                const float2 x = *reinterpret_cast<const float2*>(src + v);
-                o[v] = fmaf(f, x.x, o[v]);
-                o[v + 1] = fmaf(f, x.y, o[v + 1]);
+                for (int v = 0; v < V; v += 2) {
+                    const float2 x = *reinterpret_cast<const float2*>(src + v);
+                    o[v] = fmaf(f, x.x, o[v]);
+                    o[v + 1] = fmaf(f, x.y, o[v + 1]);
+                }
             }
-        }
-    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);    // nothing visible: a zero row
-    uint16_t* dst = p.out + (size_t)row * D + lane * V;
+        const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);    // nothing visible: a zero row
+        uint16_t* dst = p.out + ((size_t)tm.tok * p.n_q_heads + hq) * D + lane * V;
 #pragma unroll
-    for (int v = 0; v < V; v += 2) *reinterpret_cast<uint32_t*>(dst + v) = pack16<FP16>(o[v] * inv, o[v + 1] * inv);
+        for (int v = 0; v < V; v += 2) *reinterpret_cast<uint32_t*>(dst + v) = pack16<FP16>(o[v] * inv, o[v + 1] * inv);
+    }
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -385,7 +404,7 @@ Caps caps(long long n_tok, long long n_req, long long max_kv, int n_kv_heads, in
 }
 
 struct Layout {
-    size_t small, big, info, merge, ml, o, total;
+    size_t small, big, info, merge, prefix, ml, o, total;
 };
 Layout layout(const Caps& c, long long n_tok, int n_q_heads, int head_dim) {
     Layout l;
@@ -394,6 +413,7 @@ Layout layout(const Caps& c, long long n_tok, int n_q_heads, int head_dim) {
     l.big = at; at += up256((size_t)c.big * sizeof(Unit));
     l.info = at; at += up256((size_t)n_tok * sizeof(TokInfo));
     l.merge = at; at += up256((size_t)n_tok * sizeof(TokMerge));
+    l.prefix = at; at += up256((size_t)n_tok * sizeof(int4));
     l.ml = at; at += up256((size_t)c.part * n_q_heads * sizeof(float2));
     l.o = at; at += up256((size_t)c.part * n_q_heads * head_dim * sizeof(float));
     l.total = at;
@@ -443,6 +463,7 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     Params p{};
     p.n_tok = a->n_tok; p.n_req = a->n_req; p.n_groups = a->n_groups;
     p.n_q_heads = a->n_q_heads; p.n_kv_heads = a->n_kv_heads; p.G = a->n_q_heads / a->n_kv_heads;
+    p.head_dim = a->head_dim;
     p.big_tile_tok = tile_tokens(p.G);
     p.page_size = a->page_size; p.n_pages = a->n_pages; p.max_blocks = a->max_blocks;
     for (p.page_shift = 0; (1 << p.page_shift) < p.page_size; ++p.page_shift) {}
@@ -457,6 +478,7 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     p.big_units = reinterpret_cast<Unit*>(ws + l.big);
     p.tok_info = reinterpret_cast<TokInfo*>(ws + l.info);
     p.tok_merge = reinterpret_cast<TokMerge*>(ws + l.merge);
+    p.tok_prefix = reinterpret_cast<int4*>(ws + l.prefix);
     p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     p.part_o = reinterpret_cast<float*>(ws + l.o);
     p.cap_small = (int32_t)c.small; p.cap_big = (int32_t)c.big; p.cap_part = (int32_t)c.part;
@@ -496,21 +518,27 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
                        qdims, qstrides, qbox, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return PLORA_ERR_INVALID_ARG;
-    int dev = 0, sm_count = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return PLORA_ERR_CUDA;
+    Device dev{0, 0};
+    static std::atomic<int> sms_of[64];
+    if (cudaGetDevice(&dev.id) != cudaSuccess) return PLORA_ERR_CUDA;
+    if (dev.id < 64) dev.sms = sms_of[dev.id].load(std::memory_order_relaxed);
+    if (dev.sms == 0) {
+        if (cudaDeviceGetAttribute(&dev.sms, cudaDevAttrMultiProcessorCount, dev.id) != cudaSuccess) return PLORA_ERR_CUDA;
+        if (dev.id < 64) sms_of[dev.id].store(dev.sms, std::memory_order_relaxed);
+    }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    plan_kernel<<<1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads, kPlanThreads, 0, st>>>(p);
-    if (cudaGetLastError() != cudaSuccess) return PLORA_ERR_CUDA;
-    // one token per request, no groups: nothing can be larger than a small unit (and more than 16 heads never make one)
-    if ((p.tok_start || p.n_groups > 0 || p.G > kSmallRows) &&
-        launch_big(tq, tm[0], tm[1], p, a->head_dim, fp16, sm_count, st) != cudaSuccess)
-        return PLORA_ERR_CUDA;
-    if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, sm_count, st) != cudaSuccess) return PLORA_ERR_CUDA;
     void* args[] = {&p};
+    if (launch_pdl((const void*)plan_kernel, dim3(1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads), dim3(kPlanThreads), 0, st, args) !=
+        cudaSuccess)
+        return PLORA_ERR_CUDA;
+    // a small unit holds whatever fits into its rows; single tokens that share nothing always do
+    const bool big = p.G > kSmallRows || ((p.tok_start || p.n_groups > 0) && (long long)p.n_tok * p.G > kSmallRows);
+    if (big && launch_big(tq, tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return PLORA_ERR_CUDA;
+    if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return PLORA_ERR_CUDA;
     const void* mk = a->head_dim == 128 ? (fp16 ? (const void*)merge_kernel<128, true> : (const void*)merge_kernel<128, false>)
                                         : (fp16 ? (const void*)merge_kernel<64, true> : (const void*)merge_kernel<64, false>);
-    const long long rows = (long long)p.n_tok * p.n_q_heads;
-    if (launch_pdl(mk, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, args) != cudaSuccess) return PLORA_ERR_CUDA;
+    const long long ctas = ((long long)p.n_tok * p.n_q_heads + 3) / 4;
+    const int most = dev.sms * 16;
+    if (launch_pdl(mk, dim3((unsigned)(ctas < most ? ctas : most)), dim3(128), 0, st, args) != cudaSuccess) return PLORA_ERR_CUDA;
     return PLORA_OK;
 }

@@ -537,29 +537,30 @@ big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
 }
 
 template <int D, bool FP16, bool CAP, bool BIAS>
-cudaError_t go(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int sms, cudaStream_t st) {
+cudaError_t go(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, Device dev, cudaStream_t st) {
     auto kern = big_kernel<D, FP16, CAP, BIAS>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmemBytes);
+    static Configured configured;
+    const cudaError_t e = configured.ensure(reinterpret_cast<const void*>(kern), Cfg<D>::kSmemBytes, dev.id);
     if (e != cudaSuccess) return e;
     const long long items = (long long)p.cap_big * p.n_kv_heads;
-    const int grid = (int)(items < sms ? items : sms);
+    const int grid = (int)(items < dev.sms ? items : dev.sms);
     void* args[] = {const_cast<CUtensorMap*>(&q), const_cast<CUtensorMap*>(&k), const_cast<CUtensorMap*>(&v), const_cast<Params*>(&p)};
     return launch_pdl(reinterpret_cast<const void*>(kern), dim3(grid), dim3(kThreads), Cfg<D>::kSmemBytes, st, args);
 }
 template <int D, bool FP16>
-cudaError_t go2(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int sms, cudaStream_t st) {
+cudaError_t go2(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, Device dev, cudaStream_t st) {
     // (a scale that is not positive takes the form that scales before it masks and looks for the maximum)
     const bool cap = p.cap_log2e > 0.f, bias = p.slopes || !(p.scale_log2e > 0.f);
-    if (cap) return bias ? go<D, FP16, true, true>(q, k, v, p, sms, st) : go<D, FP16, true, false>(q, k, v, p, sms, st);
-    return bias ? go<D, FP16, false, true>(q, k, v, p, sms, st) : go<D, FP16, false, false>(q, k, v, p, sms, st);
+    if (cap) return bias ? go<D, FP16, true, true>(q, k, v, p, dev, st) : go<D, FP16, true, false>(q, k, v, p, dev, st);
+    return bias ? go<D, FP16, false, true>(q, k, v, p, dev, st) : go<D, FP16, false, false>(q, k, v, p, dev, st);
 }
 
 }  // namespace
 
 cudaError_t launch_big(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int head_dim, bool fp16,
-                       int sms, cudaStream_t st) {
-    if (head_dim == 128) return fp16 ? go2<128, true>(q, k, v, p, sms, st) : go2<128, false>(q, k, v, p, sms, st);
-    return fp16 ? go2<64, true>(q, k, v, p, sms, st) : go2<64, false>(q, k, v, p, sms, st);
+                       Device dev, cudaStream_t st) {
+    if (head_dim == 128) return fp16 ? go2<128, true>(q, k, v, p, dev, st) : go2<128, false>(q, k, v, p, dev, st);
+    return fp16 ? go2<64, true>(q, k, v, p, dev, st) : go2<64, false>(q, k, v, p, dev, st);
 }
 
 }  // namespace paged

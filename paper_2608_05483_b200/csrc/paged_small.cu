@@ -345,28 +345,28 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
 }
 
 template <int D, bool FP16, bool CAP, bool BIAS>
-cudaError_t go(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int sm_count, cudaStream_t st) {
+cudaError_t go(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, Device dev, cudaStream_t st) {
     auto kern = small_kernel<D, FP16, CAP, BIAS>;
-    // (set at every call: it is a host-side table write, and a process may use more than one device)
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmemBytes);
+    static Configured configured;
+    const cudaError_t e = configured.ensure(reinterpret_cast<const void*>(kern), Cfg<D>::kSmemBytes, dev.id);
     if (e != cudaSuccess) return e;
     const long long items = (long long)p.cap_small * p.n_kv_heads;
-    const int grid = (int)(items < 2 * sm_count ? items : 2 * sm_count);
+    const int grid = (int)(items < 2 * dev.sms ? items : 2 * dev.sms);
     void* args[] = {const_cast<CUtensorMap*>(&tm_k), const_cast<CUtensorMap*>(&tm_v), const_cast<Params*>(&p)};
     return launch_pdl(reinterpret_cast<const void*>(kern), dim3(grid), dim3(kThreads), Cfg<D>::kSmemBytes, st, args);
 }
 template <int D, bool FP16>
-cudaError_t go2(const CUtensorMap& k, const CUtensorMap& v, const Params& p, int sms, cudaStream_t st) {
-    if (p.cap_log2e > 0.f) return p.slopes ? go<D, FP16, true, true>(k, v, p, sms, st) : go<D, FP16, true, false>(k, v, p, sms, st);
-    return p.slopes ? go<D, FP16, false, true>(k, v, p, sms, st) : go<D, FP16, false, false>(k, v, p, sms, st);
+cudaError_t go2(const CUtensorMap& k, const CUtensorMap& v, const Params& p, Device dev, cudaStream_t st) {
+    if (p.cap_log2e > 0.f) return p.slopes ? go<D, FP16, true, true>(k, v, p, dev, st) : go<D, FP16, true, false>(k, v, p, dev, st);
+    return p.slopes ? go<D, FP16, false, true>(k, v, p, dev, st) : go<D, FP16, false, false>(k, v, p, dev, st);
 }
 
 }  // namespace
 
-cudaError_t launch_small(const CUtensorMap& k, const CUtensorMap& v, const Params& p, int head_dim, bool fp16, int sms,
+cudaError_t launch_small(const CUtensorMap& k, const CUtensorMap& v, const Params& p, int head_dim, bool fp16, Device dev,
                          cudaStream_t st) {
-    if (head_dim == 128) return fp16 ? go2<128, true>(k, v, p, sms, st) : go2<128, false>(k, v, p, sms, st);
-    return fp16 ? go2<64, true>(k, v, p, sms, st) : go2<64, false>(k, v, p, sms, st);
+    if (head_dim == 128) return fp16 ? go2<128, true>(k, v, p, dev, st) : go2<128, false>(k, v, p, dev, st);
+    return fp16 ? go2<64, true>(k, v, p, dev, st) : go2<64, false>(k, v, p, dev, st);
 }
 
 }  // namespace paged
