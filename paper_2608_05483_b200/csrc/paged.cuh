@@ -75,6 +75,7 @@ struct Params {
     int32_t page_size, page_shift, n_pages, max_blocks;
     int32_t max_kv;           // min(max_blocks, n_pages) * page_size
     float scale_log2e;        // softmax scale times log2(e): scores live in the base-2 domain
+    float cap_x;              // scale / cap
     float cap_in, cap_log2e;  // capped scores: cap_log2e * tanh(cap_in * qk), cap_in already times 2 log2(e)
 };
 
@@ -131,6 +132,15 @@ __device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, Wa
 }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const WaitCtl& w) {
     if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait_slow(bar, parity, w);
+}
+// The same for warps that nobody waits for: they look less often and leave the issue slots to the others.
+__device__ __forceinline__ bool mbar_wait_lazy(uint32_t bar, uint32_t parity, const WaitCtl& w) {
+    for (int i = 0; i < 1 << 20; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*w.abort_flag) return false;
+        __nanosleep(100);
+    }
     return mbar_wait_slow(bar, parity, w);
 }
 // A last look at a barrier before a CTA leaves, whatever the abort flag says: copies in flight must land first.

@@ -29,8 +29,8 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatever the device has: it sizes the workspace
 constexpr int kSmallItems = kPlanSms * 2 * 8;   // aimed-at items of the small kernel (two CTAs per SM)
 constexpr int kSmallMinKeys = 128;     // no split shorter than this
-constexpr int kBigItems = kPlanSms * 2;         // aimed-at items of the tensor-core kernel (one CTA per SM)
-constexpr int kBigMinKeys = 512;
+constexpr int kBigItems = kPlanSms * 8;         // aimed-at items of the tensor-core kernel (one CTA per SM)
+constexpr int kBigMinKeys = 512, kBigMaxKeys = 1 << 22;     // (tiles of keys are counted in 16 bits)
 constexpr int kGroupCache = 2048;      // group starts held in shared memory
 
 struct Sums {        // counts that the scan carries along
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     const long long per_s = (keys_s * p.n_kv_heads + kSmallItems - 1) / kSmallItems;
     const long long per_b = (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems;
     const int chunk_s = (int)min((long long)INT_MAX / 2, max((long long)kSmallMinKeys, (per_s + 63) / 64 * 64));
-    const int chunk_b = (int)min((long long)INT_MAX / 2, max((long long)kBigMinKeys, (per_b + 127) / 128 * 128));
+    const int chunk_b = (int)min((long long)kBigMaxKeys, max((long long)kBigMinKeys, (per_b + 127) / 128 * 128));
     auto splits_of = [&](int keys, bool small) { const int c = small ? chunk_s : chunk_b; return (keys + c - 1) / c; };
     auto fits = [&](const Sums& at, const Sums& want) {
         return at.small + want.small <= p.cap_small && at.big + want.big <= p.cap_big && at.part + want.part <= p.cap_part;
@@ -420,6 +420,12 @@ Layout layout(const Caps& c, long long n_tok, int n_q_heads, int head_dim) {
     return l;
 }
 
+// A launch that was refused leaves its error behind in the runtime; it is reported here and must not be found by a later call.
+plora_status cuda_failed() {
+    (void)cudaGetLastError();
+    return PLORA_ERR_CUDA;
+}
+
 bool supported(int n_q_heads, int n_kv_heads, int head_dim, int page_size) {
     if (head_dim != 64 && head_dim != 128) return false;
     if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128) return false;
@@ -491,6 +497,7 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     const float log2e = 1.4426950408889634f;
     p.scale_log2e = a->scale * log2e;
     if (a->softcap > 0.f) {
+        p.cap_x = a->scale / a->softcap;
         p.cap_in = 2.f * log2e * a->scale / a->softcap;
         p.cap_log2e = a->softcap * log2e;
     }
@@ -520,25 +527,25 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
         return PLORA_ERR_INVALID_ARG;
     Device dev{0, 0};
     static std::atomic<int> sms_of[64];
-    if (cudaGetDevice(&dev.id) != cudaSuccess) return PLORA_ERR_CUDA;
+    if (cudaGetDevice(&dev.id) != cudaSuccess) return cuda_failed();
     if (dev.id < 64) dev.sms = sms_of[dev.id].load(std::memory_order_relaxed);
     if (dev.sms == 0) {
-        if (cudaDeviceGetAttribute(&dev.sms, cudaDevAttrMultiProcessorCount, dev.id) != cudaSuccess) return PLORA_ERR_CUDA;
+        if (cudaDeviceGetAttribute(&dev.sms, cudaDevAttrMultiProcessorCount, dev.id) != cudaSuccess) return cuda_failed();
         if (dev.id < 64) sms_of[dev.id].store(dev.sms, std::memory_order_relaxed);
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     void* args[] = {&p};
     if (launch_pdl((const void*)plan_kernel, dim3(1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads), dim3(kPlanThreads), 0, st, args) !=
         cudaSuccess)
-        return PLORA_ERR_CUDA;
+        return cuda_failed();
     // a small unit holds whatever fits into its rows; single tokens that share nothing always do
     const bool big = p.G > kSmallRows || ((p.tok_start || p.n_groups > 0) && (long long)p.n_tok * p.G > kSmallRows);
-    if (big && launch_big(tq, tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return PLORA_ERR_CUDA;
-    if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return PLORA_ERR_CUDA;
+    if (big && launch_big(tq, tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return cuda_failed();
+    if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return cuda_failed();
     const void* mk = a->head_dim == 128 ? (fp16 ? (const void*)merge_kernel<128, true> : (const void*)merge_kernel<128, false>)
                                         : (fp16 ? (const void*)merge_kernel<64, true> : (const void*)merge_kernel<64, false>);
     const long long ctas = ((long long)p.n_tok * p.n_q_heads + 3) / 4;
     const int most = dev.sms * 16;
-    if (launch_pdl(mk, dim3((unsigned)(ctas < most ? ctas : most)), dim3(128), 0, st, args) != cudaSuccess) return PLORA_ERR_CUDA;
+    if (launch_pdl(mk, dim3((unsigned)(ctas < most ? ctas : most)), dim3(128), 0, st, args) != cudaSuccess) return cuda_failed();
     return PLORA_OK;
 }

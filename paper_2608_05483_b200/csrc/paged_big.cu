@@ -5,14 +5,21 @@
 //     O[128 rows, D]       += P V          P from tensor memory, where it replaces the S it was made of
 // A unit has two tiles of 128 rows (query tokens times the G heads of a KV head); they share every tile of
 // K and V, and while one tile's scores are in the softmax the tensor cores work for the other.
-// Roles: warps 0-3 and 4-7 are the softmax of the two tiles, a row per thread (no shuffles); warp 8 issues the
-// MMAs; warp 9 fetches items from a counter and keeps K and V coming through a ring (tensor-map boxes, one per page
-// piece).  Tensor memory (all 512 columns): S of the two tiles, O of the two tiles.
+// Roles: warps 0-7 and 8-15 are the softmax of the two tiles, half a row per thread; warps 16 and 17 issue their MMAs;
+// warp 18 fetches items from a counter and keeps K and V coming through a ring (tensor-map boxes, one per page piece);
+// warp 19 clears the rows of V behind an item's last key.  Tensor memory (all 512 columns): S of the two tiles, O of the
+// two tiles.
 //
 // The running maximum is followed lazily: O and l are rescaled only when a row's maximum has grown by more than
 // 2^8 over the one in use (P then stays below 2^8, far inside both 16-bit types, and fp32 sums do not care), so the
 // accumulator in tensor memory is hardly ever touched between the products.
 // P is rounded to the input type for the second product; l sums the unrounded weights in fp32.
+//
+// A tile's step is: scores (512 cycles of the tensor pipe at D = 128), softmax, O += P V (512).  The special-function unit
+// alone would take 1024 cycles for a tile's 16384 exponentials, so part of them is computed on the FMA pipe
+// (2^x = 2^n p(f), n the nearest integer, p a polynomial of degree 4 fitted on [-1/2, 1/2], relative error 2.6e-6); and
+// two threads share a row, because with one a scheduler has two warps to choose from and a tile's softmax takes twice as
+// long as its instructions.
 #include <limits.h>
 
 #include "paged.cuh"
@@ -22,11 +29,14 @@ namespace paged {
 namespace {
 
 constexpr int kTileKeys = 128;
-constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 9;
-constexpr int kThreads = 12 * 32;       // three warpgroups; the last one's two other warps only give their registers away
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;      // of 168 a thread at launch: 2 * 208 + 88 = 3 * 168
+constexpr int kSoftmaxWarps = 16, kMmaWarp = 16, kLoadWarp = 18, kTailWarp = 19;
+constexpr int kThreads = 20 * 32;
+constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;       // of 96 a thread at launch: 4 * 104 + 64 = 5 * 96
 constexpr int kSched = 2;
+constexpr int kEmulated = 6;        // of 16 pairs of weights, how many are computed on the FMA pipe
 constexpr float kLazy = 8.f;        // base-2 logarithm of the growth a row's maximum may have before O is rescaled
+
+constexpr int kExchangeBytes = kSoftmaxWarps * 32 * 4 + 2 * kSoftmaxWarps * 4;    // a float per row and half; a word per warp, twice
 
 template <int D>
 struct Cfg {
@@ -34,22 +44,25 @@ struct Cfg {
     static constexpr int kPanelBytes = 128 * 128;            // 128 rows of 64 values, 128-byte swizzled
     static constexpr int kTileBytes = kPanels * kPanelBytes;
     static constexpr int kStages = D == 128 ? 5 : 8;
-    static constexpr int kBars = 2 * kStages + 2 + 6 + 2 * kSched + 1;
-    static constexpr int kSmemBytes = 1024 + 2 * kTileBytes + kStages * kTileBytes + kBars * 8 + kSched * 48 + 32;
+    static constexpr int kBars = 2 * kStages + 2 + 6 + 2 * kSched + 4 + 8;
+    static constexpr int kSmemBytes = 2 * kTileBytes + kStages * kTileBytes + kBars * 8 + kSched * 48 + 32 + kExchangeBytes;
 };
 constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemTile = 128;    // column of tile t: base + t * 128
 
 struct Item {       // 48 bytes
     int32_t head, tok0, ntok, req;
     int32_t kf, n_tiles, k0, k1;     // first key of the first tile; keys [k0, k1)
-    int32_t part, more, pad_[2];     // more = 0: nothing follows
+    int32_t part, more;              // more = 0: nothing follows
+    int32_t range[2];                // of each tile of rows: the tiles of keys it looks at, first | (one past the last) << 16
 };
+__device__ __forceinline__ int range_first(int r) { return r & 0xffff; }
+__device__ __forceinline__ int range_end(int r) { return (int)((unsigned)r >> 16); }
 
 // ---- tcgen05 ------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // Shared-memory matrix descriptor: start address, leading and stride byte offsets (16-byte units), version 1, 128-byte swizzle.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+__device__ __forceinline__ constexpr uint64_t smem_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
     return (uint64_t)((saddr >> 4) & 0x3fffu) | ((uint64_t)((lbo >> 4) & 0x3fffu) << 16) | ((uint64_t)((sbo >> 4) & 0x3fffu) << 32) |
            ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
@@ -86,6 +99,15 @@ __device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t* r) {
           "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(a));
 }
+__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(a)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
@@ -111,15 +133,16 @@ __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* tm, in
 
 struct Smem {
     uint32_t q, ring;
-    uint32_t kv_full, kv_empty, q_full, q_empty, s_full, p_ready, o_full, sched_full, sched_empty, wind_down;
+    uint32_t kv_full, kv_empty, q_full, q_empty, s_full, p_ready, o_full, sched_full, sched_empty, wind_down, tail_go, tail_done, pair;
+    float* exchange;
+    uint32_t* votes;
     Item* items;
     uint32_t* tmem_slot;
     WaitCtl wc;
 };
 template <int D>
-__device__ __forceinline__ Smem carve(uint8_t* raw, const Params& p) {
+__device__ __forceinline__ Smem carve(uint8_t* base, const Params& p) {
     using C = Cfg<D>;
-    uint8_t* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     uint8_t* items = base + (2 + C::kStages) * C::kTileBytes;
     uint8_t* bars = items + kSched * sizeof(Item);
     uint8_t* words = bars + C::kBars * 8;
@@ -137,13 +160,18 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, const Params& p) {
     s.sched_full = s.o_full + 16;
     s.sched_empty = s.sched_full + kSched * 8;
     s.wind_down = s.sched_empty + kSched * 8;
+    s.tail_go = s.wind_down + 16;
+    s.tail_done = s.tail_go + 8;
+    s.pair = s.tail_done + 8;
+    s.exchange = reinterpret_cast<float*>(words + 16);
+    s.votes = reinterpret_cast<uint32_t*>(words + 16 + kSoftmaxWarps * 32 * 4);
     s.wc.abort_flag = reinterpret_cast<volatile int*>(words);
     s.wc.header = p.header;
     s.tmem_slot = reinterpret_cast<uint32_t*>(words + 8);
     return s;
 }
 
-// ---- warp 9: items, queries, keys and values -----------------------------------------------------------------
+// ---- warp 18: items, queries, keys and values -----------------------------------------------------------------
 template <int D>
 __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const CUtensorMap* tm_q, const CUtensorMap* tm_k,
                                           const CUtensorMap* tm_v, int n_items, int lane) {
@@ -164,28 +192,40 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
             const Unit u = p.big_units[un];
             d.head = item - un * p.n_kv_heads;
             d.tok0 = u.tok0; d.ntok = u.ntok; d.req = u.req; d.part = u.part;
-            // the keys that one of the tokens sees
-            int lo = INT_MAX, hi = 0;
+            // the keys that one of the tokens sees, for each tile of rows
+            int lo[2] = {INT_MAX, INT_MAX}, hi[2] = {0, 0};
             for (int t = lane; t < u.ntok; t += 32) {
                 const TokInfo ti = p.tok_info[u.tok0 + t];
-                if (ti.lo < ti.hi) {
-                    lo = min(lo, ti.lo);
-                    hi = max(hi, ti.hi);
+                const int a = max(ti.lo, u.k0), b = min(ti.hi, u.k1);
+                if (a < b) {
+                    if (t < TT) {
+                        lo[0] = min(lo[0], a);
+                        hi[0] = max(hi[0], b);
+                    } else {
+                        lo[1] = min(lo[1], a);
+                        hi[1] = max(hi[1], b);
+                    }
                 }
             }
-            lo = __reduce_min_sync(all, lo);
-            hi = __reduce_max_sync(all, hi);
-            d.k0 = max(lo, u.k0);
-            d.k1 = min(hi, u.k1);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                lo[t] = __reduce_min_sync(all, lo[t]);
+                hi[t] = __reduce_max_sync(all, hi[t]);
+            }
+            d.k0 = min(lo[0], lo[1]);
+            d.k1 = max(hi[0], hi[1]);
             if (d.k0 >= d.k1) d.k0 = d.k1 = 0;
             d.kf = d.k0 / bp * bp;
             d.n_tiles = (d.k1 - d.kf + kTileKeys - 1) / kTileKeys;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                d.range[t] = hi[t] > 0 ? (lo[t] - d.kf) / kTileKeys | ((hi[t] - d.kf + kTileKeys - 1) / kTileKeys) << 16 : 0;
             d.more = 1;
         }
         const uint32_t ss = ic % kSched;
         int ok = 1;
         if (lane == 0) {
-            ok = mbar_wait(sm.sched_empty + ss * 8, ((ic / kSched) & 1) ^ 1, sm.wc);
+            ok = mbar_wait_lazy(sm.sched_empty + ss * 8, ((ic / kSched) & 1) ^ 1, sm.wc);
             if (ok) {
                 sm.items[ss] = d;
                 mbar_arrive(sm.sched_full + ss * 8);
@@ -199,7 +239,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
         if (d.n_tiles == 0) continue;
         const int tiles_q = d.ntok > TT ? 2 : 1;
         if (lane == 0) {
-            ok = mbar_wait(sm.q_empty, (qn & 1) ^ 1, sm.wc);
+            ok = mbar_wait_lazy(sm.q_empty, (qn & 1) ^ 1, sm.wc);
             if (ok) {
                 mbar_arrive_expect_tx(sm.q_full, (uint32_t)tiles_q * TT * p.G * D * 2);
                 for (int t = 0; t < tiles_q; ++t)
@@ -227,7 +267,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
             for (int kv = 0; kv < 2; ++kv, ++it) {
                 const uint32_t slot = it % C::kStages, dst = sm.ring + slot * C::kTileBytes, bar = sm.kv_full + slot * 8;
                 if (lane == 0) {
-                    ok = mbar_wait(sm.kv_empty + slot * 8, ((it / C::kStages) & 1) ^ 1, sm.wc);
+                    ok = mbar_wait_lazy(sm.kv_empty + slot * 8, ((it / C::kStages) & 1) ^ 1, sm.wc);
                     if (ok) mbar_arrive_expect_tx(bar, (uint32_t)nb * bp * D * 2);
                 }
                 if (!__shfl_sync(all, ok, 0)) {
@@ -255,110 +295,234 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
     __syncwarp();
 }
 
-// ---- warp 8: the products -------------------------------------------------------------------------------------
+// ---- warps 16 and 17: the products of the two tiles -----------------------------------------------------------------
+// A warp per tile, so that what one does between its products (barriers, hand-backs) falls into the other's.  The warp
+// stays together and one elected lane issues: the MMA's operands are uniform registers, and under a plain `lane == 0` the
+// compiler cannot know that a single lane is active (an MMA then cost the issuer about 100 cycles, more than the 64 it
+// takes).  The upper half of a matrix descriptor is the same for all operands of a kind, and the lower half is an address
+// that advances by constants.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 template <int D, bool FP16>
-__device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32_t tmem, int lane) {
+__device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32_t tmem, int t) {
     using C = Cfg<D>;
     const unsigned all = 0xffffffffu;
     constexpr uint32_t idesc_s = instr_desc(kTileKeys, false, FP16), idesc_o = instr_desc(D, true, FP16);
+    constexpr uint32_t kHi = (uint32_t)(smem_desc(0, 0, 1024) >> 32);
+    constexpr uint32_t kLoK = 1u << 16, kLoV = (uint32_t)(C::kPanelBytes >> 4) << 16;     // leading offsets: unused; the next panel
     const bool withhold = p.header[kHookWord] == PLORA_HOOK_WITHHOLD_RELEASE;   // test hook: stages are never handed back
-    const int TT = p.big_tile_tok;
-    uint32_t it = 0, ic = 0, qn = 0, np[2] = {0, 0};
+    uint32_t it = 0, ic = 0, qn = 0, tails = 0, np = 0;
+    t = (int)uniform((uint32_t)t);
+    const uint32_t q = uniform((sm.q >> 4) | kLoK) + t * (C::kTileBytes >> 4), ring_lo = uniform(sm.ring >> 4);
+    const uint32_t ts = uniform(tmem) + kTmemS + t * kTmemTile, o = uniform(tmem) + kTmemO + t * kTmemTile;
+    const uint32_t s_full = sm.s_full + t * 8, p_ready = sm.p_ready + t * 8, o_full = sm.o_full + t * 8;
     bool ok = true;
     auto wait_for = [&](uint32_t bar, uint32_t parity) {
         ok = __all_sync(all, mbar_wait(bar, parity, sm.wc));
         return ok;
     };
-    auto scores = [&](int t, uint32_t slot) {        // S of tile t = Q K^T over the stage's keys
-        const uint32_t q = sm.q + t * C::kTileBytes, k = sm.ring + slot * C::kTileBytes, d = tmem + kTmemS + t * kTmemTile;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            const uint32_t off = (s >> 2) * C::kPanelBytes + (s & 3) * 32;
-            umma_ss(d, smem_desc(q + off, 16, 1024), smem_desc(k + off, 16, 1024), idesc_s, s > 0);
-        }
-        umma_commit(sm.s_full + t * 8);
-    };
     for (;; ++ic) {
         const uint32_t ss = ic % kSched;
         if (!wait_for(sm.sched_full + ss * 8, (ic / kSched) & 1)) break;
-        const Item d = sm.items[ss];
+        const Item& src = sm.items[ss];
+        const int n_tiles = (int)uniform(src.n_tiles), more = (int)uniform(src.more), last = (int)uniform(src.k1 - src.kf);
+        const int range = (int)uniform(src.range[t]), first = range_first(range), end = range_end(range);
         __syncwarp();
-        if (lane == 0) mbar_arrive(sm.sched_empty + ss * 8);
-        if (!d.more) break;
-        if (d.n_tiles == 0) continue;
-        const int tiles_q = d.ntok > TT ? 2 : 1;
+        if (elect_one()) mbar_arrive(sm.sched_empty + ss * 8);
+        if (!more) break;
+        if (n_tiles == 0) continue;
         if (!wait_for(sm.q_full, qn & 1)) break;
         ++qn;
-        // first scores
-        uint32_t slot = it % C::kStages;
-        if (!wait_for(sm.kv_full + slot * 8, (it / C::kStages) & 1)) break;
-        tc_fence_after();
-        if (lane == 0) {
-            for (int t = 0; t < tiles_q; ++t) scores(t, slot);
-            if (!withhold) umma_commit(sm.kv_empty + slot * 8);
-            if (d.n_tiles == 1) umma_commit(sm.q_empty);
-        }
-        ++it;
-        for (int j = 0; j < d.n_tiles && ok; ++j) {
-            const uint32_t vs = it % C::kStages, v = sm.ring + vs * C::kTileBytes;
-            if (!wait_for(sm.kv_full + vs * 8, (it / C::kStages) & 1)) break;
-            ++it;
-            const int left = d.k1 - (d.kf + j * kTileKeys);          // keys of this tile that count
-            const int steps = left >= kTileKeys ? kTileKeys / 16 : (left + 15) / 16;
-            if (left < steps * 16) {
-                // rows of V behind the last key may hold anything: 0 * NaN must not reach the sum
-                const int n = (steps * 16 - left) * (D / 8);
-                for (int i = lane; i < n; i += 32) {
-                    const int r = left + i / (D / 8), c = i % (D / 8);
-                    sts128(v + (c >> 3) * C::kPanelBytes + r * 128 + ((c & 7) << 4), 0u, 0u, 0u, 0u);
+        // step j: O += P V of key tile j - 1, S = Q K^T of key tile j, where the tile of rows looks at them
+        for (int j = 0; j <= n_tiles; ++j) {
+            if (j > 0) {
+                const uint32_t slot = it % C::kStages;
+                const uint32_t v = (ring_lo + slot * (C::kTileBytes >> 4)) | kLoV;
+                if (!wait_for(sm.kv_full + slot * 8, (it / C::kStages) & 1)) break;
+                ++it;
+                const int left = last - (j - 1) * kTileKeys;                   // keys of tile j - 1 that count
+                const int steps = left >= kTileKeys ? kTileKeys / 16 : (left + 15) / 16;
+                if (left < kTileKeys && (left & 15)) {
+                    if (t == 0 && elect_one()) mbar_arrive(sm.tail_go);
+                    if (!wait_for(sm.tail_done, tails & 1)) break;
+                    ++tails;
                 }
-                fence_async_smem();
-                __syncwarp();
+                if (j > first && j <= end) {
+                    if (!wait_for(p_ready, np & 1)) break;
+                    ++np;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        if (steps == kTileKeys / 16) {
+#pragma unroll
+                            for (int s = 0; s < 8; ++s)        // (P: columns 0-31 and 64-95 of the tile's S)
+                                umma_ts(o, ts + (s >> 2) * 32 + s * 8, desc_of(v + s * 128, kHi), idesc_o, j - 1 > first || s > 0);
+                        } else {
+#pragma unroll
+                            for (int s = 0; s < 8; ++s)
+                                if (s < steps) umma_ts(o, ts + (s >> 2) * 32 + s * 8, desc_of(v + s * 128, kHi), idesc_o, j - 1 > first || s > 0);
+                        }
+                        if (j == end) umma_commit(o_full);
+                    }
+                }
+                if (elect_one() && !withhold) umma_commit(sm.kv_empty + slot * 8);
             }
-            const uint32_t ks = it % C::kStages;
-            const bool again = j + 1 < d.n_tiles;
-            for (int t = 0; t < tiles_q; ++t) {
-                if (!wait_for(sm.p_ready + t * 8, np[t] & 1)) break;
-                ++np[t];
-                if (t == 0 && again && !wait_for(sm.kv_full + ks * 8, (it / C::kStages) & 1)) break;
+            if (j < n_tiles) {
+                const uint32_t slot = it % C::kStages, k = (ring_lo + slot * (C::kTileBytes >> 4)) | kLoK;
+                if (!wait_for(sm.kv_full + slot * 8, (it / C::kStages) & 1)) break;
+                ++it;
                 tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t o = tmem + kTmemO + t * kTmemTile, pa = tmem + kTmemS + t * kTmemTile;
-                    for (int s = 0; s < steps; ++s)
-                        umma_ts(o, pa + s * 8, smem_desc(v + s * 2048, C::kPanelBytes, 1024), idesc_o, j > 0 || s > 0);
-                    if (again) scores(t, ks);
-                    else umma_commit(sm.o_full + t * 8);
+                if (elect_one()) {
+                    if (j >= first && j < end) {
+#pragma unroll
+                        for (int s = 0; s < D / 16; ++s) {
+                            const uint32_t off = ((s >> 2) * C::kPanelBytes + (s & 3) * 32) >> 4;
+                            umma_ss(ts, desc_of(q + off, kHi), desc_of(k + off, kHi), idesc_s, s > 0);
+                        }
+                        umma_commit(s_full);
+                    }
+                    if (!withhold) umma_commit(sm.kv_empty + slot * 8);
+                    if (j + 1 == n_tiles) umma_commit(sm.q_empty);
                 }
             }
-            if (!ok) break;
-            if (lane == 0) {
-                if (!withhold) umma_commit(sm.kv_empty + vs * 8);
-                if (again) {
-                    if (!withhold) umma_commit(sm.kv_empty + ks * 8);
-                    if (j + 2 == d.n_tiles) umma_commit(sm.q_empty);
-                }
-            }
-            if (again) ++it;
         }
         if (!ok) break;
     }
     // nothing of the tensor pipe may be under way when the tensor memory is freed
-    if (lane == 0) {
-        umma_commit(sm.wind_down);
-        if (!mbar_drain(sm.wind_down, 0, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
+    if (elect_one()) {
+        umma_commit(sm.wind_down + t * 8);
+        if (!mbar_drain(sm.wind_down + t * 8, 0, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
     }
     __syncwarp();
 }
 
-// ---- warps 0-7: softmax and output ------------------------------------------------------------------------------
+// ---- warp 19: rows of V behind an item's last key may hold anything, and 0 * NaN must not reach the sum ----------------
+template <int D>
+__device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int lane) {
+    using C = Cfg<D>;
+    const unsigned all = 0xffffffffu;
+    uint32_t it = 0, ic = 0, tails = 0;
+    for (;; ++ic) {
+        const uint32_t ss = ic % kSched;
+        if (!__all_sync(all, mbar_wait_lazy(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) return;
+        const Item d = sm.items[ss];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sm.sched_empty + ss * 8);
+        if (!d.more) return;
+        it += 2 * d.n_tiles;
+        const int left = d.k1 - (d.kf + (d.n_tiles - 1) * kTileKeys);
+        if (d.n_tiles == 0 || left == kTileKeys || !(left & 15)) continue;      // (the product takes 16 keys at a time)
+        if (!__all_sync(all, mbar_wait_lazy(sm.tail_go, tails & 1, sm.wc))) return;
+        ++tails;
+        const uint32_t v = sm.ring + (it - 1) % C::kStages * C::kTileBytes;
+        const int n = (16 - (left & 15)) * (D / 8);
+        for (int i = lane; i < n; i += 32) {
+            const int r = left + i / (D / 8), c = i % (D / 8);
+            sts128(v + (c >> 3) * C::kPanelBytes + r * 128 + ((c & 7) << 4), 0u, 0u, 0u, 0u);
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sm.tail_done);
+    }
+}
+
+// 2^x on the FMA pipe, for x <= some ten: nearest integer by the addition of 1.5 * 2^23, whose low mantissa bits then hold it
+__device__ __forceinline__ float2 ex2_fma(float2 x) {
+    // (the maximum that hands a NaN on: a NaN among visible scores must not come out as a finite result)
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+    const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f), one = make_float2(-1.f, -1.f);
+    const float2 t = __fadd2_rn(x, magic);
+    const float2 f = __ffma2_rn(__fadd2_rn(t, minus), one, x);
+    float2 q = __ffma2_rn(f, make_float2(0.009570102207362652f, 0.009570102207362652f), make_float2(0.05591785907745361f, 0.05591785907745361f));
+    q = __ffma2_rn(q, f, make_float2(0.240247443318367f, 0.240247443318367f));
+    q = __ffma2_rn(q, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+    q = __ffma2_rn(q, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(t.x) << 23)),
+                       __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(t.y) << 23)));
+}
+
+// 32 raw products of a row -> scores in the base-2 domain (cap, bias by distance); dist0: distance of the first one's key.
+// Below |x| = 1 the cap's tanh is an odd polynomial on the FMA pipe (degree 13, fitted to tanh(x) / x in x^2, error 4.4e-8);
+// a warp that sees a larger argument takes the form with two special functions (see score()).
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void scores_of(const Params& p, float* s, float slope, float dist0) {
+    if (CAP) {
+        const float2 mul = make_float2(p.cap_x, p.cap_x), cap = make_float2(p.cap_log2e, p.cap_log2e);
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            most = fmaxf(fmaxf(most, fabsf(s[i])), fabsf(s[i + 1]));
+        }
+        if (__all_sync(0xffffffffu, most * fabsf(p.cap_x) <= 1.f)) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+                const float2 x = __fmul2_rn(make_float2(s[i], s[i + 1]), mul), u = __fmul2_rn(x, x);
+                float2 q = __ffma2_rn(u, make_float2(0.0010531365405768156f, 0.0010531365405768156f), make_float2(-0.006239818874746561f, -0.006239818874746561f));
+                q = __ffma2_rn(q, u, make_float2(0.020331112667918205f, 0.020331112667918205f));
+                q = __ffma2_rn(q, u, make_float2(-0.05347844585776329f, -0.05347844585776329f));
+                q = __ffma2_rn(q, u, make_float2(0.13325709104537964f, 0.13325709104537964f));
+                q = __ffma2_rn(q, u, make_float2(-0.33332881331443787f, -0.33332881331443787f));
+                q = __ffma2_rn(q, u, make_float2(0.9999999403953552f, 0.9999999403953552f));
+                q = __fmul2_rn(q, __fmul2_rn(x, cap));
+                s[i] = q.x;
+                s[i + 1] = q.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[i] = score<true, false>(p, s[i], 0.f, 0);
+        }
+    }
+    if (BIAS) {
+        // |distance| as a float, counted down from the first key's (an integer conversion per score would go to the
+        // special-function unit)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i] = fmaf(-slope, fabsf(dist0 - (float)i), CAP ? s[i] : s[i] * p.scale_log2e);
+    }
+}
+
+// ---- warps 0-15: softmax and output -----------------------------------------------------------------------------
+// A row of a tile belongs to two threads, in warps w and w + 4: one has its keys 0-63 of every tile and the lower half of its
+// output, the other keys 64-127 and the upper half.  They hand each other their maximum through shared memory.
 template <int D, bool FP16, bool CAP, bool BIAS>
 __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, uint32_t tmem, int warp, int lane) {
     const unsigned all = 0xffffffffu;
-    const int t = warp >> 2, row = (warp & 3) * 32 + lane, TT = p.big_tile_tok;
+    const int t = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane, TT = p.big_tile_tok;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + kTmemS + t * kTmemTile, to = tmem + lanes + kTmemO + t * kTmemTile;
+    const uint32_t ts = tmem + lanes + kTmemS + t * kTmemTile, to = tmem + lanes + kTmemO + t * kTmemTile + half * (D / 2);
+    const uint32_t s_full = sm.s_full + t * 8, p_ready = sm.p_ready + t * 8, pair = sm.pair + (t * 4 + (warp & 3)) * 8;
     const int tr = row / p.G, g = row - tr * p.G;
-    uint32_t ic = 0, ns = 0, no = 0;
+    uint32_t ic = 0, ns = 0, no = 0, nx = 0;
+    // the two warps of a pair meet; false if the wait ran out
+    auto meet = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pair);
+        const bool ok = __all_sync(all, mbar_wait(pair, nx & 1, sm.wc));
+        ++nx;
+        return ok;
+    };
+    // the partner's value for this row
+    auto exchange = [&](float mine, float& other) {
+        sm.exchange[warp * 32 + lane] = mine;
+        if (!meet()) return false;
+        other = sm.exchange[(warp ^ 4) * 32 + lane];
+        return meet();
+    };
+    // does either warp of the pair vote for it?  (Two words in turn: a warp is at most one vote ahead of its partner's look.)
+    uint32_t nv = 0;
+    auto either = [&](bool yes, bool& any) {
+        uint32_t* box = sm.votes + (nv++ & 1) * kSoftmaxWarps;
+        yes = __any_sync(all, yes);
+        if (lane == 0) box[warp] = yes;
+        if (!meet()) return false;
+        any = yes || *(volatile uint32_t*)(box + (warp ^ 4)) != 0;
+        return true;
+    };
     for (;; ++ic) {
         const uint32_t ss = ic % kSched;
         if (!__all_sync(all, mbar_wait(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) return;
@@ -380,81 +544,108 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
             if (BIAS && p.slopes) slope = p.slopes[hq] * 1.4426950408889634f;
         }
         float m = -INFINITY, l = 0.f;
-        for (int j = 0; j < d.n_tiles; ++j) {
-            const int key = d.kf + j * kTileKeys;
-            if (!__all_sync(all, mbar_wait(sm.s_full + t * 8, ns & 1, sm.wc))) return;
+        const int first = range_first(d.range[t]), end = range_end(d.range[t]);
+        for (int j = first; j < end; ++j) {
+            const int key = d.kf + j * kTileKeys + half * 64;        // the first of this thread's 64 keys
+            if (!__all_sync(all, mbar_wait(s_full, ns & 1, sm.wc))) return;
             ++ns;
             tc_fence_after();
-            uint32_t r[128];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, r + c * 32);
-            tmem_ld_wait();
-            float* s = reinterpret_cast<float*>(r);
+            // The row is read twice from tensor memory, 32 columns at a time, rather than held in registers; what the first
+            // pass changes it writes back.
+            uint32_t buf[32];
+            float* s = reinterpret_cast<float*>(buf);
             const float mul = CAP || BIAS ? 1.f : p.scale_log2e;
-            if (CAP || BIAS) {
+            const bool mask = __any_sync(all, lo > key || hi < key + 64), changed = CAP || BIAS || mask;
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < 128; ++i) s[i] = score<CAP, BIAS>(p, s[i], slope, pos - (key + i));
+            for (int c = 0; c < 2; ++c) {
+                tmem_ld32(ts + half * 64 + c * 32, buf);
+                tmem_ld_wait();
+                if (CAP || BIAS) scores_of<CAP, BIAS>(p, s, slope, (float)(pos - key - c * 32));
+                if (mask) {
+                    const int a = lo - key - c * 32, b = hi - key - c * 32;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) s[i] = i >= a && i < b ? s[i] : -INFINITY;
+                }
+                if (changed) tmem_st32(ts + half * 64 + c * 32, buf);
+#pragma unroll
+                for (int i = 0; i < 32; i += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx[e] = fmaxf(fmaxf(mx[e], s[i + e]), s[i + 4 + e]);
             }
-            if (__any_sync(all, lo > key || hi < key + kTileKeys)) {
-                const int a = lo - key, b = hi - key;
-#pragma unroll
-                for (int i = 0; i < 128; ++i) s[i] = i >= a && i < b ? s[i] : -INFINITY;
-            }
-            float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-            for (int i = 4; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], s[i]);
-            const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
-            if (j == 0) {
-                m = tile_max;
-            } else if (__any_sync(all, tile_max > m + kLazy)) {
-                // (the products of the tiles before are complete: this tile's scores were issued behind them)
-                const float mn = fmaxf(m, tile_max);
-                const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
-                l *= f;
-                m = mn;
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    uint32_t o[16];
-                    tmem_ld16(to + c * 16, o);
+            if (changed) tmem_st_wait();
+            tmem_ld32(ts + half * 64, buf);
+            float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul, other;
+            bool grown = true;
+            if (j > first && !either(tile_max > m + kLazy, grown)) return;
+            if (grown) {
+                if (!exchange(tile_max, other)) return;
+                tile_max = fmaxf(tile_max, other);
+                if (j == first) {
+                    m = tile_max;
+                } else {
+                    // (the products of the tiles before are complete: this tile's scores were issued behind them)
+                    const float mn = fmaxf(m, tile_max);
+                    const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
+                    l *= f;
+                    m = mn;
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                    tmem_st16(to + c * 16, o);
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t o[16];
+                        tmem_ld16(to + c * 16, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st16(to + c * 16, o);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    if (!meet()) return;       // both halves of O are rescaled before either half of P is handed over
                 }
             }
             const float me = m == -INFINITY ? 0.f : m;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            const float2 mul2 = make_float2(mul, mul), me2 = make_float2(-me, -me);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
+                if (c > 0) tmem_ld32(ts + half * 64 + c * 32, buf);
+                tmem_ld_wait();
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float a = ex2(fmaf(s[c * 32 + 2 * i], mul, -me)), b = ex2(fmaf(s[c * 32 + 2 * i + 1], mul, -me));
-                    sum[(2 * i) & 3] += a;
-                    sum[(2 * i + 1) & 3] += b;
-                    w[i] = pack16<FP16>(a, b);
+                    const float2 x = __ffma2_rn(make_float2(s[2 * i], s[2 * i + 1]), mul2, me2);
+                    // (spread evenly: of every 16 pairs, kEmulated go to the FMA pipe)
+                    const bool emulate = (i * kEmulated) % 16 < kEmulated;
+                    const float2 e = emulate ? ex2_fma(x) : make_float2(ex2(x.x), ex2(x.y));
+                    sum[i & 3] = __fadd2_rn(sum[i & 3], e);
+                    w[i] = pack16<FP16>(e.x, e.y);
                 }
-                tmem_st16(ts + c * 16, w);
+                tmem_st16(ts + half * 64 + c * 16, w);     // (over scores that this thread has read)
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(sm.p_ready + t * 8);
+            if (lane == 0) mbar_arrive(p_ready);
+            const float2 all2 = __fadd2_rn(__fadd2_rn(sum[0], sum[1]), __fadd2_rn(sum[2], sum[3]));
+            l += all2.x + all2.y;
         }
         // output
-        if (d.n_tiles > 0) {
+        float other = 0.f;
+        if (end > first) {
+            if (!exchange(l, other)) return;
             if (!__all_sync(all, mbar_wait(sm.o_full + t * 8, no & 1, sm.wc))) return;
             ++no;
             tc_fence_after();
         }
-        const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);    // nothing visible: a zero row
+        l += other;
+        const float inv = m == -INFINITY ? 0.f : 1.f / l;              // nothing visible: a zero row
         const size_t at = (size_t)((d.part < 0 ? d.tok0 : d.part) + rel) * p.n_q_heads + hq;
-        if (mine && d.part >= 0) p.part_ml[at] = make_float2(m, l);
+        if (mine && d.part >= 0 && half == 0) p.part_ml[at] = make_float2(m, l);
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
+        for (int c = 0; c < D / 64; ++c) {
             uint32_t o[32];
-            if (d.n_tiles > 0) {
+            if (end > first) {
                 tmem_ld32(to + c * 32, o);
                 tmem_ld_wait();
             } else {
@@ -462,8 +653,9 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
                 for (int i = 0; i < 32; ++i) o[i] = 0u;
             }
             if (!mine) continue;
+            const size_t col = at * D + half * (D / 2) + c * 32;
             if (d.part < 0) {
-                uint4* dst = reinterpret_cast<uint4*>(p.out + at * D + c * 32);
+                uint4* dst = reinterpret_cast<uint4*>(p.out + col);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     uint32_t w[4];
@@ -473,7 +665,7 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
                     dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             } else {
-                uint4* dst = reinterpret_cast<uint4*>(p.part_o + at * D + c * 32);
+                uint4* dst = reinterpret_cast<uint4*>(p.part_o + col);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             }
@@ -487,26 +679,29 @@ __global__ void __launch_bounds__(kThreads, 1)
 big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
            const Params p) {
     using C = Cfg<D>;
-    extern __shared__ uint8_t raw[];
+    extern __shared__ __align__(1024) uint8_t raw[];       // (the swizzled tiles need it; there is no static shared memory before it)
     const Smem sm = carve<D>(raw, p);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(sm.kv_full + s * 8, 1);
-            mbar_init(sm.kv_empty + s * 8, 1);
+            mbar_init(sm.kv_empty + s * 8, 2);
         }
         mbar_init(sm.q_full, 1);
-        mbar_init(sm.q_empty, 1);
+        mbar_init(sm.q_empty, 2);
         for (int t = 0; t < 2; ++t) {
             mbar_init(sm.s_full + t * 8, 1);
-            mbar_init(sm.p_ready + t * 8, 4);
+            mbar_init(sm.p_ready + t * 8, 8);
+            mbar_init(sm.wind_down + t * 8, 1);
             mbar_init(sm.o_full + t * 8, 1);
         }
         for (int s = 0; s < kSched; ++s) {
             mbar_init(sm.sched_full + s * 8, 1);
-            mbar_init(sm.sched_empty + s * 8, kSoftmaxWarps + 1);
+            mbar_init(sm.sched_empty + s * 8, kSoftmaxWarps + 3);
         }
-        mbar_init(sm.wind_down, 1);
+        mbar_init(sm.tail_go, 1);
+        mbar_init(sm.tail_done, 1);
+        for (int w = 0; w < 8; ++w) mbar_init(sm.pair + w * 8, 2);
         sm.wc.abort_flag[0] = 0;
         mbar_init_fence();
     }
@@ -527,7 +722,8 @@ big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         softmax_warp<D, FP16, CAP, BIAS>(p, sm, tmem, warp, lane);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp == kMmaWarp) mma_warp<D, FP16>(p, sm, tmem, lane);
+        if (warp < kLoadWarp) mma_warp<D, FP16>(p, sm, tmem, warp - kMmaWarp);
+        else if (warp == kTailWarp) tail_warp<D>(p, sm, lane);
         else if (warp == kLoadWarp) load_warp<D>(p, sm, &tm_q, &tm_k, &tm_v, n_items, lane);
     }
     tc_fence_before();
