@@ -134,15 +134,6 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
     if (mbar_try_wait(bar, parity)) return true;
     return mbar_wait_slow(bar, parity, w);
 }
-// The same for warps that nobody waits for: they look less often and leave the issue slots to the others.
-__device__ __forceinline__ bool mbar_wait_lazy(uint32_t bar, uint32_t parity, const WaitCtl& w) {
-    for (int i = 0; i < 1 << 20; ++i) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (*w.abort_flag) return false;
-        __nanosleep(100);
-    }
-    return mbar_wait_slow(bar, parity, w);
-}
 // A last look at a barrier before a CTA leaves, whatever the abort flag says: copies in flight must land first.
 __device__ __forceinline__ bool mbar_drain(uint32_t bar, uint32_t parity, long long limit) {
     const long long t0 = clock64();

@@ -5,10 +5,10 @@
 //     O[128 rows, D]       += P V          P from tensor memory, where it replaces the S it was made of
 // A unit has two tiles of 128 rows (query tokens times the G heads of a KV head); they share every tile of
 // K and V, and while one tile's scores are in the softmax the tensor cores work for the other.
-// Roles: warps 0-7 and 8-15 are the softmax of the two tiles, half a row per thread; warps 16 and 17 issue their MMAs;
-// warp 18 fetches items from a counter and keeps K and V coming through a ring (tensor-map boxes, one per page piece);
-// warp 19 clears the rows of V behind an item's last key.  Tensor memory (all 512 columns): S of the two tiles, O of the
-// two tiles.
+// Roles: warps 0-3 and 4-7 are the softmax of the two tiles, a row per thread (no shuffles); warp 8 issues the MMAs;
+// warps 9 and 12 keep K and V coming through a ring (tensor-map boxes, one per page piece); warp 10 clears the rows of V
+// behind an item's last key; warp 11 fetches items from a counter, an item ahead, and their queries.  Tensor memory (all
+// 512 columns): S of the two tiles, O of the two tiles.
 //
 // The running maximum is followed lazily: O and l are rescaled only when a row's maximum has grown by more than
 // 2^8 over the one in use (P then stays below 2^8, far inside both 16-bit types, and fp32 sums do not care), so the
@@ -17,9 +17,8 @@
 //
 // A tile's step is: scores (512 cycles of the tensor pipe at D = 128), softmax, O += P V (512).  The special-function unit
 // alone would take 1024 cycles for a tile's 16384 exponentials, so part of them is computed on the FMA pipe
-// (2^x = 2^n p(f), n the nearest integer, p a polynomial of degree 4 fitted on [-1/2, 1/2], relative error 2.6e-6); and
-// two threads share a row, because with one a scheduler has two warps to choose from and a tile's softmax takes twice as
-// long as its instructions.
+// (2^x = 2^n p(f), n the nearest integer, p a polynomial of degree 4 fitted on [-1/2, 1/2], relative error 2.6e-6), and
+// the second product starts on the first half of the keys while the weights of the second half are still being made.
 #include <limits.h>
 
 #include "paged.cuh"
@@ -29,14 +28,12 @@ namespace paged {
 namespace {
 
 constexpr int kTileKeys = 128;
-constexpr int kSoftmaxWarps = 16, kMmaWarp = 16, kLoadWarp = 18, kTailWarp = 19;
-constexpr int kThreads = 20 * 32;
-constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;       // of 96 a thread at launch: 4 * 104 + 64 = 5 * 96
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kKeyWarp = 9, kTailWarp = 10, kItemWarp = 11, kValueWarp = 13;
+constexpr int kThreads = 16 * 32;       // four warpgroups (the last three warps only give their registers away)
+constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;       // of 128 a thread at launch: 2 * 184 + 2 * 72 = 4 * 128
 constexpr int kSched = 2;
 constexpr int kEmulated = 6;        // of 16 pairs of weights, how many are computed on the FMA pipe
 constexpr float kLazy = 8.f;        // base-2 logarithm of the growth a row's maximum may have before O is rescaled
-
-constexpr int kExchangeBytes = kSoftmaxWarps * 32 * 4 + 2 * kSoftmaxWarps * 4;    // a float per row and half; a word per warp, twice
 
 template <int D>
 struct Cfg {
@@ -44,8 +41,8 @@ struct Cfg {
     static constexpr int kPanelBytes = 128 * 128;            // 128 rows of 64 values, 128-byte swizzled
     static constexpr int kTileBytes = kPanels * kPanelBytes;
     static constexpr int kStages = D == 128 ? 5 : 8;
-    static constexpr int kBars = 2 * kStages + 2 + 6 + 2 * kSched + 4 + 8;
-    static constexpr int kSmemBytes = 2 * kTileBytes + kStages * kTileBytes + kBars * 8 + kSched * 48 + 32 + kExchangeBytes;
+    static constexpr int kBars = 2 * kStages + 2 + 8 + 2 * kSched + 3;
+    static constexpr int kSmemBytes = 1024 + 2 * kTileBytes + kStages * kTileBytes + kBars * 8 + kSched * 48 + 32;
 };
 constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemTile = 128;    // column of tile t: base + t * 128
 
@@ -122,6 +119,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t* r) {
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void st_global32(void* p, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
 // Box of the 3-D query tensor [token][head][dim]: 64 dims of the G heads of a KV head, of the tokens of a tile.
 __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* tm, int dim, int head, int tok, uint32_t bar) {
     asm volatile(
@@ -131,18 +133,26 @@ __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* tm, in
         : "memory");
 }
 
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+
+
 struct Smem {
     uint32_t q, ring;
-    uint32_t kv_full, kv_empty, q_full, q_empty, s_full, p_ready, o_full, sched_full, sched_empty, wind_down, tail_go, tail_done, pair;
-    float* exchange;
-    uint32_t* votes;
+    uint32_t kv_full, kv_empty, q_full, q_empty, s_full, p_ready, o_full, sched_full, sched_empty, wind_down, tail_go, tail_done;
     Item* items;
     uint32_t* tmem_slot;
     WaitCtl wc;
 };
 template <int D>
-__device__ __forceinline__ Smem carve(uint8_t* base, const Params& p) {
+__device__ __forceinline__ Smem carve(uint8_t* raw, const Params& p) {
     using C = Cfg<D>;
+    uint8_t* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     uint8_t* items = base + (2 + C::kStages) * C::kTileBytes;
     uint8_t* bars = items + kSched * sizeof(Item);
     uint8_t* words = bars + C::kBars * 8;
@@ -156,30 +166,26 @@ __device__ __forceinline__ Smem carve(uint8_t* base, const Params& p) {
     s.q_empty = s.q_full + 8;
     s.s_full = s.q_empty + 8;
     s.p_ready = s.s_full + 16;
-    s.o_full = s.p_ready + 16;
+    s.o_full = s.p_ready + 32;
     s.sched_full = s.o_full + 16;
     s.sched_empty = s.sched_full + kSched * 8;
     s.wind_down = s.sched_empty + kSched * 8;
-    s.tail_go = s.wind_down + 16;
+    s.tail_go = s.wind_down + 8;
     s.tail_done = s.tail_go + 8;
-    s.pair = s.tail_done + 8;
-    s.exchange = reinterpret_cast<float*>(words + 16);
-    s.votes = reinterpret_cast<uint32_t*>(words + 16 + kSoftmaxWarps * 32 * 4);
     s.wc.abort_flag = reinterpret_cast<volatile int*>(words);
     s.wc.header = p.header;
     s.tmem_slot = reinterpret_cast<uint32_t*>(words + 8);
     return s;
 }
 
-// ---- warp 18: items, queries, keys and values -----------------------------------------------------------------
+// ---- warp 11: items and their queries --------------------------------------------------------------------------
+// It runs an item ahead of the others: the chain from the counter to a token's interval is some thousand cycles long.
 template <int D>
-__device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const CUtensorMap* tm_q, const CUtensorMap* tm_k,
-                                          const CUtensorMap* tm_v, int n_items, int lane) {
+__device__ __forceinline__ void item_warp(const Params& p, const Smem& sm, const CUtensorMap* tm_q, int n_items, int lane) {
     using C = Cfg<D>;
     const unsigned all = 0xffffffffu;
     const int bp = min(p.page_size, 64), TT = p.big_tile_tok;
-    uint32_t it = 0, ic = 0, qn = 0;     // stages, items, query loads so far
-    bool stopped = false;
+    uint32_t ic = 0, qn = 0;
     int next = 0;
     if (lane == 0) next = atomicAdd(p.header + kBigNextWord, 1);
     for (;; ++ic) {
@@ -194,16 +200,23 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
             d.tok0 = u.tok0; d.ntok = u.ntok; d.req = u.req; d.part = u.part;
             // the keys that one of the tokens sees, for each tile of rows
             int lo[2] = {INT_MAX, INT_MAX}, hi[2] = {0, 0};
-            for (int t = lane; t < u.ntok; t += 32) {
-                const TokInfo ti = p.tok_info[u.tok0 + t];
-                const int a = max(ti.lo, u.k0), b = min(ti.hi, u.k1);
-                if (a < b) {
-                    if (t < TT) {
-                        lo[0] = min(lo[0], a);
-                        hi[0] = max(hi[0], b);
-                    } else {
-                        lo[1] = min(lo[1], a);
-                        hi[1] = max(hi[1], b);
+            TokInfo ti[8];                       // (a unit has at most 256 tokens: all loads at once)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (lane + 32 * i < u.ntok) ti[i] = p.tok_info[u.tok0 + lane + 32 * i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = lane + 32 * i;
+                if (t < u.ntok) {
+                    const int a = max(ti[i].lo, u.k0), b = min(ti[i].hi, u.k1), w = t < TT ? 0 : 1;
+                    if (a < b) {
+                        if (w == 0) {
+                            lo[0] = min(lo[0], a);
+                            hi[0] = max(hi[0], b);
+                        } else {
+                            lo[1] = min(lo[1], a);
+                            hi[1] = max(hi[1], b);
+                        }
                     }
                 }
             }
@@ -225,103 +238,107 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
         const uint32_t ss = ic % kSched;
         int ok = 1;
         if (lane == 0) {
-            ok = mbar_wait_lazy(sm.sched_empty + ss * 8, ((ic / kSched) & 1) ^ 1, sm.wc);
+            ok = mbar_wait(sm.sched_empty + ss * 8, ((ic / kSched) & 1) ^ 1, sm.wc);
             if (ok) {
                 sm.items[ss] = d;
                 mbar_arrive(sm.sched_full + ss * 8);
+                if (d.n_tiles > 0) {
+                    ok = mbar_wait(sm.q_empty, (qn & 1) ^ 1, sm.wc);
+                    if (ok) {
+                        const int tiles_q = d.ntok > TT ? 2 : 1;
+                        mbar_arrive_expect_tx(sm.q_full, (uint32_t)tiles_q * TT * p.G * D * 2);
+                        for (int t = 0; t < tiles_q; ++t)
+                            for (int c = 0; c < C::kPanels; ++c)
+                                tma_box3(sm.q + t * C::kTileBytes + c * C::kPanelBytes, tm_q, c * 64, d.head * p.G, d.tok0 + t * TT, sm.q_full);
+                        ++qn;
+                    }
+                }
             }
         }
-        if (!__shfl_sync(all, ok, 0)) {
-            stopped = true;
-            break;
-        }
+        if (!__shfl_sync(all, ok, 0) || !more) break;
+    }
+    // a copy in flight must land before the CTA leaves
+    if (lane == 0 && qn > 0 && !mbar_drain(sm.q_full, (qn - 1) & 1, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
+    __syncwarp();
+}
+
+// ---- warps 9 and 12: keys, values ------------------------------------------------------------------------------------
+// A warp each: with pages of 16 tokens a tile is 16 boxes.  As with the MMAs, the warp stays together and an elected lane
+// issues (a copy that every lane issues for itself cost 100 to 200 cycles).
+template <int D>
+__device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const CUtensorMap* tm, uint32_t kv, int lane) {
+    using C = Cfg<D>;
+    const unsigned all = 0xffffffffu;
+    const int bp = min(p.page_size, 64);
+    uint32_t it = kv, ic = 0;                // stages kv, kv + 2, ...
+    bool stopped = false;
+    for (; !stopped; ++ic) {
+        const uint32_t ss = ic % kSched;
+        if (!__all_sync(all, mbar_wait(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) break;
+        const Item& src = sm.items[ss];
+        const int more = (int)uniform(src.more), n_tiles = (int)uniform(src.n_tiles), kf = (int)uniform(src.kf), k1 = (int)uniform(src.k1);
+        const int head = (int)uniform(src.head), req = (int)uniform(src.req);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sm.sched_empty + ss * 8);
         if (!more) break;
-        if (d.n_tiles == 0) continue;
-        const int tiles_q = d.ntok > TT ? 2 : 1;
-        if (lane == 0) {
-            ok = mbar_wait_lazy(sm.q_empty, (qn & 1) ^ 1, sm.wc);
-            if (ok) {
-                mbar_arrive_expect_tx(sm.q_full, (uint32_t)tiles_q * TT * p.G * D * 2);
-                for (int t = 0; t < tiles_q; ++t)
-                    for (int c = 0; c < C::kPanels; ++c)
-                        tma_box3(sm.q + t * C::kTileBytes + c * C::kPanelBytes, tm_q, c * 64, d.head * p.G, d.tok0 + t * TT, sm.q_full);
+        const int32_t* table = p.block_table + (size_t)req * p.max_blocks;
+        auto page_of = [&](int j) {              // the page of this lane's piece of key tile j
+            const int key = kf + j * kTileKeys + lane * bp;
+            return lane < kTileKeys / bp && key < k1 ? table[key >> p.page_shift] : 0;
+        };
+        int page_next = page_of(0);
+        for (int j = 0; j < n_tiles; ++j, it += 2) {
+            const int key = kf + j * kTileKeys, nb = (min(kTileKeys, k1 - key) + bp - 1) / bp;
+            int page = page_next;
+            if (j + 1 < n_tiles) page_next = page_of(j + 1);
+            if (lane < nb && (unsigned)page >= (unsigned)p.n_pages) {   // such a page reads as zeros
+                atomicCAS(p.header, 0, PLORA_ERR_INVALID_ARG);
+                page = p.n_pages;
             }
-        }
-        if (!__shfl_sync(all, ok, 0)) {
-            stopped = true;
-            break;
-        }
-        ++qn;
-        const int32_t* table = p.block_table + (size_t)d.req * p.max_blocks;
-        for (int j = 0; j < d.n_tiles && !stopped; ++j) {
-            const int key = d.kf + j * kTileKeys, nb = (min(kTileKeys, d.k1 - key) + bp - 1) / bp;
-            const int my_key = key + lane * bp, so = my_key & (p.page_size - 1);
-            int page = 0;
-            if (lane < nb) {
-                page = table[my_key >> p.page_shift];
-                if ((unsigned)page >= (unsigned)p.n_pages) {   // such a page reads as zeros
-                    atomicCAS(p.header, 0, PLORA_ERR_INVALID_ARG);
-                    page = p.n_pages;
-                }
+            const uint32_t slot = it % C::kStages, dst = sm.ring + slot * C::kTileBytes, bar = sm.kv_full + slot * 8;
+            if (!__all_sync(all, mbar_wait(sm.kv_empty + slot * 8, ((it / C::kStages) & 1) ^ 1, sm.wc))) {
+                stopped = true;
+                break;
             }
-            for (int kv = 0; kv < 2; ++kv, ++it) {
-                const uint32_t slot = it % C::kStages, dst = sm.ring + slot * C::kTileBytes, bar = sm.kv_full + slot * 8;
-                if (lane == 0) {
-                    ok = mbar_wait_lazy(sm.kv_empty + slot * 8, ((it / C::kStages) & 1) ^ 1, sm.wc);
-                    if (ok) mbar_arrive_expect_tx(bar, (uint32_t)nb * bp * D * 2);
-                }
-                if (!__shfl_sync(all, ok, 0)) {
-                    stopped = true;
-                    break;
-                }
-                if (lane < nb) {
+            if (elect_one()) mbar_arrive_expect_tx(bar, (uint32_t)nb * bp * D * 2);
+            for (int i = 0; i < nb; ++i) {
+                const int pg = __shfl_sync(all, page, i), so = (key + i * bp) & (p.page_size - 1);
+                if (elect_one()) {
 #pragma unroll
                     for (int c = 0; c < C::kPanels; ++c)
-                        tma_box4(dst + c * C::kPanelBytes + lane * bp * 128, kv ? tm_v : tm_k, c * 64, so, d.head, page, bar);
+                        tma_box4(dst + c * C::kPanelBytes + i * bp * 128, tm, c * 64, so, head, pg, bar);
                 }
             }
         }
-        if (stopped) break;
     }
-    // copies in flight must land before the CTA leaves
+    // copies in flight must land before the CTA leaves.  (An older stage than these has been used again, and so has landed; of
+    // these a barrier is at most one phase further on, and then it answers yes.)
     if (lane == 0) {
         const long long limit = wait_limit(p.header);
-        for (uint32_t k = 1; k <= (uint32_t)C::kStages && k <= it; ++k) {
+        for (uint32_t k = 2; k <= (uint32_t)C::kStages && k <= it; k += 2) {
             const uint32_t j = it - k;
             if (!mbar_drain(sm.kv_full + (j % C::kStages) * 8, (j / C::kStages) & 1, limit)) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
         }
-        if (qn > 0 && !mbar_drain(sm.q_full, (qn - 1) & 1, limit)) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
     }
     __syncwarp();
 }
 
-// ---- warps 16 and 17: the products of the two tiles -----------------------------------------------------------------
-// A warp per tile, so that what one does between its products (barriers, hand-backs) falls into the other's.  The warp
-// stays together and one elected lane issues: the MMA's operands are uniform registers, and under a plain `lane == 0` the
-// compiler cannot know that a single lane is active (an MMA then cost the issuer about 100 cycles, more than the 64 it
-// takes).  The upper half of a matrix descriptor is the same for all operands of a kind, and the lower half is an address
-// that advances by constants.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
-__device__ __forceinline__ uint64_t desc_of(uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); }
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
-
+// ---- warp 8: the products ---------------------------------------------------------------------------------------
+// The warp stays together and one elected lane issues: the MMA's operands are uniform registers, and under a plain
+// `lane == 0` the compiler cannot know that a single lane is active (an MMA then cost the issuer about 100 cycles, more
+// than the 64 it takes).  The upper half of a matrix descriptor is the same for all operands of a kind, and the lower half
+// is an address that advances by constants.
 template <int D, bool FP16>
-__device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32_t tmem, int t) {
+__device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32_t tmem) {
     using C = Cfg<D>;
     const unsigned all = 0xffffffffu;
     constexpr uint32_t idesc_s = instr_desc(kTileKeys, false, FP16), idesc_o = instr_desc(D, true, FP16);
     constexpr uint32_t kHi = (uint32_t)(smem_desc(0, 0, 1024) >> 32);
     constexpr uint32_t kLoK = 1u << 16, kLoV = (uint32_t)(C::kPanelBytes >> 4) << 16;     // leading offsets: unused; the next panel
     const bool withhold = p.header[kHookWord] == PLORA_HOOK_WITHHOLD_RELEASE;   // test hook: stages are never handed back
-    uint32_t it = 0, ic = 0, qn = 0, tails = 0, np = 0;
-    t = (int)uniform((uint32_t)t);
-    const uint32_t q = uniform((sm.q >> 4) | kLoK) + t * (C::kTileBytes >> 4), ring_lo = uniform(sm.ring >> 4);
-    const uint32_t ts = uniform(tmem) + kTmemS + t * kTmemTile, o = uniform(tmem) + kTmemO + t * kTmemTile;
-    const uint32_t s_full = sm.s_full + t * 8, p_ready = sm.p_ready + t * 8, o_full = sm.o_full + t * 8;
+    uint32_t it = 0, ic = 0, qn = 0, tails = 0, np[2] = {0, 0};
+    const uint32_t q_lo = uniform((sm.q >> 4) | kLoK), ring_lo = uniform(sm.ring >> 4);
+    tmem = uniform(tmem);
     bool ok = true;
     auto wait_for = [&](uint32_t bar, uint32_t parity) {
         ok = __all_sync(all, mbar_wait(bar, parity, sm.wc));
@@ -332,76 +349,90 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
         if (!wait_for(sm.sched_full + ss * 8, (ic / kSched) & 1)) break;
         const Item& src = sm.items[ss];
         const int n_tiles = (int)uniform(src.n_tiles), more = (int)uniform(src.more), last = (int)uniform(src.k1 - src.kf);
-        const int range = (int)uniform(src.range[t]), first = range_first(range), end = range_end(range);
-        __syncwarp();
+        const int ranges[2] = {(int)uniform(src.range[0]), (int)uniform(src.range[1])};
         if (elect_one()) mbar_arrive(sm.sched_empty + ss * 8);
         if (!more) break;
         if (n_tiles == 0) continue;
         if (!wait_for(sm.q_full, qn & 1)) break;
         ++qn;
-        // step j: O += P V of key tile j - 1, S = Q K^T of key tile j, where the tile of rows looks at them
+        // step j: O += P V of key tile j - 1, then S = Q K^T of key tile j, for each tile of rows that looks at them.  What the
+        // step needs of K and V is waited for first, so that nothing stands between a tile's weights and its next scores:
+        // the two tiles then settle into turns, one in the softmax while the other has the tensor cores.
         for (int j = 0; j <= n_tiles; ++j) {
+            uint32_t v_slot = 0, k_slot = 0;
+            int steps = kTileKeys / 16;
             if (j > 0) {
-                const uint32_t slot = it % C::kStages;
-                const uint32_t v = (ring_lo + slot * (C::kTileBytes >> 4)) | kLoV;
-                if (!wait_for(sm.kv_full + slot * 8, (it / C::kStages) & 1)) break;
+                v_slot = it % C::kStages;
+                if (!wait_for(sm.kv_full + v_slot * 8, (it / C::kStages) & 1)) break;
                 ++it;
                 const int left = last - (j - 1) * kTileKeys;                   // keys of tile j - 1 that count
-                const int steps = left >= kTileKeys ? kTileKeys / 16 : (left + 15) / 16;
-                if (left < kTileKeys && (left & 15)) {
-                    if (t == 0 && elect_one()) mbar_arrive(sm.tail_go);
-                    if (!wait_for(sm.tail_done, tails & 1)) break;
-                    ++tails;
-                }
-                if (j > first && j <= end) {
-                    if (!wait_for(p_ready, np & 1)) break;
-                    ++np;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        if (steps == kTileKeys / 16) {
-#pragma unroll
-                            for (int s = 0; s < 8; ++s)        // (P: columns 0-31 and 64-95 of the tile's S)
-                                umma_ts(o, ts + (s >> 2) * 32 + s * 8, desc_of(v + s * 128, kHi), idesc_o, j - 1 > first || s > 0);
-                        } else {
-#pragma unroll
-                            for (int s = 0; s < 8; ++s)
-                                if (s < steps) umma_ts(o, ts + (s >> 2) * 32 + s * 8, desc_of(v + s * 128, kHi), idesc_o, j - 1 > first || s > 0);
-                        }
-                        if (j == end) umma_commit(o_full);
+                if (left < kTileKeys) {
+                    steps = (left + 15) / 16;
+                    if (left & 15) {
+                        if (elect_one()) mbar_arrive(sm.tail_go);
+                        if (!wait_for(sm.tail_done, tails & 1)) break;
+                        ++tails;
                     }
                 }
-                if (elect_one() && !withhold) umma_commit(sm.kv_empty + slot * 8);
             }
             if (j < n_tiles) {
-                const uint32_t slot = it % C::kStages, k = (ring_lo + slot * (C::kTileBytes >> 4)) | kLoK;
-                if (!wait_for(sm.kv_full + slot * 8, (it / C::kStages) & 1)) break;
+                k_slot = it % C::kStages;
+                if (!wait_for(sm.kv_full + k_slot * 8, (it / C::kStages) & 1)) break;
                 ++it;
+            }
+            const uint32_t v = (ring_lo + v_slot * (C::kTileBytes >> 4)) | kLoV, k = (ring_lo + k_slot * (C::kTileBytes >> 4)) | kLoK;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int first = range_first(ranges[t]), end = range_end(ranges[t]);
+                const uint32_t o = tmem + kTmemO + t * kTmemTile, ts = tmem + kTmemS + t * kTmemTile, q = q_lo + t * (C::kTileBytes >> 4);
+                const bool pv = j > first && j <= end, qk = j >= first && j < end;
+                if (pv) {
+                    if (!wait_for(sm.p_ready + t * 16, np[t] & 1)) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int s = 0; s < 4; ++s)
+                            if (s < steps) umma_ts(o, ts + s * 8, desc_of(v + s * 128, kHi), idesc_o, j - 1 > first || s > 0);
+                    }
+                    if (!wait_for(sm.p_ready + t * 16 + 8, np[t] & 1)) break;
+                    ++np[t];
+                }
                 tc_fence_after();
                 if (elect_one()) {
-                    if (j >= first && j < end) {
+                    if (pv) {
+#pragma unroll
+                        for (int s = 4; s < 8; ++s)
+                            if (s < steps) umma_ts(o, ts + s * 8, desc_of(v + s * 128, kHi), idesc_o, true);
+                    }
+                    if (qk) {
 #pragma unroll
                         for (int s = 0; s < D / 16; ++s) {
                             const uint32_t off = ((s >> 2) * C::kPanelBytes + (s & 3) * 32) >> 4;
                             umma_ss(ts, desc_of(q + off, kHi), desc_of(k + off, kHi), idesc_s, s > 0);
                         }
-                        umma_commit(s_full);
+                        umma_commit(sm.s_full + t * 8);
                     }
-                    if (!withhold) umma_commit(sm.kv_empty + slot * 8);
-                    if (j + 1 == n_tiles) umma_commit(sm.q_empty);
+                    if (pv && j == end) umma_commit(sm.o_full + t * 8);
                 }
+            }
+            if (!ok) break;
+            if (elect_one()) {
+                if (j > 0 && !withhold) umma_commit(sm.kv_empty + v_slot * 8);
+                if (j < n_tiles && !withhold) umma_commit(sm.kv_empty + k_slot * 8);
+                if (j + 1 == n_tiles) umma_commit(sm.q_empty);
             }
         }
         if (!ok) break;
     }
     // nothing of the tensor pipe may be under way when the tensor memory is freed
     if (elect_one()) {
-        umma_commit(sm.wind_down + t * 8);
-        if (!mbar_drain(sm.wind_down + t * 8, 0, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
+        umma_commit(sm.wind_down);
+        if (!mbar_drain(sm.wind_down, 0, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
     }
     __syncwarp();
 }
 
-// ---- warp 19: rows of V behind an item's last key may hold anything, and 0 * NaN must not reach the sum ----------------
+// ---- warp 10: rows of V behind an item's last key may hold anything, and 0 * NaN must not reach the sum ----------------
 template <int D>
 __device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int lane) {
     using C = Cfg<D>;
@@ -409,7 +440,7 @@ __device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int l
     uint32_t it = 0, ic = 0, tails = 0;
     for (;; ++ic) {
         const uint32_t ss = ic % kSched;
-        if (!__all_sync(all, mbar_wait_lazy(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) return;
+        if (!__all_sync(all, mbar_wait(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) return;
         const Item d = sm.items[ss];
         __syncwarp();
         if (lane == 0) mbar_arrive(sm.sched_empty + ss * 8);
@@ -417,7 +448,7 @@ __device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int l
         it += 2 * d.n_tiles;
         const int left = d.k1 - (d.kf + (d.n_tiles - 1) * kTileKeys);
         if (d.n_tiles == 0 || left == kTileKeys || !(left & 15)) continue;      // (the product takes 16 keys at a time)
-        if (!__all_sync(all, mbar_wait_lazy(sm.tail_go, tails & 1, sm.wc))) return;
+        if (!__all_sync(all, mbar_wait(sm.tail_go, tails & 1, sm.wc))) return;
         ++tails;
         const uint32_t v = sm.ring + (it - 1) % C::kStages * C::kTileBytes;
         const int n = (16 - (left & 15)) * (D / 8);
@@ -486,43 +517,15 @@ __device__ __forceinline__ void scores_of(const Params& p, float* s, float slope
     }
 }
 
-// ---- warps 0-15: softmax and output -----------------------------------------------------------------------------
-// A row of a tile belongs to two threads, in warps w and w + 4: one has its keys 0-63 of every tile and the lower half of its
-// output, the other keys 64-127 and the upper half.  They hand each other their maximum through shared memory.
+// ---- warps 0-7: softmax and output ------------------------------------------------------------------------------
 template <int D, bool FP16, bool CAP, bool BIAS>
 __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, uint32_t tmem, int warp, int lane) {
     const unsigned all = 0xffffffffu;
-    const int t = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane, TT = p.big_tile_tok;
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane, TT = p.big_tile_tok;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + kTmemS + t * kTmemTile, to = tmem + lanes + kTmemO + t * kTmemTile + half * (D / 2);
-    const uint32_t s_full = sm.s_full + t * 8, p_ready = sm.p_ready + t * 8, pair = sm.pair + (t * 4 + (warp & 3)) * 8;
+    const uint32_t ts = tmem + lanes + kTmemS + t * kTmemTile, to = tmem + lanes + kTmemO + t * kTmemTile;
     const int tr = row / p.G, g = row - tr * p.G;
-    uint32_t ic = 0, ns = 0, no = 0, nx = 0;
-    // the two warps of a pair meet; false if the wait ran out
-    auto meet = [&]() {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(pair);
-        const bool ok = __all_sync(all, mbar_wait(pair, nx & 1, sm.wc));
-        ++nx;
-        return ok;
-    };
-    // the partner's value for this row
-    auto exchange = [&](float mine, float& other) {
-        sm.exchange[warp * 32 + lane] = mine;
-        if (!meet()) return false;
-        other = sm.exchange[(warp ^ 4) * 32 + lane];
-        return meet();
-    };
-    // does either warp of the pair vote for it?  (Two words in turn: a warp is at most one vote ahead of its partner's look.)
-    uint32_t nv = 0;
-    auto either = [&](bool yes, bool& any) {
-        uint32_t* box = sm.votes + (nv++ & 1) * kSoftmaxWarps;
-        yes = __any_sync(all, yes);
-        if (lane == 0) box[warp] = yes;
-        if (!meet()) return false;
-        any = yes || *(volatile uint32_t*)(box + (warp ^ 4)) != 0;
-        return true;
-    };
+    uint32_t ic = 0, ns = 0, no = 0;
     for (;; ++ic) {
         const uint32_t ss = ic % kSched;
         if (!__all_sync(all, mbar_wait(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) return;
@@ -546,104 +549,96 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
         float m = -INFINITY, l = 0.f;
         const int first = range_first(d.range[t]), end = range_end(d.range[t]);
         for (int j = first; j < end; ++j) {
-            const int key = d.kf + j * kTileKeys + half * 64;        // the first of this thread's 64 keys
-            if (!__all_sync(all, mbar_wait(s_full, ns & 1, sm.wc))) return;
+            const int key = d.kf + j * kTileKeys;
+            if (!__all_sync(all, mbar_wait(sm.s_full + t * 8, ns & 1, sm.wc))) return;
             ++ns;
             tc_fence_after();
-            // The row is read twice from tensor memory, 32 columns at a time, rather than held in registers; what the first
-            // pass changes it writes back.
+            // The row is read twice from tensor memory, 32 columns at a time, rather than held in 128 registers: the room is
+            // worth more to the scheduler of the second pass.  What the first pass changes it writes back.
             uint32_t buf[32];
             float* s = reinterpret_cast<float*>(buf);
             const float mul = CAP || BIAS ? 1.f : p.scale_log2e;
-            const bool mask = __any_sync(all, lo > key || hi < key + 64), changed = CAP || BIAS || mask;
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            const bool mask = __any_sync(all, lo > key || hi < key + kTileKeys), changed = CAP || BIAS || mask;
+            float mx[8];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                tmem_ld32(ts + half * 64 + c * 32, buf);
+            for (int i = 0; i < 8; ++i) mx[i] = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                tmem_ld32(ts + c * 32, buf);
                 tmem_ld_wait();
                 if (CAP || BIAS) scores_of<CAP, BIAS>(p, s, slope, (float)(pos - key - c * 32));
                 if (mask) {
-                    const int a = lo - key - c * 32, b = hi - key - c * 32;
+                    const int a = min(max(lo - key - c * 32, 0), 32), b = min(max(hi - key - c * 32, 0), 32);
+                    // bits [a, b) of the 32 (a shift by 32 gives 0)
+                    const uint32_t see = a < b ? __funnelshift_lc(0u, 0xffffffffu, a) & ~__funnelshift_lc(0u, 0xffffffffu, b) : 0u;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) s[i] = i >= a && i < b ? s[i] : -INFINITY;
+                    for (int i = 0; i < 32; ++i) s[i] = see & (1u << i) ? s[i] : -INFINITY;
                 }
-                if (changed) tmem_st32(ts + half * 64 + c * 32, buf);
+                if (changed) tmem_st32(ts + c * 32, buf);
 #pragma unroll
-                for (int i = 0; i < 32; i += 8)
+                for (int i = 0; i < 32; i += 16)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) mx[e] = fmaxf(fmaxf(mx[e], s[i + e]), s[i + 4 + e]);
+                    for (int e = 0; e < 8; ++e) mx[e] = fmaxf(fmaxf(mx[e], s[i + e]), s[i + 8 + e]);
             }
             if (changed) tmem_st_wait();
-            tmem_ld32(ts + half * 64, buf);
-            float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul, other;
-            bool grown = true;
-            if (j > first && !either(tile_max > m + kLazy, grown)) return;
-            if (grown) {
-                if (!exchange(tile_max, other)) return;
-                tile_max = fmaxf(tile_max, other);
-                if (j == first) {
-                    m = tile_max;
-                } else {
-                    // (the products of the tiles before are complete: this tile's scores were issued behind them)
-                    const float mn = fmaxf(m, tile_max);
-                    const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
-                    l *= f;
-                    m = mn;
+            const float tile_max = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * mul;
+            if (j == first) {
+                m = tile_max;
+            } else if (__any_sync(all, tile_max > m + kLazy)) {
+                // (the products of the tiles before are complete: this tile's scores were issued behind them)
+                const float mn = fmaxf(m, tile_max);
+                const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
+                l *= f;
+                m = mn;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    uint32_t o[16];
+                    tmem_ld16(to + c * 16, o);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t o[16];
-                        tmem_ld16(to + c * 16, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_st16(to + c * 16, o);
-                    }
-                    tmem_st_wait();
-                    tc_fence_before();
-                    if (!meet()) return;       // both halves of O are rescaled before either half of P is handed over
+                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    tmem_st16(to + c * 16, o);
                 }
             }
             const float me = m == -INFINITY ? 0.f : m;
             float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             const float2 mul2 = make_float2(mul, mul), me2 = make_float2(-me, -me);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (c > 0) tmem_ld32(ts + half * 64 + c * 32, buf);
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                tmem_ld32(ts + c * 32, buf);
                 tmem_ld_wait();
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float2 x = __ffma2_rn(make_float2(s[2 * i], s[2 * i + 1]), mul2, me2);
-                    // (spread evenly: of every 16 pairs, kEmulated go to the FMA pipe)
+                    // (spread evenly: every 16 pairs, kEmulated of them go to the FMA pipe)
                     const bool emulate = (i * kEmulated) % 16 < kEmulated;
                     const float2 e = emulate ? ex2_fma(x) : make_float2(ex2(x.x), ex2(x.y));
                     sum[i & 3] = __fadd2_rn(sum[i & 3], e);
                     w[i] = pack16<FP16>(e.x, e.y);
                 }
-                tmem_st16(ts + half * 64 + c * 16, w);     // (over scores that this thread has read)
+                tmem_st16(ts + c * 16, w);
+                if (c & 1) {                              // half of the keys: the second product may start
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sm.p_ready + t * 16 + (c >> 1) * 8);
+                }
             }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_ready);
             const float2 all2 = __fadd2_rn(__fadd2_rn(sum[0], sum[1]), __fadd2_rn(sum[2], sum[3]));
             l += all2.x + all2.y;
         }
         // output
-        float other = 0.f;
         if (end > first) {
-            if (!exchange(l, other)) return;
             if (!__all_sync(all, mbar_wait(sm.o_full + t * 8, no & 1, sm.wc))) return;
             ++no;
             tc_fence_after();
         }
-        l += other;
         const float inv = m == -INFINITY ? 0.f : 1.f / l;              // nothing visible: a zero row
         const size_t at = (size_t)((d.part < 0 ? d.tok0 : d.part) + rel) * p.n_q_heads + hq;
-        if (mine && d.part >= 0 && half == 0) p.part_ml[at] = make_float2(m, l);
+        if (mine && d.part >= 0) p.part_ml[at] = make_float2(m, l);
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
+        for (int c = 0; c < D / 32; ++c) {
             uint32_t o[32];
             if (end > first) {
                 tmem_ld32(to + c * 32, o);
@@ -653,21 +648,21 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
                 for (int i = 0; i < 32; ++i) o[i] = 0u;
             }
             if (!mine) continue;
-            const size_t col = at * D + half * (D / 2) + c * 32;
+            // (32 bytes per lane and store: the rows lie far apart, and the store unit is paced by the lines it touches)
             if (d.part < 0) {
-                uint4* dst = reinterpret_cast<uint4*>(p.out + col);
+                uint16_t* dst = p.out + at * D + c * 32;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t w[4];
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t w[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        w[e] = pack16<FP16>(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
-                    dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int e = 0; e < 8; ++e)
+                        w[e] = pack16<FP16>(__uint_as_float(o[16 * i + 2 * e]) * inv, __uint_as_float(o[16 * i + 2 * e + 1]) * inv);
+                    st_global32(dst + 16 * i, w);
                 }
             } else {
-                uint4* dst = reinterpret_cast<uint4*>(p.part_o + col);
+                float* dst = p.part_o + at * D + c * 32;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                for (int i = 0; i < 4; ++i) st_global32(dst + 8 * i, o + 8 * i);
             }
         }
         tc_fence_before();
@@ -679,29 +674,29 @@ __global__ void __launch_bounds__(kThreads, 1)
 big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
            const Params p) {
     using C = Cfg<D>;
-    extern __shared__ __align__(1024) uint8_t raw[];       // (the swizzled tiles need it; there is no static shared memory before it)
+    extern __shared__ uint8_t raw[];
     const Smem sm = carve<D>(raw, p);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(sm.kv_full + s * 8, 1);
-            mbar_init(sm.kv_empty + s * 8, 2);
+            mbar_init(sm.kv_empty + s * 8, 1);
         }
         mbar_init(sm.q_full, 1);
-        mbar_init(sm.q_empty, 2);
+        mbar_init(sm.q_empty, 1);
         for (int t = 0; t < 2; ++t) {
             mbar_init(sm.s_full + t * 8, 1);
-            mbar_init(sm.p_ready + t * 8, 8);
-            mbar_init(sm.wind_down + t * 8, 1);
+            mbar_init(sm.p_ready + t * 16, 4);
+            mbar_init(sm.p_ready + t * 16 + 8, 4);
             mbar_init(sm.o_full + t * 8, 1);
         }
         for (int s = 0; s < kSched; ++s) {
             mbar_init(sm.sched_full + s * 8, 1);
-            mbar_init(sm.sched_empty + s * 8, kSoftmaxWarps + 3);
+            mbar_init(sm.sched_empty + s * 8, kSoftmaxWarps + 4);
         }
+        mbar_init(sm.wind_down, 1);
         mbar_init(sm.tail_go, 1);
         mbar_init(sm.tail_done, 1);
-        for (int w = 0; w < 8; ++w) mbar_init(sm.pair + w * 8, 2);
         sm.wc.abort_flag[0] = 0;
         mbar_init_fence();
     }
@@ -722,9 +717,11 @@ big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         softmax_warp<D, FP16, CAP, BIAS>(p, sm, tmem, warp, lane);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp < kLoadWarp) mma_warp<D, FP16>(p, sm, tmem, warp - kMmaWarp);
+        if (warp == kMmaWarp) mma_warp<D, FP16>(p, sm, tmem);
         else if (warp == kTailWarp) tail_warp<D>(p, sm, lane);
-        else if (warp == kLoadWarp) load_warp<D>(p, sm, &tm_q, &tm_k, &tm_v, n_items, lane);
+        else if (warp == kItemWarp) item_warp<D>(p, sm, &tm_q, n_items, lane);
+        else if (warp == kKeyWarp) load_warp<D>(p, sm, &tm_k, 0, lane);
+        else if (warp == kValueWarp) load_warp<D>(p, sm, &tm_v, 1, lane);
     }
     tc_fence_before();
     __syncthreads();
