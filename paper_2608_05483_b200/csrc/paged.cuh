@@ -115,19 +115,17 @@ __device__ __forceinline__ long long wait_limit(const int32_t* header) {
     const long long v = *reinterpret_cast<const volatile long long*>(header + kLimitWord);
     return v > 0 ? v : kWaitCycles;
 }
-__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, WaitCtl w) {
+// (Kept small: it stands at some thirty places, and an unrolled loop of tries here once made the kernels' code so large that
+// instruction fetch bounded them.)
+__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, const WaitCtl& w) {
     const long long t0 = clock64();
-    long long limit = 0;
-    for (;;) {
-        for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
-        if (*w.abort_flag) return false;
-        if (limit == 0) limit = wait_limit(w.header);
-        if (clock64() - t0 > limit) break;
+#pragma unroll 1
+    for (uint32_t n = 1;; ++n) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((n & 63) == 0 && (*w.abort_flag || clock64() - t0 > wait_limit(w.header))) break;
     }
+    if (!*w.abort_flag) atomicCAS(w.header, 0, PLORA_ERR_TIMEOUT);
     *w.abort_flag = 1;
-    __threadfence_block();
-    atomicCAS(w.header, 0, PLORA_ERR_TIMEOUT);
     return false;
 }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const WaitCtl& w) {
@@ -137,6 +135,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
 // A last look at a barrier before a CTA leaves, whatever the abort flag says: copies in flight must land first.
 __device__ __forceinline__ bool mbar_drain(uint32_t bar, uint32_t parity, long long limit) {
     const long long t0 = clock64();
+#pragma unroll 1
     while (!mbar_try_wait(bar, parity))
         if (clock64() - t0 > limit) return false;
     return true;

@@ -30,7 +30,7 @@ constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatev
 constexpr int kSmallItems = kPlanSms * 2 * 8;   // aimed-at items of the small kernel (two CTAs per SM)
 constexpr int kSmallMinKeys = 128;     // no split shorter than this
 constexpr int kBigItems = kPlanSms * 8;         // aimed-at items of the tensor-core kernel (one CTA per SM)
-constexpr int kBigMinKeys = 512, kBigMaxKeys = 1 << 22;     // (tiles of keys are counted in 16 bits)
+constexpr int kBigMinKeys = 512, kBigMaxKeys = 1 << 21;     // (tiles of keys are counted in 16 bits)
 constexpr int kGroupCache = 2048;      // group starts held in shared memory
 
 struct Sums {        // counts that the scan carries along
