@@ -188,6 +188,7 @@ __device__ __forceinline__ void item_warp(const Params& p, const Smem& sm, const
     uint32_t ic = 0, qn = 0;
     int next = 0;
     if (lane == 0) next = atomicAdd(p.header + kBigNextWord, 1);
+#pragma unroll 1
     for (;; ++ic) {
         const int item = __shfl_sync(all, next, 0);
         const bool more = item < n_items;
@@ -247,6 +248,7 @@ __device__ __forceinline__ void item_warp(const Params& p, const Smem& sm, const
                     if (ok) {
                         const int tiles_q = d.ntok > TT ? 2 : 1;
                         mbar_arrive_expect_tx(sm.q_full, (uint32_t)tiles_q * TT * p.G * D * 2);
+#pragma unroll 1
                         for (int t = 0; t < tiles_q; ++t)
                             for (int c = 0; c < C::kPanels; ++c)
                                 tma_box3(sm.q + t * C::kTileBytes + c * C::kPanelBytes, tm_q, c * 64, d.head * p.G, d.tok0 + t * TT, sm.q_full);
@@ -272,6 +274,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
     const int bp = min(p.page_size, 64);
     uint32_t it = kv, ic = 0;                // stages kv, kv + 2, ...
     bool stopped = false;
+#pragma unroll 1
     for (; !stopped; ++ic) {
         const uint32_t ss = ic % kSched;
         if (!__all_sync(all, mbar_wait(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) break;
@@ -287,6 +290,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
             return lane < kTileKeys / bp && key < k1 ? table[key >> p.page_shift] : 0;
         };
         int page_next = page_of(0);
+#pragma unroll 1
         for (int j = 0; j < n_tiles; ++j, it += 2) {
             const int key = kf + j * kTileKeys, nb = (min(kTileKeys, k1 - key) + bp - 1) / bp;
             int page = page_next;
@@ -301,6 +305,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
                 break;
             }
             if (elect_one()) mbar_arrive_expect_tx(bar, (uint32_t)nb * bp * D * 2);
+#pragma unroll 1
             for (int i = 0; i < nb; ++i) {
                 const int pg = __shfl_sync(all, page, i), so = (key + i * bp) & (p.page_size - 1);
                 if (elect_one()) {
@@ -315,6 +320,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
     // these a barrier is at most one phase further on, and then it answers yes.)
     if (lane == 0) {
         const long long limit = wait_limit(p.header);
+#pragma unroll 1
         for (uint32_t k = 2; k <= (uint32_t)C::kStages && k <= it; k += 2) {
             const uint32_t j = it - k;
             if (!mbar_drain(sm.kv_full + (j % C::kStages) * 8, (j / C::kStages) & 1, limit)) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
@@ -336,7 +342,7 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
     constexpr uint32_t kHi = (uint32_t)(smem_desc(0, 0, 1024) >> 32);
     constexpr uint32_t kLoK = 1u << 16, kLoV = (uint32_t)(C::kPanelBytes >> 4) << 16;     // leading offsets: unused; the next panel
     const bool withhold = p.header[kHookWord] == PLORA_HOOK_WITHHOLD_RELEASE;   // test hook: stages are never handed back
-    uint32_t it = 0, ic = 0, qn = 0, tails = 0, np[2] = {0, 0};
+    uint32_t it = 0, ic = 0, qn = 0, tails = 0, np = 0;       // np: a phase bit for each tile
     const uint32_t q_lo = uniform((sm.q >> 4) | kLoK), ring_lo = uniform(sm.ring >> 4);
     tmem = uniform(tmem);
     bool ok = true;
@@ -344,12 +350,13 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
         ok = __all_sync(all, mbar_wait(bar, parity, sm.wc));
         return ok;
     };
+#pragma unroll 1
     for (;; ++ic) {
         const uint32_t ss = ic % kSched;
         if (!wait_for(sm.sched_full + ss * 8, (ic / kSched) & 1)) break;
         const Item& src = sm.items[ss];
         const int n_tiles = (int)uniform(src.n_tiles), more = (int)uniform(src.more), last = (int)uniform(src.k1 - src.kf);
-        const int ranges[2] = {(int)uniform(src.range[0]), (int)uniform(src.range[1])};
+        const int range0 = (int)uniform(src.range[0]), range1 = (int)uniform(src.range[1]);
         if (elect_one()) mbar_arrive(sm.sched_empty + ss * 8);
         if (!more) break;
         if (n_tiles == 0) continue;
@@ -358,6 +365,7 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
         // step j: O += P V of key tile j - 1, then S = Q K^T of key tile j, for each tile of rows that looks at them.  What the
         // step needs of K and V is waited for first, so that nothing stands between a tile's weights and its next scores:
         // the two tiles then settle into turns, one in the softmax while the other has the tensor cores.
+#pragma unroll 1
         for (int j = 0; j <= n_tiles; ++j) {
             uint32_t v_slot = 0, k_slot = 0;
             int steps = kTileKeys / 16;
@@ -381,21 +389,21 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
                 ++it;
             }
             const uint32_t v = (ring_lo + v_slot * (C::kTileBytes >> 4)) | kLoV, k = (ring_lo + k_slot * (C::kTileBytes >> 4)) | kLoK;
-#pragma unroll
+#pragma unroll 1
             for (int t = 0; t < 2; ++t) {
-                const int first = range_first(ranges[t]), end = range_end(ranges[t]);
+                const int range = t ? range1 : range0, first = range_first(range), end = range_end(range);
                 const uint32_t o = tmem + kTmemO + t * kTmemTile, ts = tmem + kTmemS + t * kTmemTile, q = q_lo + t * (C::kTileBytes >> 4);
                 const bool pv = j > first && j <= end, qk = j >= first && j < end;
                 if (pv) {
-                    if (!wait_for(sm.p_ready + t * 16, np[t] & 1)) break;
+                    if (!wait_for(sm.p_ready + t * 16, (np >> t) & 1)) break;
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
                         for (int s = 0; s < 4; ++s)
                             if (s < steps) umma_ts(o, ts + s * 8, desc_of(v + s * 128, kHi), idesc_o, j - 1 > first || s > 0);
                     }
-                    if (!wait_for(sm.p_ready + t * 16 + 8, np[t] & 1)) break;
-                    ++np[t];
+                    if (!wait_for(sm.p_ready + t * 16 + 8, (np >> t) & 1)) break;
+                    np ^= 1u << t;
                 }
                 tc_fence_after();
                 if (elect_one()) {
@@ -438,6 +446,7 @@ __device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int l
     using C = Cfg<D>;
     const unsigned all = 0xffffffffu;
     uint32_t it = 0, ic = 0, tails = 0;
+#pragma unroll 1
     for (;; ++ic) {
         const uint32_t ss = ic % kSched;
         if (!__all_sync(all, mbar_wait(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) return;
@@ -452,6 +461,7 @@ __device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int l
         ++tails;
         const uint32_t v = sm.ring + (it - 1) % C::kStages * C::kTileBytes;
         const int n = (16 - (left & 15)) * (D / 8);
+#pragma unroll 1
         for (int i = lane; i < n; i += 32) {
             const int r = left + i / (D / 8), c = i % (D / 8);
             sts128(v + (c >> 3) * C::kPanelBytes + r * 128 + ((c & 7) << 4), 0u, 0u, 0u, 0u);
@@ -526,6 +536,7 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
     const uint32_t ts = tmem + lanes + kTmemS + t * kTmemTile, to = tmem + lanes + kTmemO + t * kTmemTile;
     const int tr = row / p.G, g = row - tr * p.G;
     uint32_t ic = 0, ns = 0, no = 0;
+#pragma unroll 1
     for (;; ++ic) {
         const uint32_t ss = ic % kSched;
         if (!__all_sync(all, mbar_wait(sm.sched_full + ss * 8, (ic / kSched) & 1, sm.wc))) return;
@@ -548,6 +559,7 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
         }
         float m = -INFINITY, l = 0.f;
         const int first = range_first(d.range[t]), end = range_end(d.range[t]);
+#pragma unroll 1
         for (int j = first; j < end; ++j) {
             const int key = d.kf + j * kTileKeys;
             if (!__all_sync(all, mbar_wait(sm.s_full + t * 8, ns & 1, sm.wc))) return;
@@ -590,7 +602,7 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
                 const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
                 l *= f;
                 m = mn;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D / 16; ++c) {
                     uint32_t o[16];
                     tmem_ld16(to + c * 16, o);
@@ -637,7 +649,7 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
         const float inv = m == -INFINITY ? 0.f : 1.f / l;              // nothing visible: a zero row
         const size_t at = (size_t)((d.part < 0 ? d.tok0 : d.part) + rel) * p.n_q_heads + hq;
         if (mine && d.part >= 0) p.part_ml[at] = make_float2(m, l);
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
             uint32_t o[32];
             if (end > first) {
