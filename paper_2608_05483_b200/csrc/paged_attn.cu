@@ -29,9 +29,15 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatever the device has: it sizes the workspace
 constexpr int kSmallItems = kPlanSms * 2 * 8;   // aimed-at items of the small kernel (two CTAs per SM)
 constexpr int kSmallMinKeys = 128;     // no split shorter than this
-constexpr int kBigItems = kPlanSms * 8;         // aimed-at items of the tensor-core kernel (one CTA per SM)
-constexpr int kBigMinKeys = 512, kBigMaxKeys = 1 << 21;     // (tiles of keys are counted in 16 bits)
+// Splits of the tensor-core kernel (one CTA per SM).  A CTA alone is slow to start (some 4 us until its first scores), so a
+// batch that gives a CTA no more than kBigOneRound keys is cut into at most one item per SM (128 of the 148: the last
+// pieces are short ones); a longer one into four per SM, which even out as they are taken from a counter.
+// (64 requests in groups: 43 us with pieces of 512 keys, two rounds; 16 to 8192 prompt tokens behind caches: fewer and
+// longer pieces, or the merge costs what the balance gains.)
+constexpr int kBigItemsOne = 128, kBigItems = kPlanSms * 8;
+constexpr int kBigMinKeys = 256, kBigOneRound = 2048, kBigMaxKeys = 1 << 22;     // (tiles of keys are counted in 16 bits)
 constexpr int kGroupCache = 2048;      // group starts held in shared memory
+constexpr int kLargeCache = 256;       // large requests of 1024 whose units are written by a warp each (the others: by a thread)
 
 struct Sums {        // counts that the scan carries along
     int small, big, part;
@@ -55,15 +61,6 @@ __device__ __forceinline__ void token_range(const Params& p, int r, int& tok0, i
     }
 }
 __device__ __forceinline__ int kv_of(const Params& p, int r) { return clampi(p.kv_len[r], 0, p.max_kv); }
-
-// Do requests [s, e) read a common prefix together: more than one, and one token each?
-__device__ __forceinline__ bool one_token_each(const Params& p, int s, int e) {
-    if (e - s < 2) return false;
-    int t0, t1, n;
-    token_range(p, s, t0, n);
-    token_range(p, e - 1, t1, n);
-    return t1 + n - t0 == e - s;
-}
 
 // Keys [lo, hi) visible to the token at position pos of a cache of kv tokens.
 __device__ __forceinline__ TokInfo visible(const Params& p, int t, int pos, int kv) {
@@ -121,11 +118,12 @@ __device__ __forceinline__ void sum_all(long long& a, long long& b, long long (*
     }
 }
 
-__device__ void write_token_info(const Params& p) {
+template <bool RAGGED>
+__device__ __forceinline__ void write_token_info(const Params& p) {
     const int t = (blockIdx.x - 1) * kPlanThreads + threadIdx.x;
     if (t >= p.n_tok) return;
     int r = t, pos, kv;
-    if (p.tok_start) {
+    if (RAGGED) {
         int lo = 0, hi = p.n_req;        // the last request whose first token is not behind t
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -149,41 +147,80 @@ __device__ void write_token_info(const Params& p) {
     p.tok_info[t] = visible(p, t, pos, kv);
 }
 
+// A large request, kept for the warps that write its units.
+struct Large {
+    Req q;
+    int r, unit, part;
+    bool room;
+};
+
+// RAGGED: token counts per request are given; GROUPED: groups are given.  (Forms of their own, because the plan's time is
+// that of a few dependent loads and of fetching its code.)
+template <bool RAGGED, bool GROUPED>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     grid_wait();
     grid_launch_dependents();
     if (blockIdx.x > 0) {
-        write_token_info(p);
+        write_token_info<RAGGED>(p);
         return;
     }
     __shared__ Sums warp_sums[kPlanThreads / 32];
     __shared__ long long red[2][kPlanThreads / 32];
     __shared__ int s_group[kGroupCache + 1], s_prefix[kGroupCache];
-    __shared__ int s_merge;
+    __shared__ int s_kv[kPlanThreads], s_tok[kPlanThreads + 1];
+    __shared__ Large s_large[kLargeCache];
+    __shared__ int s_merge, s_n_large;
     const int tid = threadIdx.x;
     if (tid == 0) s_merge = 0;
     // tokens of a unit: the rows of a tile of the small kernel, or two tiles of the big one
     const int TBs = max(1, kSmallRows / p.G), TBb = 2 * p.big_tile_tok;
-    auto is_small = [&](int n) { return n * p.G <= kSmallRows; };
-    const bool cached = p.n_groups <= kGroupCache;
-    auto group_at = [&](int g) { return clampi(p.group_start[g], 0, p.n_req); };
-    auto read_prefix = [&](int g) {                // tokens of the prefix that group g reads together, 0: none
-        const int s = group_at(g), e = group_at(g + 1), pre = p.prefix_len[g];
-        return one_token_each(p, s, e) ? clampi(pre, 0, kv_of(p, s)) : 0;
-    };
-    if (p.n_groups > 0 && cached) {
-        for (int g = tid; g <= p.n_groups; g += kPlanThreads) s_group[g] = group_at(g);
-        for (int g = tid; g < p.n_groups; g += kPlanThreads) s_prefix[g] = read_prefix(g);
+    auto is_small = [&](int n) { return n * p.G <= kSmallRows; };       // (one token is, unless a KV head has more query heads)
+    // What is looked at again and again is loaded once, all at the same time (most batches have no more requests than the
+    // CTA has threads; what does not fit is read where it lies).
+    const bool cached = p.n_groups <= kGroupCache, held = p.n_req <= kPlanThreads;
+    if (tid < p.n_req) {
+        s_kv[tid] = kv_of(p, tid);
+        if (RAGGED) s_tok[tid] = clampi(p.tok_start[tid], 0, p.n_tok);
+    }
+    if (RAGGED && tid == 0 && held) s_tok[p.n_req] = clampi(p.tok_start[p.n_req], 0, p.n_tok);
+    if (GROUPED && cached) {
+        for (int g = tid; g <= p.n_groups; g += kPlanThreads) s_group[g] = clampi(p.group_start[g], 0, p.n_req);
+        for (int g = tid; g < p.n_groups; g += kPlanThreads) s_prefix[g] = p.prefix_len[g];
     }
     __syncthreads();
-    auto gstart = [&](int g) { return cached ? s_group[g] : group_at(g); };
-    auto prefix_of = [&](int g) { return cached ? s_prefix[g] : read_prefix(g); };
+    auto kv_at = [&](int r) { return held ? s_kv[r] : kv_of(p, r); };
+    auto tokens_of = [&](int r, int& tok0, int& n) {
+        if (!RAGGED) {
+            tok0 = r;
+            n = 1;
+        } else if (held) {
+            tok0 = s_tok[r];
+            n = max(s_tok[r + 1], tok0) - tok0;
+        } else {
+            token_range(p, r, tok0, n);
+        }
+    };
+    auto gstart = [&](int g) { return cached ? s_group[g] : clampi(p.group_start[g], 0, p.n_req); };
+    // tokens of the prefix that group g reads together (more than one request, one token each), 0: none
+    auto read_prefix = [&](int g, int len) {
+        const int s = gstart(g), e = gstart(g + 1);
+        if (e - s < 2) return 0;
+        int t0, t1, n;
+        tokens_of(s, t0, n);
+        tokens_of(e - 1, t1, n);
+        return t1 + n - t0 == e - s ? clampi(len, 0, kv_at(s)) : 0;
+    };
+    if (GROUPED && cached) {
+        for (int g = tid; g < p.n_groups; g += kPlanThreads) s_prefix[g] = read_prefix(g, s_prefix[g]);
+        __syncthreads();
+    }
+    auto prefix_of = [&](int g) { return cached ? s_prefix[g] : read_prefix(g, p.prefix_len[g]); };
     auto request = [&](int r) {
         Req q{0, 0, 0, 0};
         if (r >= p.n_req) return q;
-        token_range(p, r, q.tok0, q.n);
-        q.kv = kv_of(p, r);
-        if (p.n_groups > 0) {
+        tokens_of(r, q.tok0, q.n);
+        q.kv = kv_at(r);
+        if (GROUPED) {
             int lo = 0, hi = p.n_groups;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -221,25 +258,32 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     const Req first = request(tid);              // (kept: most batches have no more requests than the CTA has threads)
     for (int r = tid; r < p.n_req; r += kPlanThreads) {
         const Req q = r == tid ? first : request(r);
-        const int TB = is_small(q.n) ? TBs : TBb;
-        long long keys = 0;
-        for (int b = 0; b * TB < q.n; ++b) {
-            int k0, k1;
-            block_keys(q, b, TB, k0, k1);
-            keys += k1 - k0;
+        int k0, k1;
+        if (is_small(q.n)) {
+            if (q.n > 0) {
+                block_keys(q, 0, TBs, k0, k1);
+                keys_s += k1 - k0;
+            }
+        } else if (p.key_hi || q.kv < q.n + q.pre) {
+            for (int b = 0; b * TBb < q.n; ++b) {
+                block_keys(q, b, TBb, k0, k1);
+                keys_b += k1 - k0;
+            }
+        } else {           // block b sees kv - n + min(n, (b + 1) TBb) keys
+            const long long nb = (q.n + TBb - 1) / TBb;
+            keys_b += nb * (q.kv - q.n - q.pre) + TBb * (nb * (nb - 1) / 2) + q.n;
         }
-        if (is_small(q.n)) keys_s += keys;
-        else keys_b += keys;
     }
-    for (int g = tid; g < p.n_groups; g += kPlanThreads) {
+    for (int g = tid; GROUPED && g < p.n_groups; g += kPlanThreads) {
         const int n = gstart(g + 1) - gstart(g), pre = prefix_of(g);
         if (is_small(n)) keys_s += pre;
         else keys_b += (long long)pre * ((n + TBb - 1) / TBb);
     }
     sum_all(keys_s, keys_b, red);
     const long long per_s = (keys_s * p.n_kv_heads + kSmallItems - 1) / kSmallItems;
-    const long long per_b = (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems;
     const int chunk_s = (int)min((long long)INT_MAX / 2, max((long long)kSmallMinKeys, (per_s + 63) / 64 * 64));
+    long long per_b = (keys_b * p.n_kv_heads + kBigItemsOne - 1) / kBigItemsOne;
+    if (per_b > kBigOneRound) per_b = max((long long)kBigOneRound, (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems);
     const int chunk_b = (int)min((long long)kBigMaxKeys, max((long long)kBigMinKeys, (per_b + 127) / 128 * 128));
     auto splits_of = [&](int keys, bool small) { const int c = small ? chunk_s : chunk_b; return (keys + c - 1) / c; };
     auto fits = [&](const Sums& at, const Sums& want) {
@@ -249,7 +293,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
 
     Sums carry{0, 0, 0}, total;
     // the groups' prefixes: always partial results
-    for (int g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
+    for (int g0 = 0; GROUPED && g0 < p.n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
         int pre = 0, s = 0, n = 0, tok0 = 0, nn;
         if (g < p.n_groups) {
@@ -285,38 +329,86 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         const int r = r0 + tid;
         const Req q = r0 == 0 ? first : request(r);
         const bool small = is_small(q.n);
-        const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b;
+        const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b, nb = (q.n + TB - 1) / TB;
         Sums want{0, 0, 0};
-        for (int b = 0; b * TB < q.n; ++b) {
-            int k0, k1;
-            block_keys(q, b, TB, k0, k1);
-            const int splits = splits_of(k1 - k0, small);
-            (small ? want.small : want.big) += splits;
-            if (splits > 1 || q.pre > 0) want.part += splits * min(TB, q.n - b * TB);
+        if (!small && q.kv - q.pre <= chunk && q.kv >= q.n + q.pre && !p.key_hi) {
+            want.big = nb;                          // no block is split, and each has a key
+            want.part = q.pre > 0 ? q.n : 0;
+        } else {
+            for (int b = 0; b < nb; ++b) {
+                int k0, k1;
+                block_keys(q, b, TB, k0, k1);
+                const int splits = splits_of(k1 - k0, small);
+                (small ? want.small : want.big) += splits;
+                if (splits > 1 || q.pre > 0) want.part += splits * min(TB, q.n - b * TB);
+            }
         }
-        Sums at = carry + scan_exclusive(want, total, warp_sums);
+        const Sums at = carry + scan_exclusive(want, total, warp_sums);
         const bool room = fits(at, want);
         if (!room) atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
-        // (the last block first: it sees the most keys, and the items are taken in this order)
-        int unit = small ? at.small : at.big;
-        for (int b = (q.n + TB - 1) / TB - 1; b >= 0; --b) {
-            int k0, k1;
-            block_keys(q, b, TB, k0, k1);
-            const int splits = room ? splits_of(k1 - k0, small) : 0, nt = min(TB, q.n - b * TB);
+        // writes the units of one block, and lists its tokens if they need a merge
+        auto write_block = [&](const Req& q, int r, int b, bool small, int splits, int k0, int k1, int unit, int part) {
+            const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b, nt = min(TB, q.n - b * TB);
             const bool direct = splits == 1 && q.pre == 0;
             for (int i = 0; i < splits; ++i)
                 put(small, unit + i, Unit{q.tok0 + b * TB, nt, r, k0 + i * chunk, min(k1, k0 + (i + 1) * chunk),
-                                          direct ? -1 : at.part + i * nt, {0, 0}});
-            if (!direct) {
-                const int m0 = atomicAdd(&s_merge, nt);      // (in any order: every token's result is its own)
-                for (int t = 0; t < nt; ++t) {
-                    const int tok = q.tok0 + b * TB + t;
-                    const int4 pre = q.pre > 0 ? p.tok_prefix[tok] : make_int4(0, 0, 0, 0);
-                    if (m0 + t < p.n_tok) p.tok_merge[m0 + t] = TokMerge{tok, {at.part + t, pre.x}, {splits, pre.y}, {nt, pre.z}, 0};
-                }
-                at.part += splits * nt;
+                                          direct ? -1 : part + i * nt, {0, 0}});
+            if (direct) return;
+            const int m0 = atomicAdd(&s_merge, nt);      // (in any order: every token's result is its own)
+            for (int t = 0; t < nt; ++t) {
+                const int tok = q.tok0 + b * TB + t;
+                const int4 pre = q.pre > 0 ? p.tok_prefix[tok] : make_int4(0, 0, 0, 0);
+                if (m0 + t < p.n_tok) p.tok_merge[m0 + t] = TokMerge{tok, {part + t, pre.x}, {splits, pre.y}, {nt, pre.z}, 0};
             }
-            unit += splits;
+        };
+        int slot = kLargeCache;
+        if (RAGGED) {
+            if (tid == 0) s_n_large = 0;
+            __syncthreads();
+        }
+        if (RAGGED && !small) slot = atomicAdd(&s_n_large, 1);
+        if (slot < kLargeCache) {
+            s_large[slot] = Large{q, r, at.big, at.part, room};
+        } else if (q.n > 0) {
+            // (the last block first: it sees the most keys, and the items are taken in this order)
+            int unit = small ? at.small : at.big, part = at.part;
+            for (int b = nb - 1; b >= 0; --b) {
+                int k0, k1;
+                block_keys(q, b, TB, k0, k1);
+                const int splits = room ? splits_of(k1 - k0, small) : 0;
+                write_block(q, r, b, small, splits, k0, k1, unit, part);
+                unit += splits;
+                if (splits > 1 || q.pre > 0) part += splits * min(TB, q.n - b * TB);
+            }
+        }
+        // large requests: a warp each, a lane per block
+        if (RAGGED) __syncthreads();
+        const int lane = tid & 31;
+        for (int w = tid >> 5; RAGGED && w < min(s_n_large, kLargeCache); w += kPlanThreads / 32) {
+            const Large big = s_large[w];
+            const int blocks = (big.q.n + TBb - 1) / TBb;
+            int unit = big.unit, part = big.part;
+            for (int b0 = blocks - 1; b0 >= 0; b0 -= 32) {
+                const int b = b0 - lane;
+                int k0 = 0, k1 = 0, splits = 0, parts = 0;
+                if (b >= 0) {
+                    block_keys(big.q, b, TBb, k0, k1);
+                    splits = big.room ? splits_of(k1 - k0, false) : 0;
+                    if (splits > 1 || big.q.pre > 0) parts = splits * min(TBb, big.q.n - b * TBb);
+                }
+                int su = splits, sp = parts;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int a = __shfl_up_sync(0xffffffffu, su, d), c = __shfl_up_sync(0xffffffffu, sp, d);
+                    if (lane >= d) {
+                        su += a;
+                        sp += c;
+                    }
+                }
+                if (b >= 0) write_block(big.q, big.r, b, false, splits, k0, k1, unit + su - splits, part + sp - parts);
+                unit += __shfl_sync(0xffffffffu, su, 31);
+                part += __shfl_sync(0xffffffffu, sp, 31);
+            }
         }
         carry = carry + total;
     }
@@ -341,28 +433,43 @@ __global__ void __launch_bounds__(128) merge_kernel(const Params p) {
         const int hq = (int)(row % p.n_q_heads);
         const TokMerge tm = p.tok_merge[row / p.n_q_heads];
         constexpr int V = D / 32;
+        // A lane looks at one partial result's maximum and sum, all at once (32 at a time); then the outputs are added up.
         float o[V], M = -INFINITY, L = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) o[v] = 0.f;
+        const int n = tm.n[0] + tm.n[1];
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const int i = i0 + lane;
+            const bool own = i < tm.n[0];
+            size_t at = 0;
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (i < n) {
+                at = (size_t)(own ? tm.base[0] + i * tm.stride[0] : tm.base[1] + (i - tm.n[0]) * tm.stride[1]) * p.n_q_heads + hq;
+                ml = p.part_ml[at];
+            }
+            float m = ml.x;
+            for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            const float Mn = fmaxf(M, m), Me = Mn == -INFINITY ? 0.f : Mn, back = ex2(M - Me), f = ex2(ml.x - Me);
+            float l = f * ml.y;
+            for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+            L = L * back + l;
+            M = Mn;
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-            for (int i = 0; i < tm.n[s]; ++i) M = fmaxf(M, p.part_ml[(size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq].x);
-        const float Me = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            for (int i = 0; i < tm.n[s]; ++i) {
-                const size_t at = (size_t)(tm.base[s] + i * tm.stride[s]) * p.n_q_heads + hq;
-                const float2 ml = p.part_ml[at];
-                const float f = ex2(ml.x - Me);
-                L = fmaf(f, ml.y, L);
-                const float* src = p.part_o + at * D + lane * V;
+            for (int v = 0; v < V; ++v) o[v] *= back;
+            const int here = min(32, n - i0);
+#pragma unroll 4
+            for (int k = 0; k < here; ++k) {
+                const float fk = __shfl_sync(0xffffffffu, f, k);
+                const size_t ak = __shfl_sync(0xffffffffu, (unsigned long long)at, k);
+                const float* src = p.part_o + ak * D + lane * V;
 #pragma unroll
                 for (int v = 0; v < V; v += 2) {
                     const float2 x = *reinterpret_cast<const float2*>(src + v);
-                    o[v] = fmaf(f, x.x, o[v]);
-                    o[v + 1] = fmaf(f, x.y, o[v + 1]);
+                    o[v] = fmaf(fk, x.x, o[v]);
+                    o[v + 1] = fmaf(fk, x.y, o[v + 1]);
                 }
             }
+        }
         const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);    // nothing visible: a zero row
         uint16_t* dst = p.out + ((size_t)tm.tok * p.n_q_heads + hq) * D + lane * V;
 #pragma unroll
@@ -393,7 +500,7 @@ int tile_tokens(int G) { return kBigRows / G; }
 // kind, so the units are at most one per block plus that many / heads; blocks that are split make at most twice that many.
 Caps caps(long long n_tok, long long n_req, long long max_kv, int n_kv_heads, int G) {
     const long long TBs = kSmallRows / G > 0 ? kSmallRows / G : 1, TBb = 2 * tile_tokens(G);
-    const long long extra_s = (kSmallItems + n_kv_heads - 1) / n_kv_heads, extra_b = (kBigItems + n_kv_heads - 1) / n_kv_heads;
+    const long long extra_s = (kSmallItems + n_kv_heads - 1) / n_kv_heads, extra_b = (kBigItems + n_kv_heads - 1) / n_kv_heads;   // (kBigItems > kBigItemsOne)
     Caps c;
     c.small = 2 * n_req + extra_s + 1;
     c.big = n_tok / TBb + 2 * n_req + extra_b + 1;
@@ -535,8 +642,10 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     void* args[] = {&p};
-    if (launch_pdl((const void*)plan_kernel, dim3(1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads), dim3(kPlanThreads), 0, st, args) !=
-        cudaSuccess)
+    const bool ragged = p.tok_start != nullptr, grouped = p.n_groups > 0;
+    const void* pk = ragged ? (grouped ? (const void*)plan_kernel<true, true> : (const void*)plan_kernel<true, false>)
+                            : (grouped ? (const void*)plan_kernel<false, true> : (const void*)plan_kernel<false, false>);
+    if (launch_pdl(pk, dim3(1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads), dim3(kPlanThreads), 0, st, args) != cudaSuccess)
         return cuda_failed();
     // a small unit holds whatever fits into its rows; single tokens that share nothing always do
     const bool big = p.G > kSmallRows || ((p.tok_start || p.n_groups > 0) && (long long)p.n_tok * p.G > kSmallRows);
