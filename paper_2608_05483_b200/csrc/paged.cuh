@@ -75,7 +75,8 @@ struct Params {
     int32_t page_size, page_shift, n_pages, max_blocks;
     int32_t max_kv;           // min(max_blocks, n_pages) * page_size
     float scale_log2e;        // softmax scale times log2(e): scores live in the base-2 domain
-    float cap_x;              // scale / cap
+    float cap_d[5];           // its polynomial, for |qk| <= cap_poly_below
+    float cap_poly_below;
     float cap_in, cap_log2e;  // capped scores: cap_log2e * tanh(cap_in * qk), cap_in already times 2 log2(e)
 };
 

@@ -32,7 +32,8 @@ constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kKeyWarp = 9, kTailWarp = 10, kIt
 constexpr int kThreads = 16 * 32;       // four warpgroups (the last three warps only give their registers away)
 constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;       // of 128 a thread at launch: 2 * 184 + 2 * 72 = 4 * 128
 constexpr int kSched = 2;
-constexpr int kEmulated = 6;        // of 16 pairs of weights, how many are computed on the FMA pipe
+// Of 16 pairs of weights, how many are computed on the FMA pipe (which the cap's polynomial keeps busy already).
+constexpr int kEmulated = 6, kEmulatedCap = 2;
 constexpr float kLazy = 8.f;        // base-2 logarithm of the growth a row's maximum may have before O is rescaled
 
 template <int D>
@@ -489,28 +490,24 @@ __device__ __forceinline__ float2 ex2_fma(float2 x) {
 }
 
 // 32 raw products of a row -> scores in the base-2 domain (cap, bias by distance); dist0: distance of the first one's key.
-// Below |x| = 1 the cap's tanh is an odd polynomial on the FMA pipe (degree 13, fitted to tanh(x) / x in x^2, error 4.4e-8);
-// a warp that sees a larger argument takes the form with two special functions (see score()).
+// Below |x| = 3/4 the cap's tanh(x) is x P(x^2) on the FMA pipe, P of degree 4 fitted for the least absolute error (1.9e-7; it
+// is multiplied by the cap), its coefficients scaled so that it takes the raw product: s (d0 + s^2 (d1 + ...)).  A warp that
+// sees a larger argument takes the form with two special functions (see score()).
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ void scores_of(const Params& p, float* s, float slope, float dist0) {
     if (CAP) {
-        const float2 mul = make_float2(p.cap_x, p.cap_x), cap = make_float2(p.cap_log2e, p.cap_log2e);
         float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            most = fmaxf(fmaxf(most, fabsf(s[i])), fabsf(s[i + 1]));
-        }
-        if (__all_sync(0xffffffffu, most * fabsf(p.cap_x) <= 1.f)) {
+        for (int i = 0; i < 32; i += 2) most = fmaxf(fmaxf(most, fabsf(s[i])), fabsf(s[i + 1]));
+        if (__all_sync(0xffffffffu, most <= p.cap_poly_below)) {
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-                const float2 x = __fmul2_rn(make_float2(s[i], s[i + 1]), mul), u = __fmul2_rn(x, x);
-                float2 q = __ffma2_rn(u, make_float2(0.0010531365405768156f, 0.0010531365405768156f), make_float2(-0.006239818874746561f, -0.006239818874746561f));
-                q = __ffma2_rn(q, u, make_float2(0.020331112667918205f, 0.020331112667918205f));
-                q = __ffma2_rn(q, u, make_float2(-0.05347844585776329f, -0.05347844585776329f));
-                q = __ffma2_rn(q, u, make_float2(0.13325709104537964f, 0.13325709104537964f));
-                q = __ffma2_rn(q, u, make_float2(-0.33332881331443787f, -0.33332881331443787f));
-                q = __ffma2_rn(q, u, make_float2(0.9999999403953552f, 0.9999999403953552f));
-                q = __fmul2_rn(q, __fmul2_rn(x, cap));
+                const float2 x = make_float2(s[i], s[i + 1]), u = __fmul2_rn(x, x);
+                float2 q = __ffma2_rn(u, make_float2(p.cap_d[4], p.cap_d[4]), make_float2(p.cap_d[3], p.cap_d[3]));
+                q = __ffma2_rn(q, u, make_float2(p.cap_d[2], p.cap_d[2]));
+                q = __ffma2_rn(q, u, make_float2(p.cap_d[1], p.cap_d[1]));
+                q = __ffma2_rn(q, u, make_float2(p.cap_d[0], p.cap_d[0]));
+                q = __fmul2_rn(q, x);
                 s[i] = q.x;
                 s[i + 1] = q.y;
             }
@@ -623,8 +620,8 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float2 x = __ffma2_rn(make_float2(s[2 * i], s[2 * i + 1]), mul2, me2);
-                    // (spread evenly: every 16 pairs, kEmulated of them go to the FMA pipe)
-                    const bool emulate = (i * kEmulated) % 16 < kEmulated;
+                    constexpr int kFma = CAP ? kEmulatedCap : kEmulated;       // (spread evenly)
+                    const bool emulate = (i * kFma) % 16 < kFma;
                     const float2 e = emulate ? ex2_fma(x) : make_float2(ex2(x.x), ex2(x.y));
                     sum[i & 3] = __fadd2_rn(sum[i & 3], e);
                     w[i] = pack16<FP16>(e.x, e.y);
