@@ -42,6 +42,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     __shared__ int s_tok[kPlanThreads], s_page[kPlanThreads], s_old[kPlanThreads];
     __shared__ int2 s_warp[kPlanThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int cursor = p.cursor_in ? *p.cursor_in : 0;
     const int t = blockIdx.x * kPlanThreads + tid;      // this thread's token
     int2 carry = make_int2(0, 0);
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(256) table_kernel(const TableParams p) {
 
 // ---- rotary positions and the cache write -------------------------------------------------------------------------
 // A thread takes 2 V values of one head: V pairs (a, b) of the rotated part (its halves, or neighbours), or 2 V values
-// of the part that passes through.  Pure streaming: every projection value is read once and leaves once.
+// of the part that passes through.  Pure streaming: every projection value is read once and leaves once; bound by HBM.
 struct RopeParams {
     const void *q, *k, *v;
     long long q_stride, k_stride, v_stride;   // elements between tokens
@@ -194,29 +196,65 @@ template <typename T, int V>
 struct alignas((sizeof(T) * V) < 16 ? sizeof(T) * V : 16) Vec {
     T x[V];
 };
-template <typename T, int V>
-__device__ __forceinline__ void load(const T* p, float (&f)[V]) {
-    const Vec<T, V> v = *reinterpret_cast<const Vec<T, V>*>(p);
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_f(v.x[i]);
+// Two runs of V values; 32 bytes that lie together go in one access.
+__device__ __forceinline__ void ld32(const void* p, uint32_t (&w)[8]) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
 }
-template <typename T, int V>
-__device__ __forceinline__ void store(T* p, const float (&f)[V]) {
-    Vec<T, V> v;
+__device__ __forceinline__ void st32(void* p, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+template <typename T, int V, bool WIDE>
+__device__ __forceinline__ void load(const T* p, int ia, int ib, float (&f)[2 * V]) {
+    if (WIDE && sizeof(T) * V == 16 && ib == ia + V) {
+        uint32_t w[8];
+        ld32(p + ia, w);
 #pragma unroll
-    for (int i = 0; i < V; ++i) from_f(f[i], v.x[i]);
-    *reinterpret_cast<Vec<T, V>*>(p) = v;
+        for (int i = 0; i < 2 * V; ++i) f[i] = to_f(reinterpret_cast<const T*>(w)[i]);
+        return;
+    }
+    const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(p + ia), b = *reinterpret_cast<const Vec<T, V>*>(p + ib);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        f[i] = to_f(a.x[i]);
+        f[V + i] = to_f(b.x[i]);
+    }
+}
+template <typename T, int V, bool WIDE>
+__device__ __forceinline__ void store(T* p, int ia, int ib, const float (&f)[2 * V]) {
+    Vec<T, V> a, b;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        from_f(f[i], a.x[i]);
+        from_f(f[V + i], b.x[i]);
+    }
+    if (WIDE && sizeof(T) * V == 16 && ib == ia + V) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = reinterpret_cast<const uint32_t*>(&a)[i];
+            w[4 + i] = reinterpret_cast<const uint32_t*>(&b)[i];
+        }
+        st32(p + ia, w);
+        return;
+    }
+    *reinterpret_cast<Vec<T, V>*>(p + ia) = a;
+    *reinterpret_cast<Vec<T, V>*>(p + ib) = b;
 }
 
-template <typename TI, typename TO, int V, bool INTER>
-__global__ void __launch_bounds__(256) rope_kernel(const RopeParams p) {
-    const long long n = (long long)p.n_tok * p.per_tok;
-    const long long j = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (j >= n) return;
-    const int t = (int)(j / p.per_tok), rest = (int)(j - (long long)t * p.per_tok);
+// WIDE: bases and strides are multiples of 32 bytes.
+template <typename TI, typename TO, int V, bool INTER, bool WIDE>
+__global__ void __launch_bounds__(256, 8) rope_kernel(const RopeParams p) {
+    // the block's first chunk: one 64-bit division for the block, small ones for the threads
+    const long long first = (long long)blockIdx.x * 256;
+    const int t0 = (int)(first / p.per_tok);
+    const unsigned x0 = (unsigned)(first - (long long)t0 * p.per_tok) + threadIdx.x, more = x0 / (unsigned)p.per_tok;
+    const int t = t0 + (int)more, rest = (int)(x0 - more * (unsigned)p.per_tok);
+    if (t >= p.n_tok) return;
     const int h = rest / p.per_head, c = rest - h * p.per_head;
     const int D = p.head_dim, half = p.rot_dim / 2, rot_chunks = half / V;
-    int pos = p.positions[t];
+    const int pos = p.positions[t], slot = p.n_kv > 0 ? p.slots[t] : -1;
     const bool is_q = h < p.n_q, is_v = h >= p.n_q + p.n_kv;
     bool pad = pos < 0;
     if (!pad && p.rot_dim > 0 && pos >= p.max_pos) {
@@ -229,7 +267,7 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeParams p) {
         src = static_cast<const TI*>(p.q) + t * p.q_stride + (long long)h * D;
         dst = static_cast<TO*>(p.q_out) + ((long long)t * p.n_q + h) * D;
     } else {
-        const int slot = p.slots[t], page = slot >> p.page_shift;
+        const int page = slot >> p.page_shift;
         if (slot < 0 || pad) return;
         if (page >= p.n_pages) {
             if (p.status) atomicCAS(p.status, 0, PLORA_ERR_INVALID_ARG);
@@ -245,69 +283,58 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeParams p) {
     const bool split = !INTER && c < rot_chunks;
     const int ia = split ? c * V : 2 * c * V;
     const int ib = split ? half + c * V : ia + V;
-    float a[V], b[V];
+    float x[2 * V];
     if (pad) {       // a padding token: its query row is zero, its key and value go nowhere
 #pragma unroll
-        for (int i = 0; i < V; ++i) a[i] = b[i] = 0.f;
+        for (int i = 0; i < 2 * V; ++i) x[i] = 0.f;
     } else {
-        load<TI, V>(src + ia, a);
-        load<TI, V>(src + ib, b);
+        load<TI, V, WIDE>(src, ia, ib, x);
         if (turns) {
-            float cs[2 * V];
-            const float* tab = p.table + ((long long)pos * half + c * V) * 2;
+            const Vec<float, 2 * V> cs = *reinterpret_cast<const Vec<float, 2 * V>*>(p.table + ((long long)pos * half + c * V) * 2);
 #pragma unroll
-            for (int i = 0; i < 2 * V; i += 2) {
-                const float2 w = *reinterpret_cast<const float2*>(tab + i);
-                cs[i] = w.x;
-                cs[i + 1] = w.y;
-            }
-            if (INTER) {
-                // pairs (x[2 i], x[2 i + 1]) run through a, then b
-                float x[2 * V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    x[i] = a[i];
-                    x[V + i] = b[i];
-                }
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float u = x[2 * i], w = x[2 * i + 1], co = cs[2 * i], si = cs[2 * i + 1];
-                    x[2 * i] = u * co - w * si;
-                    x[2 * i + 1] = w * co + u * si;
-                }
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    a[i] = x[i];
-                    b[i] = x[V + i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float u = a[i], w = b[i], co = cs[2 * i], si = cs[2 * i + 1];
-                    a[i] = u * co - w * si;
-                    b[i] = w * co + u * si;
-                }
+            for (int v = 0; v < V; ++v) {
+                const int ja = INTER ? 2 * v : v, jb = INTER ? 2 * v + 1 : V + v;
+                const float u = x[ja], w = x[jb], co = cs.x[2 * v], si = cs.x[2 * v + 1];
+                x[ja] = u * co - w * si;
+                x[jb] = w * co + u * si;
             }
         }
     }
-    store<TO, V>(dst + ia, a);
-    store<TO, V>(dst + ib, b);
+    store<TO, V, WIDE>(dst, ia, ib, x);
 }
 
-template <typename TI, typename TO, int V>
-void rope_go(const RopeParams& p, bool inter, cudaStream_t st) {
+// Launched so that it may start while the kernel before it drains; it waits for that kernel before it reads anything.
+cudaError_t launch(const void* kern, dim3 grid, unsigned block, cudaStream_t st, void** args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelExC(&cfg, kern, args);
+    if (e != cudaSuccess) (void)cudaGetLastError();      // reported by the caller; a later call must not find it
+    return e;
+}
+
+template <typename TI, typename TO, int V, bool WIDE>
+cudaError_t rope_go(const RopeParams& p, bool inter, cudaStream_t st) {
     const long long n = (long long)p.n_tok * p.per_tok;
+    // (an ordinary launch: waiting for the kernel before costs every CTA some hundred cycles, and these live for two thousand)
     const unsigned grid = (unsigned)((n + 255) / 256);
-    if (inter) rope_kernel<TI, TO, V, true><<<grid, 256, 0, st>>>(p);
-    else rope_kernel<TI, TO, V, false><<<grid, 256, 0, st>>>(p);
+    if (inter) rope_kernel<TI, TO, V, true, WIDE><<<grid, 256, 0, st>>>(p);
+    else rope_kernel<TI, TO, V, false, WIDE><<<grid, 256, 0, st>>>(p);
+    return cudaGetLastError();
 }
 template <typename TI, typename TO>
-void rope_go_v(const RopeParams& p, int V, bool inter, cudaStream_t st) {
+cudaError_t rope_go_v(const RopeParams& p, int V, bool wide, bool inter, cudaStream_t st) {
     switch (V) {
-        case 8: rope_go<TI, TO, 8>(p, inter, st); break;
-        case 4: rope_go<TI, TO, 4>(p, inter, st); break;
-        case 2: rope_go<TI, TO, 2>(p, inter, st); break;
-        default: rope_go<TI, TO, 1>(p, inter, st); break;
+        case 8: return wide ? rope_go<TI, TO, 8, true>(p, inter, st) : rope_go<TI, TO, 8, false>(p, inter, st);
+        case 4: return rope_go<TI, TO, 4, false>(p, inter, st);
+        case 2: return rope_go<TI, TO, 2, false>(p, inter, st);
+        default: return rope_go<TI, TO, 1, false>(p, inter, st);
     }
 }
 
@@ -340,8 +367,10 @@ extern "C" PLORA_API plora_status plora_kv_plan(const int32_t* kv_len, const int
     PlanParams p{kv_len, new_len, free_pages, cursor_in, block_table, tok_start, positions, tok_req, slots, kv_len_out, cursor_out,
                  n_req, page_size, shift_of(page_size), n_free, max_blocks, max_tokens};
     const int grid = max_tokens > 0 ? (int)(((long long)max_tokens + kPlanThreads - 1) / kPlanThreads) : 1;
-    plan_kernel<<<grid, kPlanThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return cudaGetLastError() == cudaSuccess ? PLORA_OK : PLORA_ERR_CUDA;
+    void* args[] = {&p};
+    return launch((const void*)plan_kernel, dim3((unsigned)grid), kPlanThreads, static_cast<cudaStream_t>(stream), args) == cudaSuccess
+               ? PLORA_OK
+               : PLORA_ERR_CUDA;
 }
 
 extern "C" PLORA_API plora_status plora_rope_table(const plora_rope_desc* d, int32_t max_pos, float* table, void* stream) {
@@ -406,15 +435,18 @@ extern "C" PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args* 
     p.per_head = a->head_dim / (2 * V);
     p.per_tok = p.per_head * (p.n_q + 2 * p.n_kv);
     if (((long long)p.n_tok * p.per_tok + 255) / 256 > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
+    // 32-byte accesses where the runs lie together (16 values of a 16-bit type): every base and stride has to allow them
+    const int W = 32 / (int)es;
+    const bool wide = V == 8 && p.q_stride % W == 0 && p.k_stride % W == 0 && p.v_stride % W == 0 && p.page_stride % 16 == 0 &&
+                      a->head_dim % 16 == 0 && a->rot_dim % 16 == 0 && aligned(a->q, 32) && aligned(a->k, 32) && aligned(a->v, 32) &&
+                      aligned(a->q_out, 32) && aligned(a->k_cache, 32) && aligned(a->v_cache, 32);
     const bool inter = a->layout == PLORA_ROPE_INTERLEAVED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool f32 = a->in_type == PLORA_INPUT_FP32;
-    if (a->out_type == PLORA_INPUT_BF16) {
-        if (f32) rope_go_v<float, __nv_bfloat16>(p, V, inter, st);
-        else rope_go_v<__nv_bfloat16, __nv_bfloat16>(p, V, inter, st);
-    } else {
-        if (f32) rope_go_v<float, __half>(p, V, inter, st);
-        else rope_go_v<__half, __half>(p, V, inter, st);
-    }
-    return cudaGetLastError() == cudaSuccess ? PLORA_OK : PLORA_ERR_CUDA;
+    cudaError_t e;
+    if (a->out_type == PLORA_INPUT_BF16)
+        e = f32 ? rope_go_v<float, __nv_bfloat16>(p, V, wide, inter, st) : rope_go_v<__nv_bfloat16, __nv_bfloat16>(p, V, wide, inter, st);
+    else
+        e = f32 ? rope_go_v<float, __half>(p, V, wide, inter, st) : rope_go_v<__half, __half>(p, V, wide, inter, st);
+    return e == cudaSuccess ? PLORA_OK : PLORA_ERR_CUDA;
 }
