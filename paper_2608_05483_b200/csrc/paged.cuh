@@ -81,7 +81,17 @@ struct Params {
 };
 
 constexpr int kSmallRows = 16;     // rows of a unit the mma.sync kernel takes
+constexpr int kSelfRequests = 256; // requests of single tokens that the mma.sync kernel deals out by itself
 constexpr int kBigRows = 128;      // rows of a tile of the tensor-core kernel; a unit has up to two tiles
+
+// Keys of a split of the mma.sync kernel: its items should number about kSmallItems (eight for each of two CTAs per SM).
+constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatever the device has: it sizes the workspace
+constexpr int kSmallItems = kPlanSms * 2 * 8;
+constexpr int kSmallMinKeys = 128;     // no split shorter than this
+__device__ __forceinline__ int small_chunk(long long keys, int n_kv_heads) {
+    const long long per = (keys * n_kv_heads + kSmallItems - 1) / kSmallItems;
+    return (int)min((long long)(1 << 30), max((long long)kSmallMinKeys, (per + 63) / 64 * 64));
+}
 
 // ---- PTX wrappers ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -211,7 +221,7 @@ struct Device {
 };
 
 // ---- launches -----------------------------------------------------------------------------------------
-cudaError_t launch_small(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim, bool fp16,
+cudaError_t launch_small(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim, bool fp16, bool self,
                          Device dev, cudaStream_t st);
 cudaError_t launch_big(const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim,
                        bool fp16, Device dev, cudaStream_t st);

@@ -26,9 +26,6 @@ cudaError_t launch_pdl(const void* kern, dim3 grid, dim3 block, size_t smem, cud
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatever the device has: it sizes the workspace
-constexpr int kSmallItems = kPlanSms * 2 * 8;   // aimed-at items of the small kernel (two CTAs per SM)
-constexpr int kSmallMinKeys = 128;     // no split shorter than this
 // Splits of the tensor-core kernel (one CTA per SM).  A CTA alone is slow to start (some 4 us until its first scores), so a
 // batch that gives a CTA no more than kBigOneRound keys is cut into at most one item per SM (128 of the 148: the last
 // pieces are short ones); a longer one into four per SM, which even out as they are taken from a counter.
@@ -280,8 +277,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         else keys_b += (long long)pre * ((n + TBb - 1) / TBb);
     }
     sum_all(keys_s, keys_b, red);
-    const long long per_s = (keys_s * p.n_kv_heads + kSmallItems - 1) / kSmallItems;
-    const int chunk_s = (int)min((long long)INT_MAX / 2, max((long long)kSmallMinKeys, (per_s + 63) / 64 * 64));
+    const int chunk_s = small_chunk(keys_s, p.n_kv_heads);
     long long per_b = (keys_b * p.n_kv_heads + kBigItemsOne - 1) / kBigItemsOne;
     if (per_b > kBigOneRound) per_b = max((long long)kBigOneRound, (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems);
     const int chunk_b = (int)min((long long)kBigMaxKeys, max((long long)kBigMinKeys, (per_b + 127) / 128 * 128));
@@ -650,12 +646,15 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     const bool ragged = p.tok_start != nullptr, grouped = p.n_groups > 0;
     const void* pk = ragged ? (grouped ? (const void*)plan_kernel<true, true> : (const void*)plan_kernel<true, false>)
                             : (grouped ? (const void*)plan_kernel<false, true> : (const void*)plan_kernel<false, false>);
-    if (launch_pdl(pk, dim3(1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads), dim3(kPlanThreads), 0, st, args) != cudaSuccess)
+    // Single tokens that share nothing need no plan.  (Two requests are read one by one even if they are said to share a prefix:
+    // the second then finds it in L2.)
+    const bool self = !ragged && p.G <= kSmallRows && p.n_req <= kSelfRequests && (!grouped || p.n_req <= 2);
+    if (!self && launch_pdl(pk, dim3(1 + (p.n_tok + kPlanThreads - 1) / kPlanThreads), dim3(kPlanThreads), 0, st, args) != cudaSuccess)
         return cuda_failed();
     // a small unit holds whatever fits into its rows; single tokens that share nothing always do
-    const bool big = p.G > kSmallRows || ((p.tok_start || p.n_groups > 0) && (long long)p.n_tok * p.G > kSmallRows);
+    const bool big = p.G > kSmallRows || (!self && (ragged || grouped) && (long long)p.n_tok * p.G > kSmallRows);
     if (big && launch_big(tq, tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return cuda_failed();
-    if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return cuda_failed();
+    if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, self, dev, st) != cudaSuccess) return cuda_failed();
     const void* mk = a->head_dim == 128 ? (fp16 ? (const void*)merge_kernel<128, true> : (const void*)merge_kernel<128, false>)
                                         : (fp16 ? (const void*)merge_kernel<64, true> : (const void*)merge_kernel<64, false>);
     const long long ctas = ((long long)p.n_tok * p.n_q_heads + 3) / 4;

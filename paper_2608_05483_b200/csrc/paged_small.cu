@@ -33,7 +33,7 @@ struct Cfg {
     static constexpr int kSlotBytes = (kHdrOff + 32 + 1023) / 1024 * 1024;
     static constexpr int kStages = D == 128 ? 3 : 5;
     static constexpr int kMeetPitch = D + 4;               // floats: o[D], m, l
-    static constexpr int kSmemBytes = 1024 + kStages * kSlotBytes + (2 * kStages + 1) * 8 + 16;
+    static constexpr int kSmemBytes = 1024 + kStages * kSlotBytes + (2 * kStages + 1) * 8 + 16 + 2 * kSelfRequests;
     static_assert(kConsumers * kSmallRows * kMeetPitch * 4 <= kRowOff, "the meeting place fits in a stage");
 };
 
@@ -56,7 +56,10 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int D, bool FP16, bool CAP, bool BIAS>
+// SELF: single tokens of at most kSelfRequests requests that are read one by one.  Each CTA's producer then finds its items
+// from the lengths itself, and no plan kernel runs before (5 us, as much as a short decode's reads take); CTA 0 lists the
+// tokens to merge.
+template <int D, bool FP16, bool CAP, bool BIAS, bool SELF>
 __global__ void __launch_bounds__(kThreads, 2)
 small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params p) {
     using C = Cfg<D>;
@@ -66,6 +69,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     uint8_t* bars = base + C::kStages * C::kSlotBytes;
     const uint32_t full = smem_u32(bars), empty = full + C::kStages * 8, meet = empty + C::kStages * 8;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + (2 * C::kStages + 1) * 8);
+    uint16_t* first_unit = reinterpret_cast<uint16_t*>(bars + (2 * C::kStages + 1) * 8 + 16);    // SELF: of every request
     const WaitCtl wc{abort_flag, p.header};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -81,7 +85,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     grid_launch_dependents();
     if (tid == 0) abort_flag[1] = p.header[kHookWord] == PLORA_HOOK_WITHHOLD_RELEASE;   // test hook: warp 0 never hands a stage back
     __syncthreads();
-    const int n_items = p.header[kSmallUnitsWord] * p.n_kv_heads;
+    int n_items = SELF ? 0 : p.header[kSmallUnitsWord] * p.n_kv_heads;
     const unsigned all = 0xffffffffu;
 
     if (warp == kConsumers) {
@@ -89,24 +93,87 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         const int bp = min(p.page_size, kTile);     // tokens of a box
         uint32_t it = 0;
         bool stopped = false;
-        int next = 0;
-        if (lane == 0) next = atomicAdd(p.header + kSmallNextWord, 1);
+        int next = 0, chunk = 0;
+        auto keys_of = [&](int r, int& lo, int& hi) {
+            const int kv = min(max(p.kv_len[r], 0), p.max_kv);
+            lo = p.key_lo ? max(p.key_lo[r], 0) : 0;
+            hi = max(lo, p.key_hi ? min(p.key_hi[r], kv) : kv);
+            return kv;
+        };
+        if (SELF) {
+            constexpr int kPer = kSelfRequests / 32;
+            int len[kPer];
+            long long keys = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = i * 32 + lane;
+                len[i] = 0;
+                if (r < p.n_req) {
+                    int lo, hi;
+                    keys_of(r, lo, hi);
+                    len[i] = hi - lo;
+                }
+                keys += len[i];
+            }
+            for (int d = 16; d > 0; d >>= 1) keys += __shfl_xor_sync(all, keys, d);
+            chunk = small_chunk(keys, p.n_kv_heads);
+            int before = 0, listed = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int r = i * 32 + lane, n = (len[i] + chunk - 1) / chunk;
+                int sum = n;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int v = __shfl_up_sync(all, sum, d);
+                    if (lane >= d) sum += v;
+                }
+                const int first = before + sum - n;
+                if (r < kSelfRequests) first_unit[r] = (uint16_t)first;
+                before += __shfl_sync(all, sum, 31);
+                if (blockIdx.x == 0) {      // (the partial results of a request are numbered as its units)
+                    const unsigned merges = __ballot_sync(all, r < p.n_req && n != 1);
+                    if (r < p.n_req && n != 1)
+                        p.tok_merge[listed + __popc(merges & ((1u << lane) - 1u))] = TokMerge{r, {first, 0}, {n, 0}, {1, 0}, 0};
+                    listed += __popc(merges);
+                }
+            }
+            n_items = before * p.n_kv_heads;
+            if (blockIdx.x == 0 && lane == 0) p.header[kMergeWord] = listed;
+            __syncwarp();
+            next = blockIdx.x;
+        } else if (lane == 0) {
+            next = atomicAdd(p.header + kSmallNextWord, 1);
+        }
         while (!stopped) {
             const int item = __shfl_sync(all, next, 0);
             if (item >= n_items) break;
-            if (lane == 0) next = atomicAdd(p.header + kSmallNextWord, 1);
+            if (SELF) next += gridDim.x;
+            else if (lane == 0) next = atomicAdd(p.header + kSmallNextWord, 1);
             const int un = item / p.n_kv_heads, head = item - un * p.n_kv_heads;
-            const Unit u = p.small_units[un];
+            Unit u;
+            TokInfo ti{0, 0, 0, 0};
+            if (SELF) {
+                int r = 0;                      // the last request whose first unit is not behind un (of empty ones: the next)
+                for (int step = kSelfRequests / 2; step > 0; step >>= 1)
+                    if (r + step < p.n_req && first_unit[r + step] <= un) r += step;
+                int lo, hi;
+                const int kv = keys_of(r, lo, hi), i = un - first_unit[r];
+                u = Unit{r, 1, r, lo + i * chunk, min(hi, lo + (i + 1) * chunk), hi - lo > chunk ? un : -1, {0, 0}};
+                ti = TokInfo{lo, hi, kv - 1, 0};
+            } else {
+                u = p.small_units[un];
+            }
             const int rows = u.ntok * p.G;
             // this lane's row: what it may see, and where its query lies
-            TokInfo ti{0, 0, 0, 0};
             float slope = 0.f;
             const uint16_t* qsrc = nullptr;
             if (lane < rows) {
                 const int t = u.tok0 + lane / p.G, hq = head * p.G + lane % p.G;
-                ti = p.tok_info[t];
+                if (!SELF) ti = p.tok_info[t];
                 if (BIAS) slope = p.slopes[hq] * 1.4426950408889634f;
                 qsrc = p.q + t * p.q_stride + (size_t)hq * D;
+            } else {
+                ti.lo = ti.hi = 0;
             }
             ti.lo = max(ti.lo, u.k0);
             ti.hi = min(ti.hi, u.k1);
@@ -344,9 +411,9 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     }
 }
 
-template <int D, bool FP16, bool CAP, bool BIAS>
+template <int D, bool FP16, bool CAP, bool BIAS, bool SELF>
 cudaError_t go(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, Device dev, cudaStream_t st) {
-    auto kern = small_kernel<D, FP16, CAP, BIAS>;
+    auto kern = small_kernel<D, FP16, CAP, BIAS, SELF>;
     static Configured configured;
     const cudaError_t e = configured.ensure(reinterpret_cast<const void*>(kern), Cfg<D>::kSmemBytes, dev.id);
     if (e != cudaSuccess) return e;
@@ -355,18 +422,23 @@ cudaError_t go(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p
     void* args[] = {const_cast<CUtensorMap*>(&tm_k), const_cast<CUtensorMap*>(&tm_v), const_cast<Params*>(&p)};
     return launch_pdl(reinterpret_cast<const void*>(kern), dim3(grid), dim3(kThreads), Cfg<D>::kSmemBytes, st, args);
 }
-template <int D, bool FP16>
+template <int D, bool FP16, bool SELF>
 cudaError_t go2(const CUtensorMap& k, const CUtensorMap& v, const Params& p, Device dev, cudaStream_t st) {
-    if (p.cap_log2e > 0.f) return p.slopes ? go<D, FP16, true, true>(k, v, p, dev, st) : go<D, FP16, true, false>(k, v, p, dev, st);
-    return p.slopes ? go<D, FP16, false, true>(k, v, p, dev, st) : go<D, FP16, false, false>(k, v, p, dev, st);
+    if (p.cap_log2e > 0.f)
+        return p.slopes ? go<D, FP16, true, true, SELF>(k, v, p, dev, st) : go<D, FP16, true, false, SELF>(k, v, p, dev, st);
+    return p.slopes ? go<D, FP16, false, true, SELF>(k, v, p, dev, st) : go<D, FP16, false, false, SELF>(k, v, p, dev, st);
+}
+template <int D, bool FP16>
+cudaError_t go3(const CUtensorMap& k, const CUtensorMap& v, const Params& p, bool self, Device dev, cudaStream_t st) {
+    return self ? go2<D, FP16, true>(k, v, p, dev, st) : go2<D, FP16, false>(k, v, p, dev, st);
 }
 
 }  // namespace
 
-cudaError_t launch_small(const CUtensorMap& k, const CUtensorMap& v, const Params& p, int head_dim, bool fp16, Device dev,
+cudaError_t launch_small(const CUtensorMap& k, const CUtensorMap& v, const Params& p, int head_dim, bool fp16, bool self, Device dev,
                          cudaStream_t st) {
-    if (head_dim == 128) return fp16 ? go2<128, true>(k, v, p, dev, st) : go2<128, false>(k, v, p, dev, st);
-    return fp16 ? go2<64, true>(k, v, p, dev, st) : go2<64, false>(k, v, p, dev, st);
+    if (head_dim == 128) return fp16 ? go3<128, true>(k, v, p, self, dev, st) : go3<128, false>(k, v, p, self, dev, st);
+    return fp16 ? go3<64, true>(k, v, p, self, dev, st) : go3<64, false>(k, v, p, self, dev, st);
 }
 
 }  // namespace paged
