@@ -537,7 +537,8 @@ PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args *args, void 
  *            second product.
  * q [n_tok][n_q_heads][head_dim] (q_stride elements between tokens, 0: packed), out packed; query head h reads KV
  * head h / (n_q_heads / n_kv_heads).  head_dim 64 or 128; page_size 16, 32, 64 or 128; at most 128 query heads per KV
- * head.  q, K, V and out 16-byte aligned, strides multiples of 8.  Cache slots at or beyond kv_len may hold anything.
+ * head.  q, K, V and out 16-byte aligned, strides multiples of 8.  Cache slots at or beyond kv_len may hold anything; below
+ * it K and V have to be finite, masked or not (a masked value still meets a weight of zero).
  * A block table entry outside [0, n_pages) that is needed reads as zeros and sets PLORA_ERR_INVALID_ARG in the status word.
  * workspace  256-byte aligned, at least plora_attn_paged_workspace_bytes(...) bytes (max_blocks there: min(max_blocks,
  *            n_pages)); first 256 bytes zero before the first call, scratch between calls, one stream at a time; the

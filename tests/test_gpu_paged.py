@@ -532,3 +532,15 @@ def test_attention_refusals():
         P.attn_paged(b.q, small, small.clone(), b.table, b.kv_len, 0.1, tok_start=b.tok_start)
     assert e.value.status == P.ERR_UNSUPPORTED
     torch.cuda.synchronize()
+
+
+def test_the_example_serves_requests_of_several_adapters():
+    """examples/serve_layer.py: plan, deltas, rotary positions, cache, prompt and grouped single-token attention together."""
+    import importlib.util
+    from pathlib import Path
+    path = Path(__file__).resolve().parent.parent / "examples" / "serve_layer.py"
+    spec = importlib.util.spec_from_file_location("serve_layer", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    # bf16 base products, q, K, V, weights and output, each rounded at 2^-8, behind one another, against 64 bits throughout
+    assert mod.main(steps=5) <= 6 * 2.0 ** -8
