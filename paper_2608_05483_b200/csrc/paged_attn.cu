@@ -418,58 +418,64 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     }
 }
 
-// One warp per (listed token, query head): the token's partial results, rescaled by their maxima.
+// A row is a listed token's query head; D / 4 lanes share it, four dims each.  A lane looks at one partial result's maximum
+// and sum, all at once (D / 4 at a time); then the outputs are added up.  Short chains of dependent loads on many rows: what
+// counts is the rows under way.
 template <int D, bool FP16>
 __global__ void __launch_bounds__(128) merge_kernel(const Params p) {
     grid_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31;
+    constexpr int L = D / 4;
+    const unsigned all = 0xffffffffu;
+    const int sub = threadIdx.x % L;
     const long long rows = (long long)p.header[kMergeWord] * p.n_q_heads;
-    for (long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); row < rows; row += (long long)gridDim.x * 4) {
-        const int hq = (int)(row % p.n_q_heads);
-        const TokMerge tm = p.tok_merge[row / p.n_q_heads];
-        constexpr int V = D / 32;
-        // A lane looks at one partial result's maximum and sum, all at once (32 at a time); then the outputs are added up.
-        float o[V], M = -INFINITY, L = 0.f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) o[v] = 0.f;
-        const int n = tm.n[0] + tm.n[1];
-        for (int i0 = 0; i0 < n; i0 += 32) {
-            const int i = i0 + lane;
-            const bool own = i < tm.n[0];
-            size_t at = 0;
+    const long long step = (long long)gridDim.x * (128 / L);
+    // (lanes of a warp leave together: the trip count is the warp's first row's)
+    for (long long row = (long long)blockIdx.x * (128 / L) + threadIdx.x / L; row - threadIdx.x % 32 / L < rows; row += step) {
+        const bool live = row < rows;
+        TokMerge tm{0, {0, 0}, {0, 0}, {0, 0}, 0};
+        int hq = 0;
+        if (live) {
+            hq = (int)(row % p.n_q_heads);
+            tm = p.tok_merge[row / p.n_q_heads];
+        }
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float M = -INFINITY, sum = 0.f;
+        const int n = tm.n[0] + tm.n[1], n_warp = __reduce_max_sync(all, n);
+        for (int i0 = 0; i0 < n_warp; i0 += L) {
+            const int i = i0 + sub;
+            int at = 0;
             float2 ml = make_float2(-INFINITY, 0.f);
             if (i < n) {
-                at = (size_t)(own ? tm.base[0] + i * tm.stride[0] : tm.base[1] + (i - tm.n[0]) * tm.stride[1]) * p.n_q_heads + hq;
-                ml = p.part_ml[at];
+                at = i < tm.n[0] ? tm.base[0] + i * tm.stride[0] : tm.base[1] + (i - tm.n[0]) * tm.stride[1];
+                ml = p.part_ml[(size_t)at * p.n_q_heads + hq];
             }
             float m = ml.x;
-            for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+#pragma unroll
+            for (int d = L / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(all, m, d));
             const float Mn = fmaxf(M, m), Me = Mn == -INFINITY ? 0.f : Mn, back = ex2(M - Me), f = ex2(ml.x - Me);
             float l = f * ml.y;
-            for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-            L = L * back + l;
-            M = Mn;
 #pragma unroll
-            for (int v = 0; v < V; ++v) o[v] *= back;
-            const int here = min(32, n - i0);
+            for (int d = L / 2; d > 0; d >>= 1) l += __shfl_xor_sync(all, l, d);
+            sum = sum * back + l;
+            M = Mn;
+            o.x *= back; o.y *= back; o.z *= back; o.w *= back;
+            const int here = min(L, n_warp - i0);
 #pragma unroll 4
             for (int k = 0; k < here; ++k) {
-                const float fk = __shfl_sync(0xffffffffu, f, k);
-                const size_t ak = __shfl_sync(0xffffffffu, (unsigned long long)at, k);
-                const float* src = p.part_o + ak * D + lane * V;
-#pragma unroll
-                for (int v = 0; v < V; v += 2) {
-                    const float2 x = *reinterpret_cast<const float2*>(src + v);
-                    o[v] = fmaf(fk, x.x, o[v]);
-                    o[v + 1] = fmaf(fk, x.y, o[v + 1]);
+                const float fk = __shfl_sync(all, f, k, L);
+                const int ak = __shfl_sync(all, at, k, L);
+                if (i0 + k < n) {
+                    const float4 x = *reinterpret_cast<const float4*>(p.part_o + ((size_t)ak * p.n_q_heads + hq) * D + sub * 4);
+                    o.x = fmaf(fk, x.x, o.x); o.y = fmaf(fk, x.y, o.y); o.z = fmaf(fk, x.z, o.z); o.w = fmaf(fk, x.w, o.w);
                 }
             }
         }
-        const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);    // nothing visible: a zero row
-        uint16_t* dst = p.out + ((size_t)tm.tok * p.n_q_heads + hq) * D + lane * V;
-#pragma unroll
-        for (int v = 0; v < V; v += 2) *reinterpret_cast<uint32_t*>(dst + v) = pack16<FP16>(o[v] * inv, o[v + 1] * inv);
+        if (live) {
+            const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);    // nothing visible: a zero row
+            *reinterpret_cast<uint2*>(p.out + ((size_t)tm.tok * p.n_q_heads + hq) * D + sub * 4) =
+                make_uint2(pack16<FP16>(o.x * inv, o.y * inv), pack16<FP16>(o.z * inv, o.w * inv));
+        }
     }
 }
 
@@ -657,7 +663,8 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, self, dev, st) != cudaSuccess) return cuda_failed();
     const void* mk = a->head_dim == 128 ? (fp16 ? (const void*)merge_kernel<128, true> : (const void*)merge_kernel<128, false>)
                                         : (fp16 ? (const void*)merge_kernel<64, true> : (const void*)merge_kernel<64, false>);
-    const long long ctas = ((long long)p.n_tok * p.n_q_heads + 3) / 4;
+    const int at_once = 128 / (a->head_dim / 4);
+    const long long ctas = ((long long)p.n_tok * p.n_q_heads + at_once - 1) / at_once;
     const int most = dev.sms * 16;
     if (launch_pdl(mk, dim3((unsigned)(ctas < most ? ctas : most)), dim3(128), 0, st, args) != cudaSuccess) return cuda_failed();
     return PLORA_OK;
