@@ -295,8 +295,9 @@ __global__ void __launch_bounds__(256, 8) rope_kernel(const RopeParams p) {
             for (int v = 0; v < V; ++v) {
                 const int ja = INTER ? 2 * v : v, jb = INTER ? 2 * v + 1 : V + v;
                 const float u = x[ja], w = x[jb], co = cs.x[2 * v], si = cs.x[2 * v + 1];
-                x[ja] = u * co - w * si;
-                x[jb] = w * co + u * si;
+                // (written out, so that every variant of the kernel rounds alike)
+                x[ja] = __fmaf_rn(u, co, -__fmul_rn(w, si));
+                x[jb] = __fmaf_rn(w, co, __fmul_rn(u, si));
             }
         }
     }
