@@ -15,10 +15,13 @@
 // accumulator in tensor memory is hardly ever touched between the products.
 // P is rounded to the input type for the second product; l sums the unrounded weights in fp32.
 //
-// A tile's step is: scores (512 cycles of the tensor pipe at D = 128), softmax, O += P V (512).  The special-function unit
-// alone would take 1024 cycles for a tile's 16384 exponentials, so part of them is computed on the FMA pipe
-// (2^x = 2^n p(f), n the nearest integer, p a polynomial of degree 4 fitted on [-1/2, 1/2], relative error 2.6e-6), and
-// the second product starts on the first half of the keys while the weights of the second half are still being made.
+// A tile's step is: scores (512 cycles of the tensor pipe at D = 128), softmax, O += P V (512).  Measured by the clock inside the
+// kernel on 16 prompts of 2048 to 4096 tokens: the two tiles' steps take 3700 cycles together, 2050 of them with the tensor
+// pipe busy (46 %; 0.9 PFLOP/s at the 1.7 GHz the part holds under it, 1.09 ms; 1.25 ms once the power limit sets in).  A
+// step is a chain, softmax (2000) - hand-over (250) - products (1350) - hand-over (250), and tensor memory holds the scores
+// of two tiles, so at most two chains run.  What the instructions cost hardly shows: a third of the exponentials on the FMA
+// pipe, two threads to a row, an MMA warp per tile, 64 keys with two sets of scores per tile all took as long or longer.
+// What did show is code size (instruction fetch bounds five roles that run different code): hence the rolled loops below.
 #include <limits.h>
 
 #include "paged.cuh"
@@ -32,8 +35,6 @@ constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kKeyWarp = 9, kTailWarp = 10, kIt
 constexpr int kThreads = 16 * 32;       // four warpgroups (the last three warps only give their registers away)
 constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;       // of 128 a thread at launch: 2 * 184 + 2 * 72 = 4 * 128
 constexpr int kSched = 2;
-// Of 16 pairs of weights, how many are computed on the FMA pipe (which the cap's polynomial keeps busy already).
-constexpr int kEmulated = 6, kEmulatedCap = 2;
 constexpr float kLazy = 8.f;        // base-2 logarithm of the growth a row's maximum may have before O is rescaled
 
 template <int D>
@@ -473,22 +474,6 @@ __device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int l
     }
 }
 
-// 2^x on the FMA pipe, for x <= some ten: nearest integer by the addition of 1.5 * 2^23, whose low mantissa bits then hold it
-__device__ __forceinline__ float2 ex2_fma(float2 x) {
-    // (the maximum that hands a NaN on: a NaN among visible scores must not come out as a finite result)
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
-    const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f), one = make_float2(-1.f, -1.f);
-    const float2 t = __fadd2_rn(x, magic);
-    const float2 f = __ffma2_rn(__fadd2_rn(t, minus), one, x);
-    float2 q = __ffma2_rn(f, make_float2(0.009570102207362652f, 0.009570102207362652f), make_float2(0.05591785907745361f, 0.05591785907745361f));
-    q = __ffma2_rn(q, f, make_float2(0.240247443318367f, 0.240247443318367f));
-    q = __ffma2_rn(q, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
-    q = __ffma2_rn(q, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-    return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(t.x) << 23)),
-                       __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(t.y) << 23)));
-}
-
 // 32 raw products of a row -> scores in the base-2 domain (cap, bias by distance); dist0: distance of the first one's key.
 // Below |x| = 3/4 the cap's tanh(x) is x P(x^2) on the FMA pipe, P of degree 4 fitted for the least absolute error (1.9e-7; it
 // is multiplied by the cap), its coefficients scaled so that it takes the raw product: s (d0 + s^2 (d1 + ...)).  A warp that
@@ -564,32 +549,40 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
             tc_fence_after();
             // The row is read twice from tensor memory, 32 columns at a time, rather than held in 128 registers: the room is
             // worth more to the scheduler of the second pass.  What the first pass changes it writes back.
-            uint32_t buf[32];
-            float* s = reinterpret_cast<float*>(buf);
+            uint32_t buf[2][32];                 // (one is loaded while the other is worked on)
             const float mul = CAP || BIAS ? 1.f : p.scale_log2e;
             const bool mask = __any_sync(all, lo > key || hi < key + kTileKeys), changed = CAP || BIAS || mask;
             float mx[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) mx[i] = -INFINITY;
+            tmem_ld32(ts, buf[0]);
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                tmem_ld32(ts + c * 32, buf);
-                tmem_ld_wait();
-                if (CAP || BIAS) scores_of<CAP, BIAS>(p, s, slope, (float)(pos - key - c * 32));
-                if (mask) {
-                    const int a = min(max(lo - key - c * 32, 0), 32), b = min(max(hi - key - c * 32, 0), 32);
-                    // bits [a, b) of the 32 (a shift by 32 gives 0)
-                    const uint32_t see = a < b ? __funnelshift_lc(0u, 0xffffffffu, a) & ~__funnelshift_lc(0u, 0xffffffffu, b) : 0u;
+            for (int c2 = 0; c2 < 4; c2 += 2)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) s[i] = see & (1u << i) ? s[i] : -INFINITY;
+                for (int h = 0; h < 2; ++h) {
+                    const int c = c2 + h;
+                    float* s = reinterpret_cast<float*>(buf[h]);
+                    tmem_ld_wait();
+                    tmem_ld32(ts + ((c + 1) & 3) * 32, buf[h ^ 1]);        // (after the last one the first, for the second pass)
+                    if (CAP || BIAS) scores_of<CAP, BIAS>(p, s, slope, (float)(pos - key - c * 32));
+                    if (mask) {
+                        const int a = min(max(lo - key - c * 32, 0), 32), b = min(max(hi - key - c * 32, 0), 32);
+                        // bits [a, b) of the 32 (a shift by 32 gives 0)
+                        const uint32_t see = a < b ? __funnelshift_lc(0u, 0xffffffffu, a) & ~__funnelshift_lc(0u, 0xffffffffu, b) : 0u;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) s[i] = see & (1u << i) ? s[i] : -INFINITY;
+                    }
+                    if (changed) tmem_st32(ts + c * 32, buf[h]);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 16)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) mx[e] = fmaxf(fmaxf(mx[e], s[i + e]), s[i + 8 + e]);
                 }
-                if (changed) tmem_st32(ts + c * 32, buf);
-#pragma unroll
-                for (int i = 0; i < 32; i += 16)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) mx[e] = fmaxf(fmaxf(mx[e], s[i + e]), s[i + 8 + e]);
+            if (changed) {
+                tmem_ld_wait();
+                tmem_st_wait();
+                tmem_ld32(ts, buf[0]);
             }
-            if (changed) tmem_st_wait();
             const float tile_max = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * mul;
             if (j == first) {
                 m = tile_max;
@@ -613,26 +606,27 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
             float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             const float2 mul2 = make_float2(mul, mul), me2 = make_float2(-me, -me);
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                tmem_ld32(ts + c * 32, buf);
-                tmem_ld_wait();
-                uint32_t w[16];
+            for (int c2 = 0; c2 < 4; c2 += 2) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float2 x = __ffma2_rn(make_float2(s[2 * i], s[2 * i + 1]), mul2, me2);
-                    constexpr int kFma = CAP ? kEmulatedCap : kEmulated;       // (spread evenly)
-                    const bool emulate = (i * kFma) % 16 < kFma;
-                    const float2 e = emulate ? ex2_fma(x) : make_float2(ex2(x.x), ex2(x.y));
-                    sum[i & 3] = __fadd2_rn(sum[i & 3], e);
-                    w[i] = pack16<FP16>(e.x, e.y);
+                for (int h = 0; h < 2; ++h) {
+                    const float* s = reinterpret_cast<const float*>(buf[h]);
+                    tmem_ld_wait();
+                    if (h == 0) tmem_ld32(ts + (c2 + 1) * 32, buf[1]);
+                    else if (c2 == 0) tmem_ld32(ts + 64, buf[0]);
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 x = __ffma2_rn(make_float2(s[2 * i], s[2 * i + 1]), mul2, me2);
+                        const float2 e = make_float2(ex2(x.x), ex2(x.y));
+                        sum[i & 3] = __fadd2_rn(sum[i & 3], e);
+                        w[i] = pack16<FP16>(e.x, e.y);
+                    }
+                    tmem_st16(ts + (c2 + h) * 16, w);
                 }
-                tmem_st16(ts + c * 16, w);
-                if (c & 1) {                              // half of the keys: the second product may start
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(sm.p_ready + t * 16 + (c >> 1) * 8);
-                }
+                tmem_st_wait();                           // half of the keys: the second product may start
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sm.p_ready + t * 16 + (c2 >> 1) * 8);
             }
             const float2 all2 = __fadd2_rn(__fadd2_rn(sum[0], sum[1]), __fadd2_rn(sum[2], sum[3]));
             l += all2.x + all2.y;
