@@ -58,6 +58,7 @@ struct Params {
     float2* part_ml;          // [partial token][query head] {m, l}
     float* part_o;            // [partial token][query head][D]
     int32_t cap_small, cap_big, cap_part;
+    int32_t after_big;        // the mma.sync kernel runs behind the tensor-core kernel of the same call
     int32_t big_tile_tok;     // query tokens in a 128-row tile of the tensor-core kernel
 
     const uint16_t* q;

@@ -659,6 +659,7 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
         return cuda_failed();
     // a small unit holds whatever fits into its rows; single tokens that share nothing always do
     const bool big = p.G > kSmallRows || (!self && (ragged || grouped) && (long long)p.n_tok * p.G > kSmallRows);
+    p.after_big = big;
     if (big && launch_big(tq, tm[0], tm[1], p, a->head_dim, fp16, dev, st) != cudaSuccess) return cuda_failed();
     if (p.G <= kSmallRows && launch_small(tm[0], tm[1], p, a->head_dim, fp16, self, dev, st) != cudaSuccess) return cuda_failed();
     const void* mk = a->head_dim == 128 ? (fp16 ? (const void*)merge_kernel<128, true> : (const void*)merge_kernel<128, false>)

@@ -81,11 +81,15 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         abort_flag[0] = 0;
         mbar_init_fence();
     }
-    grid_wait();                 // the units come from the plan kernel
+    // The units come from the plan kernel.  Behind the tensor-core kernel of the same call the plan is complete when this kernel
+    // starts (that kernel waits for it before it lets this one start), and the two have nothing to do with each other: this one
+    // takes the SMs that the other leaves, and waits for it only when it is done, so that its end is the end of both.  What the
+    // plan wrote is read from L2 throughout, for no wait has passed over this SM's L1.
+    if (!p.after_big) grid_wait();
     grid_launch_dependents();
-    if (tid == 0) abort_flag[1] = p.header[kHookWord] == PLORA_HOOK_WITHHOLD_RELEASE;   // test hook: warp 0 never hands a stage back
+    if (tid == 0) abort_flag[1] = __ldcg(p.header + kHookWord) == PLORA_HOOK_WITHHOLD_RELEASE;   // test hook: warp 0 never hands a stage back
     __syncthreads();
-    int n_items = SELF ? 0 : p.header[kSmallUnitsWord] * p.n_kv_heads;
+    int n_items = SELF ? 0 : __ldcg(p.header + kSmallUnitsWord) * p.n_kv_heads;
     const unsigned all = 0xffffffffu;
 
     if (warp == kConsumers) {
@@ -161,7 +165,8 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 u = Unit{r, 1, r, lo + i * chunk, min(hi, lo + (i + 1) * chunk), hi - lo > chunk ? un : -1, {0, 0}};
                 ti = TokInfo{lo, hi, kv - 1, 0};
             } else {
-                u = p.small_units[un];
+                const int4 a = __ldcg(reinterpret_cast<const int4*>(p.small_units + un)), b = __ldcg(reinterpret_cast<const int4*>(p.small_units + un) + 1);
+                u = Unit{a.x, a.y, a.z, a.w, b.x, b.y, {0, 0}};
             }
             const int rows = u.ntok * p.G;
             // this lane's row: what it may see, and where its query lies
@@ -169,8 +174,11 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             const uint16_t* qsrc = nullptr;
             if (lane < rows) {
                 const int t = u.tok0 + lane / p.G, hq = head * p.G + lane % p.G;
-                if (!SELF) ti = p.tok_info[t];
-                if (BIAS) slope = p.slopes[hq] * 1.4426950408889634f;
+                if (!SELF) {
+                    const int4 a = __ldcg(reinterpret_cast<const int4*>(p.tok_info + t));
+                    ti = TokInfo{a.x, a.y, a.z, 0};
+                }
+                if (BIAS) slope = __ldcg(p.slopes + hq) * 1.4426950408889634f;
                 qsrc = p.q + t * p.q_stride + (size_t)hq * D;
             } else {
                 ti.lo = ti.hi = 0;
@@ -186,7 +194,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 int page = 0;
                 const int my_key = key + lane * bp;
                 if (lane < nb) {
-                    page = table[my_key >> p.page_shift];
+                    page = __ldcg(table + (my_key >> p.page_shift));
                     if ((unsigned)page >= (unsigned)p.n_pages) {   // such a page reads as zeros
                         atomicCAS(p.header, 0, PLORA_ERR_INVALID_ARG);
                         page = p.n_pages;
@@ -236,6 +244,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             }
         }
         __syncwarp();
+        if (p.after_big) grid_wait();
         return;
     }
 
