@@ -261,7 +261,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
                 block_keys(q, 0, TBs, k0, k1);
                 keys_s += k1 - k0;
             }
-        } else if (p.key_hi || q.kv < q.n + q.pre) {
+        } else if (p.key_hi) {           // every block may see all of the request's keys
+            keys_b += (long long)((q.n + TBb - 1) / TBb) * max(0, q.kv - q.pre);
+        } else if (q.kv < q.n + q.pre) {
             for (int b = 0; b * TBb < q.n; ++b) {
                 block_keys(q, b, TBb, k0, k1);
                 keys_b += k1 - k0;
@@ -330,6 +332,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         if (!small && q.kv - q.pre <= chunk && q.kv >= q.n + q.pre && !p.key_hi) {
             want.big = nb;                          // no block is split, and each has a key
             want.part = q.pre > 0 ? q.n : 0;
+        } else if (!small && p.key_hi) {
+            const int splits = splits_of(max(0, q.kv - q.pre), false);
+            want.big = nb * splits;
+            want.part = splits > 1 || q.pre > 0 ? splits * q.n : 0;
         } else {
             for (int b = 0; b < nb; ++b) {
                 int k0, k1;
@@ -342,6 +348,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         const Sums at = carry + scan_exclusive(want, total, warp_sums);
         const bool room = fits(at, want);
         if (!room) atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
+        // lists a token for the merge: `splits` partial results of its own keys from `part` on, `stride` apart, and its prefix's
+        auto list = [&](int tok, int at, int part, int splits, int stride, int pre_keys) {
+            const int4 pre = pre_keys > 0 ? p.tok_prefix[tok] : make_int4(0, 0, 0, 0);
+            if (at < p.n_tok) p.tok_merge[at] = TokMerge{tok, {part, pre.x}, {splits, pre.y}, {stride, pre.z}, 0};
+        };
         // writes the units of one block, and lists its tokens if they need a merge
         auto write_block = [&](const Req& q, int r, int b, bool small, int splits, int k0, int k1, int unit, int part) {
             const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b, nt = min(TB, q.n - b * TB);
@@ -351,11 +362,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
                                           direct ? -1 : part + i * nt, {0, 0}});
             if (direct) return;
             const int m0 = atomicAdd(&s_merge, nt);      // (in any order: every token's result is its own)
-            for (int t = 0; t < nt; ++t) {
-                const int tok = q.tok0 + b * TB + t;
-                const int4 pre = q.pre > 0 ? p.tok_prefix[tok] : make_int4(0, 0, 0, 0);
-                if (m0 + t < p.n_tok) p.tok_merge[m0 + t] = TokMerge{tok, {part + t, pre.x}, {splits, pre.y}, {nt, pre.z}, 0};
-            }
+            for (int t = 0; t < nt; ++t) list(q.tok0 + b * TB + t, m0 + t, part + t, splits, nt, q.pre);
         };
         int slot = kLargeCache;
         if (RAGGED) {
@@ -401,7 +408,22 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
                         sp += c;
                     }
                 }
-                if (b >= 0) write_block(big.q, big.r, b, false, splits, k0, k1, unit + su - splits, part + sp - parts);
+                // a block that its unit finishes is a lane's work; one with tokens to list is the warp's
+                const int my_unit = unit + su - splits, my_part = part + sp - parts;
+                const bool direct = splits == 1 && big.q.pre == 0;
+                if (b >= 0 && direct) write_block(big.q, big.r, b, false, splits, k0, k1, my_unit, my_part);
+                for (unsigned left = __ballot_sync(0xffffffffu, b >= 0 && !direct); left; left &= left - 1) {
+                    const int from = __ffs(left) - 1;
+                    const int bb = b0 - from, n = __shfl_sync(0xffffffffu, splits, from), u0 = __shfl_sync(0xffffffffu, my_unit, from);
+                    const int p0 = __shfl_sync(0xffffffffu, my_part, from), a0 = __shfl_sync(0xffffffffu, k0, from);
+                    const int a1 = __shfl_sync(0xffffffffu, k1, from), tok0 = big.q.tok0 + bb * TBb, nt = min(TBb, big.q.n - bb * TBb);
+                    for (int i = lane; i < n; i += 32)
+                        put(false, u0 + i, Unit{tok0, nt, big.r, a0 + i * chunk_b, min(a1, a0 + (i + 1) * chunk_b), p0 + i * nt, {0, 0}});
+                    int m0 = 0;
+                    if (lane == 0) m0 = atomicAdd(&s_merge, nt);
+                    m0 = __shfl_sync(0xffffffffu, m0, 0);
+                    for (int t = lane; t < nt; t += 32) list(tok0 + t, m0 + t, p0 + t, n, nt, big.q.pre);
+                }
                 unit += __shfl_sync(0xffffffffu, su, 31);
                 part += __shfl_sync(0xffffffffu, sp, 31);
             }
