@@ -540,6 +540,9 @@ PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args *args, void 
  * head.  q, K, V and out 16-byte aligned, strides multiples of 8.  Cache slots at or beyond kv_len may hold anything; below
  * it K and V have to be finite, masked or not (a masked value still meets a weight of zero).
  * A block table entry outside [0, n_pages) that is needed reads as zeros and sets PLORA_ERR_INVALID_ARG in the status word.
+ * Batches with more than 16 query rows per KV head and unit (prompts, groups) run a kernel whose CTAs each take all 512
+ * tensor-memory columns of their SM; as with plora_lora_delta's tensor-core path, do not run it beside a kernel that holds
+ * tensor memory for its whole lifetime and itself waits for this call.
  * workspace  256-byte aligned, at least plora_attn_paged_workspace_bytes(...) bytes (max_blocks there: min(max_blocks,
  *            n_pages)); first 256 bytes zero before the first call, scratch between calls, one stream at a time; the
  *            status word and diagnostics are those of plora_attn_decode (plora_attn_status, plora_attn_set_debug). */

@@ -28,9 +28,9 @@ namespace {
 constexpr int kPlanThreads = 1024;
 // Splits of the tensor-core kernel (one CTA per SM).  A CTA alone is slow to start (some 4 us until its first scores), so a
 // batch that gives a CTA no more than kBigOneRound keys is cut into at most one item per SM (128 of the 148: the last
-// pieces are short ones); a longer one into four per SM, which even out as they are taken from a counter.
-// (64 requests in groups: 43 us with pieces of 512 keys, two rounds; 16 to 8192 prompt tokens behind caches: fewer and
-// longer pieces, or the merge costs what the balance gains.)
+// pieces are short ones); a longer one into eight per SM, which even out as they are taken from a counter.  (256 requests
+// behind one prefix: 394 us with pieces of 512 keys in two rounds, 382 with one of 1024; 24 chunks behind long caches: 360
+// with eight per SM, 410 with four.)
 constexpr int kBigItemsOne = 128, kBigItems = kPlanSms * 8;
 constexpr int kBigMinKeys = 256, kBigOneRound = 2048, kBigMaxKeys = 1 << 22;     // (tiles of keys are counted in 16 bits)
 constexpr int kGroupCache = 2048;      // group starts held in shared memory
@@ -524,7 +524,7 @@ int tile_tokens(int G) { return kBigRows / G; }
 // kind, so the units are at most one per block plus that many / heads; blocks that are split make at most twice that many.
 Caps caps(long long n_tok, long long n_req, long long max_kv, int n_kv_heads, int G) {
     const long long TBs = kSmallRows / G > 0 ? kSmallRows / G : 1, TBb = 2 * tile_tokens(G);
-    const long long extra_s = (kSmallItems + n_kv_heads - 1) / n_kv_heads, extra_b = (kBigItems + n_kv_heads - 1) / n_kv_heads;   // (kBigItems > kBigItemsOne)
+    const long long extra_s = (kSmallItems + n_kv_heads - 1) / n_kv_heads, extra_b = (kBigItems + n_kv_heads - 1) / n_kv_heads;
     Caps c;
     c.small = 2 * n_req + extra_s + 1;
     c.big = n_tok / TBb + 2 * n_req + extra_b + 1;

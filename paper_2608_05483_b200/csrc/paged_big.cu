@@ -6,7 +6,7 @@
 // A unit has two tiles of 128 rows (query tokens times the G heads of a KV head); they share every tile of
 // K and V, and while one tile's scores are in the softmax the tensor cores work for the other.
 // Roles: warps 0-3 and 4-7 are the softmax of the two tiles, a row per thread (no shuffles); warp 8 issues the MMAs;
-// warps 9 and 12 keep K and V coming through a ring (tensor-map boxes, one per page piece); warp 10 clears the rows of V
+// warps 9 and 13 keep K and V coming through a ring (tensor-map boxes, one per page piece); warp 10 clears the rows of V
 // behind an item's last key; warp 11 fetches items from a counter, an item ahead, and their queries.  Tensor memory (all
 // 512 columns): S of the two tiles, O of the two tiles.
 //
@@ -17,7 +17,7 @@
 //
 // A tile's step is: scores (512 cycles of the tensor pipe at D = 128), softmax, O += P V (512).  Measured by the clock inside the
 // kernel on 16 prompts of 2048 to 4096 tokens: the two tiles' steps take 3700 cycles together, 2050 of them with the tensor
-// pipe busy (46 %; 0.9 PFLOP/s at the 1.7 GHz the part holds under it, 1.09 ms; 1.25 ms once the power limit sets in).  A
+// pipe busy (46 %; 0.9 PFLOP/s at the 1.7 GHz the part holds under it, 1.09 ms; 1.22 ms once the power limit sets in).  A
 // step is a chain, softmax (2000) - hand-over (250) - products (1350) - hand-over (250), and tensor memory holds the scores
 // of two tiles, so at most two chains run.  What the instructions cost hardly shows: a third of the exponentials on the FMA
 // pipe, two threads to a row, an MMA warp per tile, 64 keys with two sets of scores per tile all took as long or longer.
@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kTileKeys = 128;
 constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kKeyWarp = 9, kTailWarp = 10, kItemWarp = 11, kValueWarp = 13;
-constexpr int kThreads = 16 * 32;       // four warpgroups (the last three warps only give their registers away)
+constexpr int kThreads = 16 * 32;       // four warpgroups (three warps only give their registers away)
 constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;       // of 128 a thread at launch: 2 * 184 + 2 * 72 = 4 * 128
 constexpr int kSched = 2;
 constexpr float kLazy = 8.f;        // base-2 logarithm of the growth a row's maximum may have before O is rescaled
@@ -266,7 +266,7 @@ __device__ __forceinline__ void item_warp(const Params& p, const Smem& sm, const
     __syncwarp();
 }
 
-// ---- warps 9 and 12: keys, values ------------------------------------------------------------------------------------
+// ---- warps 9 and 13: keys, values ------------------------------------------------------------------------------------
 // A warp each: with pages of 16 tokens a tile is 16 boxes.  As with the MMAs, the warp stays together and an elected lane
 // issues (a copy that every lane issues for itself cost 100 to 200 cycles).
 template <int D>
