@@ -321,7 +321,11 @@ def _token_stride(name, t) -> int:
     st, sh, sd = t.stride()
     if not t.is_cuda or (sd != 1 and d > 1) or (sh != d and h > 1):
         _bad(f"{name}: CUDA tensor [n_tok, heads, head_dim] with packed heads expected")
-    return st if n > 1 else h * d
+    if n < 2:
+        return h * d
+    if st == 0:      # (the C structures read 0 as packed)
+        _bad(f"{name}: a tensor that is expanded along its tokens is not supported")
+    return st
 
 
 def _page_stride(k_cache, v_cache) -> int:
@@ -331,7 +335,11 @@ def _page_stride(k_cache, v_cache) -> int:
     if (v_cache.shape != k_cache.shape or v_cache.dtype is not k_cache.dtype or v_cache.stride() != st or not k_cache.is_cuda
             or not v_cache.is_cuda or st[3] != 1 or st[2] != d or (st[1] != s * d and h > 1)):
         _bad("k_cache, v_cache: alike CUDA tensors [n_pages, n_kv_heads, page_size, head_dim] with packed pages expected")
-    return st[0] if n > 1 else h * s * d
+    if n < 2:
+        return h * s * d
+    if st[0] == 0:   # (the C structures read 0 as packed)
+        _bad("k_cache, v_cache: a cache that is expanded along its pages is not supported")
+    return st[0]
 
 
 def _raw_stream(stream, t) -> int:

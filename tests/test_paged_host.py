@@ -65,3 +65,26 @@ def test_tensors_that_are_not_on_the_gpu_are_refused():
         P.rope_table(64, 8, scaling="no such scaling")
 
 
+class _OnGpu:
+    """Stands for a CUDA tensor of this shape and stride where only its layout is looked at."""
+
+    def __init__(self, shape, stride, dtype=torch.bfloat16):
+        self.shape, self._stride, self.dtype, self.is_cuda = shape, stride, dtype, True
+
+    def stride(self):
+        return self._stride
+
+
+def test_expanded_tensors_are_refused():
+    """A stride of 0 means packed in the C structures: a tensor expanded along its tokens would be read as n packed rows."""
+    row = lambda stride, n=4: _OnGpu((n, 2, 64), (stride, 64, 1))
+    assert torch.zeros(1, 2, 64).expand(4, 2, 64).stride() == row(0).stride()
+    with pytest.raises(ValueError):
+        binding._token_stride("q", row(0))
+    assert binding._token_stride("q", row(320)) == 320
+    assert binding._token_stride("q", row(0, 1)) == 128 and binding._token_stride("q", row(128, 0)) == 128
+    cache = lambda stride, n=4: _OnGpu((n, 2, 16, 64), (stride, 1024, 64, 1))
+    with pytest.raises(ValueError):
+        binding._page_stride(cache(0), cache(0))
+    assert binding._page_stride(cache(4096), cache(4096)) == 4096
+    assert binding._page_stride(cache(0, 1), cache(0, 1)) == 2048
