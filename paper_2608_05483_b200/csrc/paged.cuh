@@ -88,10 +88,10 @@ constexpr int kBigRows = 128;      // rows of a tile of the tensor-core kernel; 
 // Keys of a split of the mma.sync kernel: its items should number about kSmallItems (eight for each of two CTAs per SM).
 constexpr int kPlanSms = 148;          // the plan aims at this many SMs, whatever the device has: it sizes the workspace
 constexpr int kSmallItems = kPlanSms * 2 * 8;
-constexpr int kSmallMinKeys = 128;     // no split shorter than this
+constexpr int kSmallMinKeys = 128, kSmallMaxKeys = 1 << 30;     // no split shorter or longer than this
 __device__ __forceinline__ int small_chunk(long long keys, int n_kv_heads) {
     const long long per = (keys * n_kv_heads + kSmallItems - 1) / kSmallItems;
-    return (int)min((long long)(1 << 30), max((long long)kSmallMinKeys, (per + 63) / 64 * 64));
+    return (int)min((long long)kSmallMaxKeys, max((long long)kSmallMinKeys, (per + 63) / 64 * 64));
 }
 
 // ---- PTX wrappers ---------------------------------------------------------------------------------

@@ -520,15 +520,19 @@ struct Caps {
     long long small, big, part;
 };
 int tile_tokens(int G) { return kBigRows / G; }
-// Upper bounds of what the plan can write.  A split length is at least 1 / kSmallItems (1 / kBigItems) of all keys of its
-// kind, so the units are at most one per block plus that many / heads; blocks that are split make at most twice that many.
+// Upper bounds of what the plan can write.  A request makes one block of each kind, a large one its tokens' more, and so does a
+// group.  A split length is at least 1 / kSmallItems (1 / kBigItems) of all keys of its kind, so the units are at most one
+// per block plus that many / heads, and blocks that are split make at most twice that many; or it is the longest there is
+// (kSmallMaxKeys, kBigMaxKeys), and then every block is cut into at most as many pieces as the longest cache.
 Caps caps(long long n_tok, long long n_req, long long max_kv, int n_kv_heads, int G) {
     const long long TBs = kSmallRows / G > 0 ? kSmallRows / G : 1, TBb = 2 * tile_tokens(G);
     const long long extra_s = (kSmallItems + n_kv_heads - 1) / n_kv_heads, extra_b = (kBigItems + n_kv_heads - 1) / n_kv_heads;
+    const long long most_s = (max_kv + kSmallMaxKeys - 1) / kSmallMaxKeys, most_b = (max_kv + kBigMaxKeys - 1) / kBigMaxKeys;
     Caps c;
-    c.small = 2 * n_req + extra_s + 1;
-    c.big = n_tok / TBb + 2 * n_req + extra_b + 1;
-    const long long by_items = 2 * n_req + 4 * (extra_s * TBs + extra_b * TBb);
+    c.small = 2 * n_req * most_s + extra_s + 1;
+    c.big = (n_tok / TBb + 2 * n_req) * most_b + extra_b + 1;
+    const long long at_longest = (most_s > 1 ? most_s : 0) + (most_b > 1 ? most_b : 0);
+    const long long by_items = 2 * n_req + 4 * (extra_s * TBs + extra_b * TBb) + (n_tok + n_req) * at_longest;
     const long long by_len = n_tok * (2 * ((max_kv + kSmallMinKeys - 1) / kSmallMinKeys) + 2);
     c.part = by_items < by_len ? by_items : by_len;
     return c;

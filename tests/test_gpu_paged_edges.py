@@ -1,0 +1,42 @@
+"""Attention over the paged cache at the edges of its plan: lists that run full, ranges and numbers at their limits."""
+import pytest
+import torch
+
+import paper_2608_05483_b200 as P
+from test_gpu_paged import DEV, Batch, _ints
+
+pytestmark = pytest.mark.gpu
+
+
+def _status(ws):
+    rc, status = P.plora_attn_status(ws.data_ptr())
+    assert rc == 0
+    return status
+
+
+def test_caches_longer_than_the_longest_split():
+    """Blocks of a prompt behind nine million keys are cut into three pieces each, more of them than items aimed at."""
+    n, hq, d, page, kv, window = 3000, 64, 64, 128, 9_000_000, 200
+    g = torch.Generator(device=DEV).manual_seed(0)
+    pages = -(-kv // page)
+    cache = torch.randn((2, pages, 1, page, d), generator=g, device=DEV, dtype=torch.bfloat16)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[None]
+    q = torch.randn((n, hq, d), generator=g, device=DEV, dtype=torch.bfloat16)
+    pos = torch.arange(kv - n, kv, device=DEV)
+    lo = (pos + 1 - window).to(torch.int32)
+    lo[::7] = 0                                       # (some see the other pieces too, if only by weights that vanish)
+    ws = P.attn_paged_workspace(q, cache[0], 1)
+    slopes = torch.full((hq,), 1.0, device=DEV)
+    got, _ = P.attn_paged(q, cache[0], cache[1], table, _ints([kv]), d ** -0.5, tok_start=_ints([0, n]), key_lo=lo, slopes=slopes,
+                          workspace=ws)
+    torch.cuda.synchronize()
+    assert _status(ws) == 0
+    K, V = (c.view(-1, d)[kv - n - window:kv].double() for c in cache)
+    key = torch.arange(kv - n - window, kv, device=DEV)
+    for a in range(0, n, 500):
+        s = torch.einsum("thd,kd->thk", q[a:a + 500].double(), K) * d ** -0.5 - (pos[a:a + 500, None, None] - key).abs()
+        see = (key >= (pos[a:a + 500, None, None] + 1 - window)) & (key <= pos[a:a + 500, None, None])
+        w = torch.softmax(s.masked_fill(~see, float("-inf")), -1)
+        want, mean = w @ V, w @ V.abs()
+        # (distances of up to 2^24 are rounded to 1 at most, where their weights are nothing)
+        assert bool(((got[a:a + 500].double() - want).abs() <= (2 * 2.0 ** -8 + 1e-4) * mean + 1e-5).all())

@@ -64,6 +64,13 @@ def test_tensors_that_are_not_on_the_gpu_are_refused():
     with pytest.raises(ValueError):
         P.rope_table(64, 8, scaling="no such scaling")
 
+@pytest.mark.parametrize("n_tok,hq,hk,d,page,blocks", [(16384, 64, 8, 128, 128, 35157), (40000, 8, 8, 64, 16, 400000)])
+def test_workspace_holds_the_partial_results_of_the_longest_caches(n_tok, hq, hk, d, page, blocks):
+    """A piece of a split has at most 2^22 keys: every token of a prompt behind a longer cache leaves a partial result per piece."""
+    pieces = -(-blocks * page // (1 << 22))
+    assert pieces > 1
+    assert P.plora_attn_paged_workspace_bytes(n_tok, 1, hq, hk, d, page, blocks) >= n_tok * pieces * hq * (d + 2) * 4
+
 
 class _OnGpu:
     """Stands for a CUDA tensor of this shape and stride where only its layout is looked at."""
