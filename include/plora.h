@@ -533,6 +533,8 @@ PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args *args, void 
  *            group has one token they are read once, for all, through the first request's block table.  (With LoRA on
  *            k and v, requests share a prefix if they share their adapter: groups are then the bucket's segments.)
  *            The result does not depend on the grouping beyond rounding.  n_groups = 0: none.
+ *            tok_start and group_start have to ascend (equal entries: a request without tokens, a group without requests); if
+ *            one does not, nothing is computed and the status word gets PLORA_ERR_INVALID_ARG.  n_groups <= n_req.
  * type       PLORA_INPUT_BF16 / FP16 of q, K, V and out; products and sums in fp32, weights rounded to the type for the
  *            second product.
  * q [n_tok][n_q_heads][head_dim] (q_stride elements between tokens, 0: packed), out packed; query head h reads KV

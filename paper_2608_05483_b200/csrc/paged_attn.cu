@@ -148,7 +148,6 @@ __device__ __forceinline__ void write_token_info(const Params& p) {
 struct Large {
     Req q;
     int r, unit, part;
-    bool room;
 };
 
 // RAGGED: token counts per request are given; GROUPED: groups are given.  (Forms of their own, because the plan's time is
@@ -184,7 +183,19 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         for (int g = tid; g <= p.n_groups; g += kPlanThreads) s_group[g] = clampi(p.group_start[g], 0, p.n_req);
         for (int g = tid; g < p.n_groups; g += kPlanThreads) s_prefix[g] = p.prefix_len[g];
     }
-    __syncthreads();
+    // Ranges that do not ascend would overlap: there is no bound on the units they want, and the lists have room for what
+    // ranges that share nothing can want (see caps()).  Such a batch gets no units.
+    bool descends = false;
+    for (int r = tid; RAGGED && r < p.n_req; r += kPlanThreads) descends |= p.tok_start[r] > p.tok_start[r + 1];
+    for (int g = tid; GROUPED && g < p.n_groups; g += kPlanThreads) descends |= p.group_start[g] > p.group_start[g + 1];
+    if (__syncthreads_or(descends)) {
+        if (tid == 0) {
+            atomicCAS(p.header, 0, PLORA_ERR_INVALID_ARG);
+            p.header[kSmallUnitsWord] = p.header[kBigUnitsWord] = p.header[kMergeWord] = 0;
+            p.header[kSmallNextWord] = p.header[kBigNextWord] = 0;
+        }
+        return;
+    }
     auto kv_at = [&](int r) { return held ? s_kv[r] : kv_of(p, r); };
     auto tokens_of = [&](int r, int& tok0, int& n) {
         if (!RAGGED) {
@@ -284,9 +295,6 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     if (per_b > kBigOneRound) per_b = max((long long)kBigOneRound, (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems);
     const int chunk_b = (int)min((long long)kBigMaxKeys, max((long long)kBigMinKeys, (per_b + 127) / 128 * 128));
     auto splits_of = [&](int keys, bool small) { const int c = small ? chunk_s : chunk_b; return (keys + c - 1) / c; };
-    auto fits = [&](const Sums& at, const Sums& want) {
-        return at.small + want.small <= p.cap_small && at.big + want.big <= p.cap_big && at.part + want.part <= p.cap_part;
-    };
     auto put = [&](bool small, int i, const Unit& u) { (small ? p.small_units : p.big_units)[i] = u; };
 
     Sums carry{0, 0, 0}, total;
@@ -302,15 +310,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         }
         const bool small = is_small(n);
         const int TB = small ? TBs : TBb, chunk = small ? chunk_s : chunk_b;
-        int splits = splits_of(pre, small);
+        const int splits = splits_of(pre, small);
         const int blocks = pre > 0 ? (n + TB - 1) / TB : 0;
         const Sums want{small ? splits * blocks : 0, small ? 0 : splits * blocks, pre > 0 ? splits * n : 0};
         const Sums at = carry + scan_exclusive(want, total, warp_sums);
         if (pre > 0) {
-            if (!fits(at, want)) {
-                atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
-                splits = 0;
-            }
             for (int b = 0; b < blocks; ++b) {
                 const int nt = min(TB, n - b * TB);
                 for (int i = 0; i < splits; ++i)
@@ -346,12 +350,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
             }
         }
         const Sums at = carry + scan_exclusive(want, total, warp_sums);
-        const bool room = fits(at, want);
-        if (!room) atomicCAS(p.header, 0, PLORA_ERR_WORKSPACE);
         // lists a token for the merge: `splits` partial results of its own keys from `part` on, `stride` apart, and its prefix's
         auto list = [&](int tok, int at, int part, int splits, int stride, int pre_keys) {
             const int4 pre = pre_keys > 0 ? p.tok_prefix[tok] : make_int4(0, 0, 0, 0);
-            if (at < p.n_tok) p.tok_merge[at] = TokMerge{tok, {part, pre.x}, {splits, pre.y}, {stride, pre.z}, 0};
+            p.tok_merge[at] = TokMerge{tok, {part, pre.x}, {splits, pre.y}, {stride, pre.z}, 0};
         };
         // writes the units of one block, and lists its tokens if they need a merge
         auto write_block = [&](const Req& q, int r, int b, bool small, int splits, int k0, int k1, int unit, int part) {
@@ -371,14 +373,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         }
         if (RAGGED && !small) slot = atomicAdd(&s_n_large, 1);
         if (slot < kLargeCache) {
-            s_large[slot] = Large{q, r, at.big, at.part, room};
+            s_large[slot] = Large{q, r, at.big, at.part};
         } else if (q.n > 0) {
             // (the last block first: it sees the most keys, and the items are taken in this order)
             int unit = small ? at.small : at.big, part = at.part;
             for (int b = nb - 1; b >= 0; --b) {
                 int k0, k1;
                 block_keys(q, b, TB, k0, k1);
-                const int splits = room ? splits_of(k1 - k0, small) : 0;
+                const int splits = splits_of(k1 - k0, small);
                 write_block(q, r, b, small, splits, k0, k1, unit, part);
                 unit += splits;
                 if (splits > 1 || q.pre > 0) part += splits * min(TB, q.n - b * TB);
@@ -396,7 +398,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
                 int k0 = 0, k1 = 0, splits = 0, parts = 0;
                 if (b >= 0) {
                     block_keys(big.q, b, TBb, k0, k1);
-                    splits = big.room ? splits_of(k1 - k0, false) : 0;
+                    splits = splits_of(k1 - k0, false);
                     if (splits > 1 || big.q.pre > 0) parts = splits * min(TBb, big.q.n - b * TBb);
                 }
                 int su = splits, sp = parts;
@@ -432,11 +434,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     }
     __syncthreads();
     if (tid == 0) {
-        p.header[kSmallUnitsWord] = min(carry.small, p.cap_small);
-        p.header[kBigUnitsWord] = min(carry.big, p.cap_big);
+        p.header[kSmallUnitsWord] = carry.small;
+        p.header[kBigUnitsWord] = carry.big;
         p.header[kSmallNextWord] = 0;
         p.header[kBigNextWord] = 0;
-        p.header[kMergeWord] = min(s_merge, p.n_tok);
+        p.header[kMergeWord] = s_merge;
     }
 }
 

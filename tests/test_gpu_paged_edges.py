@@ -40,3 +40,28 @@ def test_caches_longer_than_the_longest_split():
         want, mean = w @ V, w @ V.abs()
         # (distances of up to 2^24 are rounded to 1 at most, where their weights are nothing)
         assert bool(((got[a:a + 500].double() - want).abs() <= (2 * 2.0 ** -8 + 1e-4) * mean + 1e-5).all())
+
+
+@pytest.mark.parametrize("what", ["tokens", "groups"])
+def test_ranges_that_do_not_ascend_are_refused(what):
+    """Ranges that jump back may want any number of units.  The call says so, and runs nothing that an earlier, larger batch left
+    in the workspace."""
+    big = Batch(30, [900] * 4, [900] * 4, hq=8, hk=1, d=64)          # leaves units of up to 3600 tokens behind
+    n, n_req = (600, 400) if what == "tokens" else (40, 40)
+    ws = P.attn_paged_workspace(big.q, big.K, 400)
+    big.check(big.run(workspace=ws), big.reference())
+    b = Batch(31, [600] + [1] * (n_req - 1), [n] + [0] * (n_req - 1), hq=8, hk=1, d=64)
+    guard = torch.full((n + 8, 8, 64), 77.0, dtype=b.dtype, device=DEV)
+    table, kv = b.table[:1].expand(n_req, -1).contiguous(), _ints([600] * n_req)
+    if what == "tokens":
+        kw = dict(tok_start=_ints([0 if r % 2 == 0 else n for r in range(n_req + 1)]))
+    else:
+        kw = dict(group_start=_ints([0, 30, 10, 40]), prefix_len=_ints([100, 100, 100]))
+    P.attn_paged(b.q, b.K, b.V, table, kv, b.scale, out=guard[4:4 + n], workspace=ws, **kw)
+    torch.cuda.synchronize()
+    assert _status(ws) == P.ERR_INVALID_ARG
+    assert bool((guard[:4] == 77).all()) and bool((guard[-4:] == 77).all())
+    b.check(b.run(workspace=ws), b.reference())                          # and the workspace stays usable
+    # equal entries are none of this: requests without tokens, groups without requests
+    c = Batch(32, [40, 7, 90, 9], [20, 0, 0, 9], hq=8, hk=1, d=64)
+    c.check(c.run(workspace=ws, groups=[0, 0, 2, 2, 4], prefix=[5, 0, 9, 3]), c.reference())
