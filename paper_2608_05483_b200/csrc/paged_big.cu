@@ -149,6 +149,7 @@ struct Smem {
     uint32_t kv_full, kv_empty, q_full, q_empty, s_full, p_ready, o_full, sched_full, sched_empty, wind_down, tail_go, tail_done;
     Item* items;
     uint32_t* tmem_slot;
+    uint32_t* filled;        // [2]: how far each loader got
     WaitCtl wc;
 };
 template <int D>
@@ -177,6 +178,7 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, const Params& p) {
     s.wc.abort_flag = reinterpret_cast<volatile int*>(words);
     s.wc.header = p.header;
     s.tmem_slot = reinterpret_cast<uint32_t*>(words + 8);
+    s.filled = reinterpret_cast<uint32_t*>(words + 16);
     return s;
 }
 
@@ -318,16 +320,22 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
             }
         }
     }
-    // copies in flight must land before the CTA leaves.  (An older stage than these has been used again, and so has landed; of
-    // these a barrier is at most one phase further on, and then it answers yes.)
-    if (lane == 0) {
-        const long long limit = wait_limit(p.header);
+    if (lane == 0) sm.filled[kv] = it;
+    __syncwarp();
+}
+// When both loaders have stopped: the copies still in flight must land before the CTA leaves (after a wait that ran out, up to
+// all of a ring may be).  A lane per stage looks at what was sent there last; only then does a phase tell the copy, for
+// the two loaders share the ring, and the one that stops first does not know which stages the other has filled again.
+template <int D>
+__device__ __forceinline__ void drain_ring(const Params& p, const Smem& sm, int lane) {
+    constexpr uint32_t kStages = Cfg<D>::kStages;
+    int last = -1;                           // (stages are numbered through, K even, V odd; a loader has filled all of its below filled[])
 #pragma unroll 1
-        for (uint32_t k = 2; k <= (uint32_t)C::kStages && k <= it; k += 2) {
-            const uint32_t j = it - k;
-            if (!mbar_drain(sm.kv_full + (j % C::kStages) * 8, (j / C::kStages) & 1, limit)) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
-        }
+    for (int i = 0; i < 2 * (int)kStages; ++i) {
+        const int x = (int)sm.filled[i & 1] - 2 - (i & ~1);
+        if (lane < (int)kStages && x >= 0 && x % (int)kStages == lane) last = max(last, x);
     }
+    if (last >= 0 && !mbar_drain(sm.kv_full + lane * 8, (last / (int)kStages) & 1, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
     __syncwarp();
 }
 
@@ -729,6 +737,7 @@ big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (warp == kKeyWarp) drain_ring<D>(p, sm, lane);
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 

@@ -65,3 +65,18 @@ def test_ranges_that_do_not_ascend_are_refused(what):
     # equal entries are none of this: requests without tokens, groups without requests
     c = Batch(32, [40, 7, 90, 9], [20, 0, 0, 9], hq=8, hk=1, d=64)
     c.check(c.run(workspace=ws, groups=[0, 0, 2, 2, 4], prefix=[5, 0, 9, 3]), c.reference())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompts_whose_waits_run_out_leave_nothing_behind(d):
+    """Every CTA stops with copies under way; it waits for them before its shared memory goes to the next one, call after call."""
+    b = Batch(33, [4000, 3000], [700, 600], hq=8, hk=8, d=d, page=16)       # (items of more tiles than the ring has stages)
+    ref = b.reference()
+    ws = P.attn_paged_workspace(b.q, b.K, 2)
+    for _ in range(3):
+        assert P.plora_attn_set_debug(ws.data_ptr(), 1 << 20, P.HOOK_WITHHOLD_RELEASE) == 0
+        P.attn_paged(b.q, b.K, b.V, b.table, b.kv_len, b.scale, tok_start=b.tok_start, workspace=ws)
+        torch.cuda.synchronize()
+        assert _status(ws) == P.ERR_TIMEOUT
+        assert P.plora_attn_set_debug(ws.data_ptr(), 0, P.HOOK_NONE) == 0
+        b.check(b.run(workspace=ws), ref)
