@@ -64,7 +64,7 @@ __device__ __forceinline__ TokInfo visible(const Params& p, int t, int pos, int 
     TokInfo ti;
     ti.pos = pos;
     ti.lo = p.key_lo ? max(p.key_lo[t], 0) : 0;
-    ti.hi = p.key_hi ? min(p.key_hi[t], kv) : min(pos + 1, kv);
+    ti.hi = max(0, min(p.key_hi ? p.key_hi[t] : pos + 1, kv));     // (not below 0: the kernels take differences of it and keys)
     ti.pad_ = 0;
     return ti;
 }

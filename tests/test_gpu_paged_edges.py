@@ -80,3 +80,18 @@ def test_prompts_whose_waits_run_out_leave_nothing_behind(d):
         assert _status(ws) == P.ERR_TIMEOUT
         assert P.plora_attn_set_debug(ws.data_ptr(), 0, P.HOOK_NONE) == 0
         b.check(b.run(workspace=ws), ref)
+
+
+@pytest.mark.parametrize("new", [[300, 40, 3], None])
+def test_intervals_at_the_limits_of_their_type(new):
+    """Ends of key intervals may be any int32: the lowest for "nothing", the highest for "no limit"."""
+    b = Batch(34, [900, 700, 300], new, hq=4, hk=2, page=32)
+    n = b.tok[-1]
+    low, high = -2 ** 31, 2 ** 31 - 1
+    ends = [low, high, low + 1, 200, -1, 0, 1]
+    starts = [low, low, 0, low, high, high, 0, -1]
+    kw = dict(key_lo=_ints(starts[i % len(starts)] for i in range(n)), key_hi=_ints(ends[i % len(ends)] for i in range(n)))
+    got, ref = b.run(**kw), b.reference(**kw)
+    b.check(got, ref)
+    empty = ref[1].sum((1, 2)) == 0
+    assert empty.any() and bool((got[empty] == 0).all())
