@@ -542,6 +542,8 @@ PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args *args, void 
  * head.  q, K, V and out 16-byte aligned, strides multiples of 8.  Cache slots at or beyond kv_len may hold anything; below
  * it K and V have to be finite, masked or not (a masked value still meets a weight of zero).
  * A block table entry outside [0, n_pages) that is needed reads as zeros and sets PLORA_ERR_INVALID_ARG in the status word.
+ * (Needed is what lies between the first and the last key that one of the tokens computed together sees: consecutive tokens of a
+ * request, or of a group against its prefix.)
  * Batches with more than 16 query rows per KV head and unit (prompts, groups) run a kernel whose CTAs each take all 512
  * tensor-memory columns of their SM; as with plora_lora_delta's tensor-core path, do not run it beside a kernel that holds
  * tensor memory for its whole lifetime and itself waits for this call.

@@ -10,6 +10,8 @@
 // meet in shared memory.
 // P is rounded to the input type for the second product (at most 2^-8 or 2^-11 of each weight, zero mean; the output
 // is rounded to the same type).
+#include <limits.h>
+
 #include "paged.cuh"
 
 namespace plora {
@@ -185,8 +187,16 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             }
             ti.lo = max(ti.lo, u.k0);
             ti.hi = min(ti.hi, u.k1);
+            if (!SELF) {
+                // Of its keys a unit reads those that a token sees (pages of a prefix that lie before every window may be gone).
+                // With none there is still a tile, without a page, for the result that says so.
+                const bool sees = ti.lo < ti.hi;
+                u.k0 = __reduce_min_sync(all, sees ? ti.lo : INT_MAX);
+                u.k1 = __reduce_max_sync(all, sees ? ti.hi : 0);
+                if (u.k0 >= u.k1) u.k0 = u.k1 = 0;
+            }
             const int kf = u.k0 / bp * bp;
-            const int n_tiles = (u.k1 - kf + kTile - 1) / kTile;
+            const int n_tiles = max(1, (u.k1 - kf + kTile - 1) / kTile);
             const int32_t* table = p.block_table + (size_t)u.req * p.max_blocks;
             for (int t = 0; t < n_tiles; ++t, ++it) {
                 const uint32_t slot = it % C::kStages, dst = slots + slot * C::kSlotBytes, bar = full + slot * 8;

@@ -95,3 +95,22 @@ def test_intervals_at_the_limits_of_their_type(new):
     b.check(got, ref)
     empty = ref[1].sum((1, 2)) == 0
     assert empty.any() and bool((got[empty] == 0).all())
+
+
+@pytest.mark.parametrize("n_req,hq,hk", [(3, 4, 2), (2, 8, 1), (40, 4, 2)])
+def test_a_window_behind_released_pages_of_the_prefix(n_req, hq, hk):
+    """Sliding windows: pages that no token of a group sees any more may be gone from its table, grouped or not."""
+    prefix, window = 700, 150
+    own = [(7 * i) % 90 for i in range(n_req)]
+    b = Batch(35, [prefix + x for x in own], hq=hq, hk=hk, page=16, groups=[0, n_req], prefix=[prefix])
+    lo = [prefix + x - window for x in own]
+    b.table[:, :min(lo) // 16] = -1
+    kw = dict(key_lo=_ints(lo))
+    ref = b.reference(**kw)
+    b.check(b.run(**kw), ref)
+    b.check(b.run([0, n_req], [prefix], **kw), ref)
+    # a window that leaves nothing of the prefix, with all of its pages gone
+    b.table[:, :prefix // 16] = -1
+    kw = dict(key_lo=_ints([prefix] * n_req))
+    ref = b.reference(**kw)
+    b.check(b.run([0, n_req], [prefix], **kw), ref)
