@@ -76,9 +76,10 @@ struct Params {
     int32_t page_size, page_shift, n_pages, max_blocks;
     int32_t max_kv;           // min(max_blocks, n_pages) * page_size
     float scale_log2e;        // softmax scale times log2(e): scores live in the base-2 domain
-    float cap_d[5];           // its polynomial, for |qk| <= cap_poly_below
+    // capped scores, cap_log2e * tanh(qk * scale / softcap): see capped()
+    float cap_d[5];           // the polynomial, for |qk| <= cap_poly_below (below 0: not used)
     float cap_poly_below;
-    float cap_in, cap_log2e;  // capped scores: cap_log2e * tanh(cap_in * qk), cap_in already times 2 log2(e)
+    float cap_in, cap_log2e;  // cap_in = 2 log2(e) * scale / softcap
 };
 
 constexpr int kSmallRows = 16;     // rows of a unit the mma.sync kernel takes
@@ -195,13 +196,22 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// Score in the base-2 domain from the raw product: scale, cap, bias by distance.  tanh(x) is taken as
-// 1 - 2 / (1 + e^2x): the fast tanh instruction's 2^-11 would be multiplied by the cap before it reaches an exponential.
+// A capped score in the base-2 domain.  Its error reaches an exponential, so it has to be small against the score, whatever the
+// cap.  For |x| <= 0.6 tanh(x) is x P(x^2), P of degree 4 fitted for the least relative error (8e-8), its coefficients scaled so
+// that it takes the raw product: s (d0 + s^2 (d1 + ...)).  Beyond, it is 1 - 2 / (1 + e^2x): off by 1.5e-7 of the cap, which
+// is some 3e-7 of the score there (and could be any share of a small one).  (The fast tanh instruction is off by 2^-11.)
+__device__ __forceinline__ float capped_far(const Params& p, float qk) {
+    return fmaf(-2.f * p.cap_log2e, rcp(1.f + ex2(qk * p.cap_in)), p.cap_log2e);
+}
+__device__ __forceinline__ float capped(const Params& p, float qk) {
+    const float u = qk * qk;
+    const float near = fmaf(fmaf(fmaf(fmaf(p.cap_d[4], u, p.cap_d[3]), u, p.cap_d[2]), u, p.cap_d[1]), u, p.cap_d[0]) * qk;
+    return fabsf(qk) <= p.cap_poly_below ? near : capped_far(p, qk);
+}
+// Score in the base-2 domain from the raw product: scale, cap, bias by distance.
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ float score(const Params& p, float qk, float slope, int dist) {
-    float s;
-    if (CAP) s = fmaf(-2.f * p.cap_log2e, rcp(1.f + ex2(qk * p.cap_in)), p.cap_log2e);
-    else s = qk * p.scale_log2e;
+    float s = CAP ? capped(p, qk) : qk * p.scale_log2e;
     if (BIAS) s = fmaf(-slope, fabsf((float)dist), s);
     return s;
 }

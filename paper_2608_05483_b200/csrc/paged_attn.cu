@@ -634,12 +634,15 @@ extern "C" PLORA_API plora_status plora_attn_paged(const plora_paged_attn* a, vo
     const float log2e = 1.4426950408889634f;
     p.scale_log2e = a->scale * log2e;
     if (a->softcap > 0.f) {
-        // tanh(x) / x = c0 + c1 x^2 + ... on |x| <= 3/4, taken at x = qk * scale / cap
-        const double c[5] = {0.9999971985816956, -0.33323076367378235, 0.13226091861724854, -0.049280449748039246, 0.012318835593760014};
+        // tanh(x) / x = c0 + c1 x^2 + ... on |x| <= 0.6, taken at x = qk * scale / cap
+        const double c[5] = {0.9999999307565199, -0.33332344319327695, 0.13310648968894678, -0.05212255543054139, 0.015504650012447066};
         const double x = (double)a->scale / a->softcap;
         double power = (double)a->scale * 1.4426950408889634;
         for (int i = 0; i < 5; ++i, power *= x * x) p.cap_d[i] = (float)(c[i] * power);
-        p.cap_poly_below = x != 0.0 ? (float)(0.75 / (x < 0 ? -x : x)) : 3.0e38f;
+        // (the square of a product must stay a number; so must the coefficients, which a cap next to nothing makes overflow)
+        const double below = x != 0.0 ? 0.6 / (x < 0 ? -x : x) : 1e18;
+        p.cap_poly_below = (float)(below < 1e18 ? below : 1e18);
+        if (!(p.cap_d[4] - p.cap_d[4] == 0.f)) p.cap_poly_below = -1.f;
         p.cap_in = 2.f * log2e * a->scale / a->softcap;
         p.cap_log2e = a->softcap * log2e;
     }

@@ -35,6 +35,7 @@ constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kKeyWarp = 9, kTailWarp = 10, kIt
 constexpr int kThreads = 16 * 32;       // four warpgroups (three warps only give their registers away)
 constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;       // of 128 a thread at launch: 2 * 184 + 2 * 72 = 4 * 128
 constexpr int kSched = 2;
+constexpr float kWideCap = 256.f;   // caps above take the form of their own in scores_of()
 constexpr float kLazy = 8.f;        // base-2 logarithm of the growth a row's maximum may have before O is rescaled
 
 template <int D>
@@ -483,16 +484,21 @@ __device__ __forceinline__ void tail_warp(const Params& p, const Smem& sm, int l
 }
 
 // 32 raw products of a row -> scores in the base-2 domain (cap, bias by distance); dist0: distance of the first one's key.
-// Below |x| = 3/4 the cap's tanh(x) is x P(x^2) on the FMA pipe, P of degree 4 fitted for the least absolute error (1.9e-7; it
-// is multiplied by the cap), its coefficients scaled so that it takes the raw product: s (d0 + s^2 (d1 + ...)).  A warp that
-// sees a larger argument takes the form with two special functions (see score()).
-template <bool CAP, bool BIAS>
+// CAP 1, caps of up to kWideCap: a row whose 32 products are all small takes the cap's polynomial, two at a time on the FMA pipe;
+// one with a larger product (a hidden one may be anything) takes the other form for all, which is off by 1.5e-7 of the cap, 4e-5
+// at most.  CAP 2, larger caps: chosen product by product (see capped()).  That form for all caps costs packed documents 8 %
+// (331 -> 358 us), most of it by the loop's code size: choosing in the rare branch alone costs as much.
+template <int CAP, bool BIAS>
 __device__ __forceinline__ void scores_of(const Params& p, float* s, float slope, float dist0) {
-    if (CAP) {
+    if (CAP == 2) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i] = capped(p, s[i]);
+    }
+    if (CAP == 1) {
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < 32; i += 2) most = fmaxf(fmaxf(most, fabsf(s[i])), fabsf(s[i + 1]));
-        if (__all_sync(0xffffffffu, most <= p.cap_poly_below)) {
+        if (most <= p.cap_poly_below) {
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
                 const float2 x = make_float2(s[i], s[i + 1]), u = __fmul2_rn(x, x);
@@ -506,8 +512,9 @@ __device__ __forceinline__ void scores_of(const Params& p, float* s, float slope
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s[i] = score<true, false>(p, s[i], 0.f, 0);
+            for (int i = 0; i < 32; ++i) s[i] = capped_far(p, s[i]);
         }
+        __syncwarp();
     }
     if (BIAS) {
         // |distance| as a float, counted down from the first key's (an integer conversion per score would go to the
@@ -518,7 +525,7 @@ __device__ __forceinline__ void scores_of(const Params& p, float* s, float slope
 }
 
 // ---- warps 0-7: softmax and output ------------------------------------------------------------------------------
-template <int D, bool FP16, bool CAP, bool BIAS>
+template <int D, bool FP16, int CAP, bool BIAS>
 __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, uint32_t tmem, int warp, int lane) {
     const unsigned all = 0xffffffffu;
     const int t = warp >> 2, row = (warp & 3) * 32 + lane, TT = p.big_tile_tok;
@@ -680,7 +687,7 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
     }
 }
 
-template <int D, bool FP16, bool CAP, bool BIAS>
+template <int D, bool FP16, int CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1)
 big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
            const Params p) {
@@ -741,7 +748,7 @@ big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-template <int D, bool FP16, bool CAP, bool BIAS>
+template <int D, bool FP16, int CAP, bool BIAS>
 cudaError_t go(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, Device dev, cudaStream_t st) {
     auto kern = big_kernel<D, FP16, CAP, BIAS>;
     static Configured configured;
@@ -755,9 +762,11 @@ cudaError_t go(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
 template <int D, bool FP16>
 cudaError_t go2(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, Device dev, cudaStream_t st) {
     // (a scale that is not positive takes the form that scales before it masks and looks for the maximum)
-    const bool cap = p.cap_log2e > 0.f, bias = p.slopes || !(p.scale_log2e > 0.f);
-    if (cap) return bias ? go<D, FP16, true, true>(q, k, v, p, dev, st) : go<D, FP16, true, false>(q, k, v, p, dev, st);
-    return bias ? go<D, FP16, false, true>(q, k, v, p, dev, st) : go<D, FP16, false, false>(q, k, v, p, dev, st);
+    const bool bias = p.slopes || !(p.scale_log2e > 0.f);
+    if (p.cap_log2e > kWideCap * 1.4426950408889634f)
+        return bias ? go<D, FP16, 2, true>(q, k, v, p, dev, st) : go<D, FP16, 2, false>(q, k, v, p, dev, st);
+    if (p.cap_log2e > 0.f) return bias ? go<D, FP16, 1, true>(q, k, v, p, dev, st) : go<D, FP16, 1, false>(q, k, v, p, dev, st);
+    return bias ? go<D, FP16, 0, true>(q, k, v, p, dev, st) : go<D, FP16, 0, false>(q, k, v, p, dev, st);
 }
 
 }  // namespace

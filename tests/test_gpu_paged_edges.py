@@ -114,3 +114,20 @@ def test_a_window_behind_released_pages_of_the_prefix(n_req, hq, hk):
     kw = dict(key_lo=_ints([prefix] * n_req))
     ref = b.reference(**kw)
     b.check(b.run([0, n_req], [prefix], **kw), ref)
+
+
+@pytest.mark.parametrize("new", [[300, 1, 40, 3], None])
+@pytest.mark.parametrize("cap", [1e-30, 0.01, 2.0, 1e4, 1e6, 1e12, 3e38])
+def test_caps_of_any_size(cap, new):
+    """A cap far above the scores changes nothing, one far below them makes all weights of a row alike; and a row of large scores
+    takes no accuracy from its neighbours."""
+    b = Batch(36, [500, 700, 400, 90], new, hq=4, hk=2, dtype=torch.float16)
+    n = b.tok[-1]
+    huge = 2 if new is None else 25
+    b.q = b.q.clone()
+    b.q[huge] *= 3000.0
+    got, (want, mean) = b.run(softcap=cap), b.reference(softcap=cap)
+    assert torch.isfinite(got).all()
+    keep = torch.arange(n, device=DEV) != huge        # (scores of 10^4: half an fp32 unit of them is 5e-4 in the exponent)
+    tol = (2 * 2.0 ** -11 + 1e-5) * mean + 701 * 2.0 ** -25 * 5.0 + 1e-6
+    assert bool(((got.double() - want).abs() <= tol)[keep].all())
