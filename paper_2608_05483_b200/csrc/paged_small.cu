@@ -8,9 +8,14 @@
 // softmax per warp in 32 bits.  (The legacy tensor instruction fits: its operands stay in registers, and at
 // 16 rows the tensor pipe is idle nine tenths of the time anyway.)  At the end of an item the warps' (m, l, o)
 // meet in shared memory.
-// P is rounded to the input type for the second product (at most 2^-8 or 2^-11 of each weight, zero mean; the output
-// is rounded to the same type).
+// The weights P enter the second product in two parts of the input type, the rounded value and the rest (16 bits of a bf16
+// weight, 22 of a half one, so that the output's own rounding is what is left of the error, as in plora_attn_decode).  With at
+// most 8 rows the rests are rows 8 to 15 of the same instruction and cost nothing there; with more the product runs twice.
+// Half-precision weights are held times 2^15, so that those of distant keys do not sink below its range (their row's
+// maximum then counts 15 less).
 #include <limits.h>
+
+#include <type_traits>
 
 #include "paged.cuh"
 
@@ -56,6 +61,20 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
     else
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// two weights -> their values in the input type, and what is left of them
+template <bool FP16>
+__device__ __forceinline__ void split16(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = pack16<FP16>(x, y);
+    float2 h;
+    if (FP16) {
+        h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    } else {
+        h.x = __uint_as_float(hi << 16);
+        h.y = __uint_as_float(hi & 0xffff0000u);
+    }
+    lo = pack16<FP16>(x - h.x, y - h.y);
 }
 
 // SELF: single tokens of at most kSelfRequests requests that are read one by one.  Each CTA's producer then finds its items
@@ -261,6 +280,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     // ------------------------------- consumer warps -------------------------------
     const int r0 = lane >> 2, c0 = (lane & 3) * 2;      // rows r0 and r0 + 8, columns c0, c0 + 1 of every 8-column block
     const int mi = lane >> 3, mr = lane & 7;            // ldmatrix: which 8 x 8 matrix this lane addresses, and which row of it
+    constexpr float kLift = FP16 ? 15.f : 0.f;
     uint32_t qf[D / 16][4];
     float o[D / 8][4];
     float m[2], l[2], slope[2];
@@ -321,32 +341,49 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 mma<FP16>(s[1], qf[ks], b[2], b[3]);
             }
         }
-        float mx[2] = {-INFINITY, -INFINITY};
+        // weights of the first `n_rows` of this lane's two rows
+        float al[2];
+        auto softmax = [&](auto n_rows) {
+            constexpr int R = decltype(n_rows)::value;
+            float mx[2] = {-INFINITY, -INFINITY}, me[2];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = e >> 1, key = key0 + n * 8 + c0 + (e & 1);
-                const float v = score<CAP, BIAS>(p, s[n][e], slope[i], pos[i] - key);
-                s[n][e] = key >= lo[i] && key < hi[i] ? v : -INFINITY;
-                mx[i] = fmaxf(mx[i], s[n][e]);
+                for (int e = 0; e < 2 * R; ++e) {
+                    const int i = e >> 1, key = key0 + n * 8 + c0 + (e & 1);
+                    const float v = score<CAP, BIAS>(p, s[n][e], slope[i], pos[i] - key);
+                    s[n][e] = key >= lo[i] && key < hi[i] ? v : -INFINITY;
+                    mx[i] = fmaxf(mx[i], s[n][e]);
+                }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(all, mx[i], 1));
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(all, mx[i], 2));
+                const float mn = fmaxf(m[i], mx[i]);
+                me[i] = mn == -INFINITY ? 0.f : mn;      // a row that has seen nothing yet: all its weights are 2^-inf
+                al[i] = ex2(m[i] - me[i]);
+                me[i] -= kLift;
+                m[i] = mn;
             }
-        float al[2], me[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            mx[i] = fmaxf(mx[i], __shfl_xor_sync(all, mx[i], 1));
-            mx[i] = fmaxf(mx[i], __shfl_xor_sync(all, mx[i], 2));
-            const float mn = fmaxf(m[i], mx[i]);
-            me[i] = mn == -INFINITY ? 0.f : mn;      // a row that has seen nothing yet: all its weights are 2^-inf
-            al[i] = ex2(m[i] - me[i]);
-            m[i] = mn;
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 2 * R; ++e) s[n][e] = ex2(s[n][e] - me[e >> 1]);
+#pragma unroll
+            for (int i = 0; i < R; ++i) l[i] = l[i] * al[i] + ((s[0][2 * i] + s[0][2 * i + 1]) + (s[1][2 * i] + s[1][2 * i + 1]));
+        };
+        const bool halves = rows <= 8;               // rows 8 to 15 are the rests of rows 0 to 7
+        uint32_t pf[4], pl[4];
+        if (halves) {
+            softmax(std::integral_constant<int, 1>{});
+            al[1] = al[0];
+            split16<FP16>(s[0][0], s[0][1], pf[0], pf[1]);
+            split16<FP16>(s[1][0], s[1][1], pf[2], pf[3]);
+        } else {
+            softmax(std::integral_constant<int, 2>{});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split16<FP16>(s[e >> 1][2 * (e & 1)], s[e >> 1][2 * (e & 1) + 1], pf[e], pl[e]);
         }
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = ex2(s[n][e] - me[e >> 1]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) l[i] = l[i] * al[i] + ((s[0][2 * i] + s[0][2 * i + 1]) + (s[1][2 * i] + s[1][2 * i + 1]));
         if (__any_sync(all, al[0] != 1.f || al[1] != 1.f)) {
 #pragma unroll
             for (int n = 0; n < D / 8; ++n) {
@@ -354,8 +391,6 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 o[n][2] *= al[1]; o[n][3] *= al[1];
             }
         }
-        const uint32_t pf[4] = {pack16<FP16>(s[0][0], s[0][1]), pack16<FP16>(s[0][2], s[0][3]),
-                                pack16<FP16>(s[1][0], s[1][1]), pack16<FP16>(s[1][2], s[1][3])};
         {
             const int r = row0 + (mi & 1) * 8 + mr;
 #pragma unroll
@@ -365,6 +400,10 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 ldsm4_t(st + C::kKBytes + (ch >> 3) * C::kPanelBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4), b);
                 mma<FP16>(o[2 * j], pf, b[0], b[1]);
                 mma<FP16>(o[2 * j + 1], pf, b[2], b[3]);
+                if (!halves) {
+                    mma<FP16>(o[2 * j], pl, b[0], b[1]);
+                    mma<FP16>(o[2 * j + 1], pl, b[2], b[3]);
+                }
             }
         }
         if (flags & kFlagLast) {
@@ -373,6 +412,13 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             for (int i = 0; i < 2; ++i) {
                 l[i] += __shfl_xor_sync(all, l[i], 1);
                 l[i] += __shfl_xor_sync(all, l[i], 2);
+            }
+            if (halves) {
+#pragma unroll
+                for (int n = 0; n < D / 8; ++n) {
+                    o[n][0] += o[n][2];
+                    o[n][1] += o[n][3];
+                }
             }
             consumer_meet();      // nobody reads the tile any more
             float* scr = reinterpret_cast<float*>(base + slot * C::kSlotBytes);
@@ -417,7 +463,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                     } else {
                         const size_t at = (size_t)(part + tr) * p.n_q_heads + hq;
                         *reinterpret_cast<float4*>(p.part_o + at * D + d) = O;
-                        if (d == 0) p.part_ml[at] = make_float2(M, L);
+                        if (d == 0) p.part_ml[at] = make_float2(M - kLift, L);
                     }
                 }
             }

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2608_05483_b200 as P
-from test_gpu_paged import DEV, Batch, _ints
+from test_gpu_paged import DEV, ROUND, Batch, _ints
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +131,17 @@ def test_caps_of_any_size(cap, new):
     keep = torch.arange(n, device=DEV) != huge        # (scores of 10^4: half an fp32 unit of them is 5e-4 in the exponent)
     tol = (2 * 2.0 ** -11 + 1e-5) * mean + 701 * 2.0 ** -25 * 5.0 + 1e-6
     assert bool(((got.double() - want).abs() <= tol)[keep].all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("hq,hk,new,groups", [(1, 1, None, False), (8, 1, None, False), (8, 2, None, True), (16, 1, None, False),
+                                              (12, 1, None, False), (4, 2, [2, 1, 2, 1], False), (10, 2, [3, 1, 3, 2], False)])
+def test_units_of_few_rows_keep_their_weights(hq, hk, new, groups, dtype):
+    """Up to 16 rows: an output is off by its own rounding (the type's unit roundoff) and next to nothing else.  The weights keep
+    16 bits or more, the scores of up to 10 and the exponentials are off by some 2^-20, fp32 sums by less."""
+    group = dict(groups=[0, 2, 4], prefix=[1500, 300]) if groups else {}
+    b = Batch(37, [3000, 1700, 400, 4097], new, hq=hq, hk=hk, d=128, page=64, dtype=dtype, **group)
+    got, (want, mean) = b.run(*group.values()), b.reference()
+    tol = 1.02 * ROUND[dtype] * want.abs() + 2.0 ** -16 * mean + 2.0 ** -25      # (half a unit below the normal range: 2^-25)
+    err = (got.double() - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
