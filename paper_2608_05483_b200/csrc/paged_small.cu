@@ -206,9 +206,10 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             }
             ti.lo = max(ti.lo, u.k0);
             ti.hi = min(ti.hi, u.k1);
-            if (!SELF) {
+            if (!SELF && (p.key_lo || p.key_hi)) {
                 // Of its keys a unit reads those that a token sees (pages of a prefix that lie before every window may be gone).
-                // With none there is still a tile, without a page, for the result that says so.
+                // With none there is still a tile, without a page, for the result that says so.  (Without intervals the plan's
+                // ranges are right as they are, and the pages need not wait for the tokens' intervals.)
                 const bool sees = ti.lo < ti.hi;
                 u.k0 = __reduce_min_sync(all, sees ? ti.lo : INT_MAX);
                 u.k1 = __reduce_max_sync(all, sees ? ti.hi : 0);
