@@ -234,6 +234,14 @@ def plora_stream_read(buf_ptr, nbytes: int, sink_ptr, sink_bytes: int, stream=0)
     return load().plora_stream_read(buf_ptr, int(nbytes), sink_ptr, int(sink_bytes), stream)
 
 
+def _new_on(stream, make, *size, **kw):
+    """A tensor made on the stream that the call runs on: zeroed before the kernels read it, and its memory handed on only
+    behind them."""
+    import torch
+    with torch.cuda.stream(stream):
+        return make(*size, **kw)
+
+
 def attn_decode(q, k_cache, v_cache, kv_len, scale, out=None, workspace=None, stream=None):
     """Torch convenience: q bf16 [B, Hq, 128], k_cache / v_cache bf16 [B, Hkv, Lmax, 128], kv_len int32 [B] (all CUDA);
     returns (out fp32 [B, Hq, 128], workspace).  Pass the returned workspace back in to reuse it."""
@@ -242,9 +250,9 @@ def attn_decode(q, k_cache, v_cache, kv_len, scale, out=None, workspace=None, st
     Hkv, Lmax = int(k_cache.shape[1]), int(k_cache.shape[2])
     need = plora_attn_workspace_bytes(B, Lmax, Hkv, Hq // Hkv)
     if workspace is None:
-        workspace = torch.zeros(need, dtype=torch.uint8, device=q.device)
+        workspace = _new_on(stream, torch.zeros, need, dtype=torch.uint8, device=q.device)
     if out is None:
-        out = torch.empty((B, Hq, d), dtype=torch.float32, device=q.device)
+        out = _new_on(stream, torch.empty, (B, Hq, d), dtype=torch.float32, device=q.device)
     _check(plora_attn_decode(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), kv_len.data_ptr(), B, Lmax, Hkv, Hq // Hkv,
                              d, scale, out.data_ptr(), workspace.data_ptr(), int(workspace.numel()), _stream_handle(stream)),
            "plora_attn_decode")
@@ -353,7 +361,9 @@ def kv_plan(kv_len, new_len, page_size: int, free_pages, block_table, max_tokens
     n, = kv_len.shape
     one, toks = (n,), (max_tokens,)
     if out is None:
-        buf = torch.empty(2 * n + 2 + 3 * max_tokens, dtype=torch.int32, device=kv_len.device)
+        size = 2 * n + 2 + 3 * max_tokens
+        buf = (torch.empty(size, dtype=torch.int32, device=kv_len.device) if stream is None
+               else _new_on(stream, torch.empty, size, dtype=torch.int32, device=kv_len.device))
         out = KvPlan(*buf.split_with_sizes((n + 1, max_tokens, max_tokens, max_tokens, n, 1)))
         at = buf.data_ptr()
         ptrs = (at, at + 4 * (n + 1), at + 4 * (n + 1 + max_tokens), at + 4 * (n + 1 + 2 * max_tokens),
@@ -380,7 +390,7 @@ def rope_table(rot_dim: int, max_pos: int, base: float = 10000.0, scaling: str =
     """The fp32 table [max_pos, rot_dim // 2, 2] of cosines and sines (plora_rope_table)."""
     if scaling not in _SCALINGS:
         _bad(f"scaling: one of {sorted(_SCALINGS)} expected, got {scaling!r}")
-    table = torch.empty((max(0, int(max_pos)), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
+    table = _new_on(stream, torch.empty, (max(0, int(max_pos)), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
     d = RopeDesc(int(rot_dim), _SCALINGS[scaling], base, factor, orig_len, low, high, magnitude)
     _check(plora_rope_table(d, int(max_pos), table.data_ptr(), _raw_stream(stream, table)), "plora_rope_table")
     return table
@@ -405,7 +415,8 @@ def rope_cache(q, k, v, positions, slots, table, k_cache, v_cache, q_out=None, i
     if k.shape != (n, hk, d) or v.shape != (n, hk, d) or ch != hk or cd != d:
         _bad("q, k, v and the caches: shapes do not agree")
     if q_out is None:
-        q_out = torch.empty((n, hq, d), dtype=k_cache.dtype, device=q.device)
+        q_out = (torch.empty((n, hq, d), dtype=k_cache.dtype, device=q.device) if stream is None
+                 else _new_on(stream, torch.empty, (n, hq, d), dtype=k_cache.dtype, device=q.device))
     elif q_out.dtype is not k_cache.dtype or q_out.shape != (n, hq, d) or not q_out.is_cuda or not q_out.is_contiguous():
         _bad("q_out: packed, of the cache's type and q's shape, expected")
     rot = max_pos = at = 0
@@ -425,8 +436,8 @@ def rope_cache(q, k, v, positions, slots, table, k_cache, v_cache, q_out=None, i
 
 
 def attn_paged_workspace(q, k_cache, n_req: int, max_blocks=None):
-    """A zeroed workspace for attn_paged on batches of q's size over this cache (max_blocks: the block table's width, None:
-    any)."""
+    """A workspace for attn_paged on batches of q's size over this cache (max_blocks: the block table's width, None: any),
+    zeroed on the current stream."""
     n_pages, hk, page, d = k_cache.shape
     need = plora_attn_paged_workspace_bytes(max(1, q.shape[0]), int(n_req), q.shape[1], hk, d, page,
                                             n_pages if max_blocks is None else min(n_pages, int(max_blocks)))
@@ -447,11 +458,12 @@ def attn_paged(q, k_cache, v_cache, block_table, kv_len, scale: float, tok_start
     if q.dtype is not k_cache.dtype or cd != d or hk == 0 or hq % hk != 0:
         _bad("q and the caches do not agree")
     if out is None:
-        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+        out = (torch.empty((n, hq, d), dtype=q.dtype, device=q.device) if stream is None
+               else _new_on(stream, torch.empty, (n, hq, d), dtype=q.dtype, device=q.device))
     elif out.dtype is not q.dtype or out.shape != (n, hq, d) or not out.is_cuda or not out.is_contiguous():
         _bad("out: packed, of q's shape and type, expected")
     if workspace is None:
-        workspace = attn_paged_workspace(q, k_cache, n_req, width)
+        workspace = _new_on(stream, attn_paged_workspace, q, k_cache, n_req, width)
     elif workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
         _bad("workspace: packed uint8 CUDA tensor expected")
     if (group_start is None) != (prefix_len is None):

@@ -145,3 +145,38 @@ def test_units_of_few_rows_keep_their_weights(hq, hk, new, groups, dtype):
     tol = 1.02 * ROUND[dtype] * want.abs() + 2.0 ** -16 * mean + 2.0 ** -25      # (half a unit below the normal range: 2^-25)
     err = (got.double() - want).abs()
     assert bool((err <= tol).all()), float((err / tol).max())
+
+
+def test_what_a_call_allocates_belongs_to_its_stream(monkeypatch):
+    """With `stream` given, the workspace is zeroed and the outputs are made on that stream, whatever the current one is doing."""
+    made = []
+    for name in ("zeros", "empty"):
+        make = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, _make=make, **k: (made.append(torch.cuda.current_stream()), _make(*a, **k))[1])
+    b = Batch(38, [900, 50], [30, 1], hq=4, hk=2)
+    one = Batch(39, [900, 50], hq=4, hk=2)
+    refs = b.reference(), one.reference()
+    table, lens, free, blocks = P.rope_table(128, 8), _ints([3, 0]), _ints(range(9)), torch.zeros((2, 4), dtype=torch.int32, device=DEV)
+    y, pos = torch.randn(3, 4, 128, device=DEV), _ints([0, 1, 2])
+    kc = torch.zeros((1, 4, 16, 128), dtype=torch.bfloat16, device=DEV)
+    vc = torch.zeros_like(kc)
+    qd, kd = torch.randn(2, 4, 128, device=DEV).bfloat16(), torch.randn(2, 4, 64, 128, device=DEV).bfloat16()
+    len_d = _ints([64, 10])
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    made.clear()
+    torch.cuda._sleep(200_000_000)                   # (the current stream is busy for a tenth of a second)
+    outs = [P.attn_paged(x.q, x.K, x.V, x.table, x.kv_len, x.scale, tok_start=x.tok_start, stream=s) for x in (b, one)]
+    P.rope_table(128, 8, stream=s)
+    P.kv_plan(lens, lens, 16, free, blocks, 8, stream=s)
+    P.rope_cache(y, y, y, pos, pos, table, kc, vc, stream=s)
+    dec, _ = P.attn_decode(qd, kd, kd, len_d, 0.1, stream=s)
+    assert len(made) >= 9 and all(m == s for m in made)
+    s.synchronize()
+    for (out, ws), x, ref in zip(outs, (b, one), refs):
+        with torch.cuda.stream(s):
+            x.check(out, ref)
+        rc, status = P.plora_attn_status(ws.data_ptr(), s.cuda_stream)
+        assert rc == 0 and status == 0
+    torch.cuda.synchronize()
+    assert torch.equal(dec, P.attn_decode(qd, kd, kd, len_d, 0.1)[0])
