@@ -15,9 +15,20 @@ from pathlib import Path
 from typing import Any, NamedTuple
 
 import numpy as np
-import torch
 
 from . import _build
+
+
+class _Torch:
+    """Stands in for the module until the torch layer first needs it: the C ABI is used without torch, too."""
+
+    def __getattr__(self, name):
+        global torch
+        import torch
+        return getattr(torch, name)
+
+
+torch = _Torch()
 
 OK = 0
 ERR_INVALID_ARG = -1

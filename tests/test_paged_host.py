@@ -1,5 +1,8 @@
 """The paged cache's calls without a GPU: layouts of the argument structures, sizes, and refusals before anything is launched."""
 import ctypes
+import subprocess
+import sys
+from pathlib import Path
 
 import pytest
 import torch
@@ -95,3 +98,12 @@ def test_expanded_tensors_are_refused():
         binding._page_stride(cache(0), cache(0))
     assert binding._page_stride(cache(4096), cache(4096)) == 4096
     assert binding._page_stride(cache(0, 1), cache(0, 1)) == 2048
+
+
+def test_the_c_abi_is_used_without_torch():
+    code = ("import sys; sys.modules['torch'] = None\n"
+            "import paper_2608_05483_b200 as P\n"
+            "assert P.load() and P.status_string(P.OK) and P.plora_attn_paged_workspace_bytes(1, 1, 8, 8, 128, 16, 4) > 0\n"
+            "assert P.plora_attn_paged(P.PagedAttn()) == P.OK\n")
+    run = subprocess.run([sys.executable, "-c", code], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stderr[-2000:]
