@@ -474,9 +474,9 @@ PLORA_API plora_status plora_kv_plan(const int32_t *kv_len_dev, const int32_t *n
  *   LINEAR  f_i / factor (positions interpolated)
  *   NTK     base * factor^(rot_dim / (rot_dim - 2)) in place of base
  *   BANDS   by the number of turns n_i = orig_len f_i / 2 pi: f_i above `high`, f_i / factor below `low`,
- *           interpolated linearly in n_i between
+ *           interpolated linearly in n_i between (usually low 1, high 4)
  *   RAMP    f_i up to the pair that turns `high` times over orig_len, f_i / factor from the one that turns `low` times
- *           on, interpolated linearly in i between (pairs rounded outwards) */
+ *           on, interpolated linearly in i between (pairs rounded outwards; usually low 1, high 32) */
 #define PLORA_ROPE_NONE 0
 #define PLORA_ROPE_LINEAR 1
 #define PLORA_ROPE_NTK 2

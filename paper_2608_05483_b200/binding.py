@@ -397,11 +397,15 @@ _SCALINGS = {"none": ROPE_NONE, "linear": ROPE_LINEAR, "ntk": ROPE_NTK, "bands":
 
 
 def rope_table(rot_dim: int, max_pos: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
-               orig_len: float = 0.0, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0, device="cuda", stream=None):
-    """The fp32 table [max_pos, rot_dim // 2, 2] of cosines and sines (plora_rope_table)."""
+               orig_len: float = 0.0, low: float | None = None, high: float | None = None, magnitude: float = 1.0, device="cuda",
+               stream=None):
+    """The fp32 table [max_pos, rot_dim // 2, 2] of cosines and sines (plora_rope_table).  low and high, the turns over orig_len
+    between which "bands" and "ramp" change over: 1 and 4 for bands, 1 and 32 for a ramp unless given."""
     if scaling not in _SCALINGS:
         _bad(f"scaling: one of {sorted(_SCALINGS)} expected, got {scaling!r}")
     table = _new_on(stream, torch.empty, (max(0, int(max_pos)), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
+    low = 1.0 if low is None else low
+    high = (32.0 if scaling == "ramp" else 4.0) if high is None else high
     d = RopeDesc(int(rot_dim), _SCALINGS[scaling], base, factor, orig_len, low, high, magnitude)
     _check(plora_rope_table(d, int(max_pos), table.data_ptr(), _raw_stream(stream, table)), "plora_rope_table")
     return table

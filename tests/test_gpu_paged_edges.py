@@ -180,3 +180,10 @@ def test_what_a_call_allocates_belongs_to_its_stream(monkeypatch):
         assert rc == 0 and status == 0
     torch.cuda.synchronize()
     assert torch.equal(dec, P.attn_decode(qd, kd, kd, len_d, 0.1)[0])
+
+
+def test_each_scaling_has_its_own_default_turns():
+    kw = dict(rot_dim=128, max_pos=4000, factor=8.0, orig_len=4096.0)
+    for scaling, high in (("bands", 4.0), ("ramp", 32.0)):
+        assert torch.equal(P.rope_table(scaling=scaling, **kw), P.rope_table(scaling=scaling, low=1.0, high=high, **kw))
+    assert not torch.equal(P.rope_table(scaling="ramp", **kw), P.rope_table(scaling="ramp", low=1.0, high=4.0, **kw))
