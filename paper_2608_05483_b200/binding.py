@@ -454,7 +454,7 @@ def attn_paged_workspace(q, k_cache, n_req: int, max_blocks=None):
     """A workspace for attn_paged on batches of q's size over this cache (max_blocks: the block table's width, None: any),
     zeroed on the current stream."""
     n_pages, hk, page, d = k_cache.shape
-    need = plora_attn_paged_workspace_bytes(max(1, q.shape[0]), int(n_req), q.shape[1], hk, d, page,
+    need = plora_attn_paged_workspace_bytes(max(1, q.shape[0]), max(1, int(n_req)), q.shape[1], hk, d, page,
                                             n_pages if max_blocks is None else min(n_pages, int(max_blocks)))
     if need == 0:
         raise PloraError(ERR_UNSUPPORTED, "plora_attn_paged_workspace_bytes")

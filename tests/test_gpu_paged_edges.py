@@ -187,3 +187,17 @@ def test_each_scaling_has_its_own_default_turns():
     for scaling, high in (("bands", 4.0), ("ramp", 32.0)):
         assert torch.equal(P.rope_table(scaling=scaling, **kw), P.rope_table(scaling=scaling, low=1.0, high=high, **kw))
     assert not torch.equal(P.rope_table(scaling="ramp", **kw), P.rope_table(scaling="ramp", low=1.0, high=4.0, **kw))
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_a_step_without_requests(ragged):
+    none, table = _ints([]), torch.zeros((0, 5), dtype=torch.int32, device=DEV)
+    cache = torch.zeros((3, 2, 16, 64), dtype=torch.bfloat16, device=DEV)
+    q = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device=DEV)
+    p = P.kv_plan(none, none, 16, _ints([0, 1, 2]), table, 4)
+    assert p.tok_start.tolist() == [0] and p.cursor.tolist() == [0] and p.positions.tolist() == [-1] * 4
+    y = torch.zeros((0, 4, 64), device=DEV)
+    assert P.rope_cache(y, y[:, :2], y[:, :2], none, none, None, cache, cache.clone()).shape == (0, 4, 64)
+    out, _ = P.attn_paged(q, cache, cache.clone(), table, none, 1.0, tok_start=_ints([0]) if ragged else None)
+    torch.cuda.synchronize()
+    assert out.shape == (0, 4, 64)
