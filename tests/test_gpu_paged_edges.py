@@ -201,3 +201,73 @@ def test_a_step_without_requests(ragged):
     out, _ = P.attn_paged(q, cache, cache.clone(), table, none, 1.0, tok_start=_ints([0]) if ragged else None)
     torch.cuda.synchronize()
     assert out.shape == (0, 4, 64)
+
+
+def _check_norms(b, got, ref):
+    """Per token and head, the error against the output's norm: at most the output's rounding, u, and that of the weights, which
+    by random signs stays below u.  (Element by element the bound grows with the mean of |v|, while the output of n random
+    keys shrinks as n^-1/2: sixteen keys lost or doubled among nine thousand are 4 % of the norm, and within that bound.)"""
+    b.check(got, ref)
+    want = ref[0]
+    err, size = (got.double() - want).norm(dim=-1), want.norm(dim=-1)
+    # (weights below half's normal range are off by up to 2^-25 each, of either sign)
+    floor = (want.shape[-1] * max(b.kv)) ** 0.5 * 2.0 ** -25 if b.dtype is torch.float16 else 0.0
+    worst = ((err - floor) / size.clamp(min=1e-30)).max()
+    assert float(worst) <= 2 * ROUND[b.dtype], float(worst)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("kv,new,hq,hk,d,page", [
+    ([9001], None, 8, 1, 128, 64), ([9001], None, 32, 1, 64, 16), ([5000, 4999, 5008, 1], None, 2, 2, 128, 32),
+    ([9001], [128], 8, 1, 128, 64), ([9001, 4097], [40, 3], 8, 8, 64, 16), ([4200, 6000], [700, 2], 4, 1, 128, 128)])
+def test_no_key_of_a_long_cache_is_lost_or_read_twice(kv, new, hq, hk, d, page, dtype):
+    b = Batch(40, kv, new, hq=hq, hk=hk, d=d, page=page, dtype=dtype)
+    got = b.run()
+    _check_norms(b, got, b.reference())
+    with pytest.raises(AssertionError):      # (that the check would notice: sixteen keys fewer)
+        _check_norms(b, got, b.reference(key_lo=_ints([16] * b.tok[-1])))
+
+
+@pytest.mark.parametrize("n", [3, 60])
+def test_no_key_of_a_long_prefix_is_lost_or_read_twice(n):
+    prefix = 5003
+    b = Batch(41, [prefix + 37 * r for r in range(n)], hq=4, hk=2, page=32, groups=[0, n], prefix=[prefix])
+    _check_norms(b, b.run([0, n], [prefix]), b.reference())
+
+
+@pytest.mark.parametrize("n", [255, 256, 257, 1024, 1100])
+def test_many_single_tokens(n):
+    """Up to 256 the attention kernel deals them out itself, beyond that the plan does, and from 1025 on in two rounds."""
+    b = Batch(42, [(r * 29) % 41 for r in range(n)], hq=4, hk=2, d=64, page=16)
+    _check_norms(b, b.run(), b.reference())
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_more_ragged_requests_than_the_plan_has_threads(masked):
+    n = 1500
+    new = [r % 4 for r in range(n)]
+    kv = [x + (r * 7) % 30 for r, x in enumerate(new)]
+    for r in (3, 1023, 1024, 1300, 1499):                # long ones on both sides of the rounds' border
+        new[r], kv[r] = 150, 400
+    b = Batch(43, kv, new, hq=4, hk=2, d=64, page=16)
+    kw = {}
+    if masked:
+        pos = torch.cat([torch.arange(k - x, k) for x, k in zip(new, kv)])
+        kw = dict(key_lo=(pos - 20).clamp(min=0).to(torch.int32).to(DEV), key_hi=(pos + 3).to(torch.int32).to(DEV))
+    _check_norms(b, b.run(**kw), b.reference(**kw))
+
+
+def test_more_prompts_than_the_plan_writes_by_warps():
+    n = 300
+    b = Batch(44, [20 + r % 50 for r in range(n)], [17 + r % 4 for r in range(n)], hq=2, hk=1, d=64, page=16)
+    _check_norms(b, b.run(), b.reference())
+
+
+def test_more_groups_than_the_plan_holds():
+    starts, prefix = [0], []
+    for g in range(2100):
+        starts.append(starts[-1] + (40 if g in (5, 1500, 2099) else 2 + g % 2))
+        prefix.append(16 * (g % 3) + g % 5)
+    kv = [p + (r * 13) % 23 for g, p in enumerate(prefix) for r in range(starts[g], starts[g + 1])]
+    b = Batch(45, kv, hq=2, hk=1, d=64, page=16, groups=starts, prefix=prefix)
+    _check_norms(b, b.run(starts, prefix), b.reference())
