@@ -10,7 +10,8 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libplora_b200.so"
-# the same sources compiled with -DPLORA_DEBUG: every address a kernel forms is checked against its buffer
+# the same sources compiled with -DPLORA_DEBUG: every address that the delta kernels and the paged attention form is checked
+# against its buffer
 LIB_DEBUG = PKG / "libplora_b200_debug.so"
 OBJ_DIR = PKG / "build"
 

@@ -112,7 +112,8 @@ _lib = None
 
 def _debug_build() -> bool:
     """PLORA_DEBUG_BUILD=1 in the environment selects the checked build of the library (same sources compiled with
-    -DPLORA_DEBUG: kernels check every address against its buffer and report PLORA_ERR_DEBUG_CHECK)."""
+    -DPLORA_DEBUG: the delta kernels and the paged attention check every address against its buffer and report
+    PLORA_ERR_DEBUG_CHECK)."""
     import os
     return os.environ.get("PLORA_DEBUG_BUILD", "") == "1"
 

@@ -18,6 +18,7 @@
 #include <atomic>
 
 #include "plora.h"
+#include "plora_internal.cuh"
 
 namespace plora {
 namespace paged {
@@ -81,6 +82,27 @@ struct Params {
     float cap_poly_below;
     float cap_in, cap_log2e;  // cap_in = 2 log2(e) * scale / softcap
 };
+
+// Debug build: a unit whose tokens, keys or partial results lie outside the call's is reported and becomes one without tokens.
+__device__ __forceinline__ Unit checked(const Params& p, const Unit& u) {
+#ifdef PLORA_DEBUG
+    const bool tokens = u.tok0 >= 0 && u.ntok >= 0 && u.ntok <= p.n_tok - u.tok0, keys = u.k0 >= 0 && u.k0 <= u.k1 && u.k1 <= p.max_kv;
+    if (!tokens || !keys || u.req < 0 || u.req >= p.n_req || (u.part >= 0 && u.ntok > p.cap_part - u.part)) {
+        atomicCAS(p.header, 0, PLORA_ERR_DEBUG_CHECK);
+        return Unit{0, 0, 0, 0, 0, -1, {0, 0}};
+    }
+#endif
+    return u;
+}
+// Where rows of the output and of the partial results lie (debug build: one that does not exist is reported).
+__device__ __forceinline__ bool row_exists(const Params& p, int i, bool partial) {
+#ifdef PLORA_DEBUG
+    PLORA_CHECKED(i >= 0 && i < (partial ? p.cap_part : p.n_tok), p.header) return true;
+    return false;
+#else
+    return true;
+#endif
+}
 
 constexpr int kSmallRows = 16;     // rows of a unit the mma.sync kernel takes
 constexpr int kSelfRequests = 256; // requests of single tokens that the mma.sync kernel deals out by itself

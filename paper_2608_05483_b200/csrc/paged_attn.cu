@@ -295,7 +295,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
     if (per_b > kBigOneRound) per_b = max((long long)kBigOneRound, (keys_b * p.n_kv_heads + kBigItems - 1) / kBigItems);
     const int chunk_b = (int)min((long long)kBigMaxKeys, max((long long)kBigMinKeys, (per_b + 127) / 128 * 128));
     auto splits_of = [&](int keys, bool small) { const int c = small ? chunk_s : chunk_b; return (keys + c - 1) / c; };
-    auto put = [&](bool small, int i, const Unit& u) { (small ? p.small_units : p.big_units)[i] = u; };
+    auto put = [&](bool small, int i, const Unit& u) {
+        PLORA_CHECKED(i >= 0 && i < (small ? p.cap_small : p.cap_big), p.header) (small ? p.small_units : p.big_units)[i] = checked(p, u);
+    };
 
     Sums carry{0, 0, 0}, total;
     // the groups' prefixes: always partial results
@@ -321,7 +323,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
                     put(small, (small ? at.small : at.big) + b * splits + i,
                         Unit{tok0 + b * TB, nt, s, i * chunk, min(pre, (i + 1) * chunk), at.part + i * n + b * TB, {0, 0}});
             }
-            for (int t = 0; t < n; ++t) p.tok_prefix[tok0 + t] = make_int4(at.part + t, splits, n, 0);
+            for (int t = 0; t < n; ++t)
+                if (row_exists(p, tok0 + t, false)) p.tok_prefix[tok0 + t] = make_int4(at.part + t, splits, n, 0);
         }
         carry = carry + total;
     }
@@ -353,7 +356,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const Params p) {
         // lists a token for the merge: `splits` partial results of its own keys from `part` on, `stride` apart, and its prefix's
         auto list = [&](int tok, int at, int part, int splits, int stride, int pre_keys) {
             const int4 pre = pre_keys > 0 ? p.tok_prefix[tok] : make_int4(0, 0, 0, 0);
-            p.tok_merge[at] = TokMerge{tok, {part, pre.x}, {splits, pre.y}, {stride, pre.z}, 0};
+            if (row_exists(p, at, false)) p.tok_merge[at] = TokMerge{tok, {part, pre.x}, {splits, pre.y}, {stride, pre.z}, 0};
         };
         // writes the units of one block, and lists its tokens if they need a merge
         auto write_block = [&](const Req& q, int r, int b, bool small, int splits, int k0, int k1, int unit, int part) {
@@ -472,7 +475,8 @@ __global__ void __launch_bounds__(128) merge_kernel(const Params p) {
             float2 ml = make_float2(-INFINITY, 0.f);
             if (i < n) {
                 at = i < tm.n[0] ? tm.base[0] + i * tm.stride[0] : tm.base[1] + (i - tm.n[0]) * tm.stride[1];
-                ml = p.part_ml[(size_t)at * p.n_q_heads + hq];
+                if (row_exists(p, at, true)) ml = p.part_ml[(size_t)at * p.n_q_heads + hq];
+                else at = 0;
             }
             float m = ml.x;
 #pragma unroll
@@ -495,7 +499,7 @@ __global__ void __launch_bounds__(128) merge_kernel(const Params p) {
                 }
             }
         }
-        if (live) {
+        if (live && row_exists(p, tm.tok, false)) {
             const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);    // nothing visible: a zero row
             *reinterpret_cast<uint2*>(p.out + ((size_t)tm.tok * p.n_q_heads + hq) * D + sub * 4) =
                 make_uint2(pack16<FP16>(o.x * inv, o.y * inv), pack16<FP16>(o.z * inv, o.w * inv));

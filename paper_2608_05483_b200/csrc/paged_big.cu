@@ -201,7 +201,7 @@ __device__ __forceinline__ void item_warp(const Params& p, const Smem& sm, const
         if (more) {
             if (lane == 0) next = atomicAdd(p.header + kBigNextWord, 1);
             const int un = item / p.n_kv_heads;
-            const Unit u = p.big_units[un];
+            const Unit u = checked(p, p.big_units[un]);
             d.head = item - un * p.n_kv_heads;
             d.tok0 = u.tok0; d.ntok = u.ntok; d.req = u.req; d.part = u.part;
             // the keys that one of the tokens sees, for each tile of rows
@@ -292,7 +292,9 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
         const int32_t* table = p.block_table + (size_t)req * p.max_blocks;
         auto page_of = [&](int j) {              // the page of this lane's piece of key tile j
             const int key = kf + j * kTileKeys + lane * bp;
-            return lane < kTileKeys / bp && key < k1 ? table[key >> p.page_shift] : 0;
+            int page = 0;
+            if (lane < kTileKeys / bp && key < k1) PLORA_CHECKED(key < p.max_kv, p.header) page = table[key >> p.page_shift];
+            return page;
         };
         int page_next = page_of(0);
 #pragma unroll 1
@@ -654,7 +656,8 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
         }
         const float inv = m == -INFINITY ? 0.f : 1.f / l;              // nothing visible: a zero row
         const size_t at = (size_t)((d.part < 0 ? d.tok0 : d.part) + rel) * p.n_q_heads + hq;
-        if (mine && d.part >= 0) p.part_ml[at] = make_float2(m, l);
+        const bool writes = mine && row_exists(p, (d.part < 0 ? d.tok0 : d.part) + rel, d.part >= 0);
+        if (writes && d.part >= 0) p.part_ml[at] = make_float2(m, l);
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
             uint32_t o[32];
@@ -665,7 +668,7 @@ __device__ __forceinline__ void softmax_warp(const Params& p, const Smem& sm, ui
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = 0u;
             }
-            if (!mine) continue;
+            if (!writes) continue;
             // (32 bytes per lane and store: the rows lie far apart, and the store unit is paced by the lines it touches)
             if (d.part < 0) {
                 uint16_t* dst = p.out + at * D + c * 32;

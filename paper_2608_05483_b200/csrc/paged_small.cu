@@ -189,6 +189,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 const int4 a = __ldcg(reinterpret_cast<const int4*>(p.small_units + un)), b = __ldcg(reinterpret_cast<const int4*>(p.small_units + un) + 1);
                 u = Unit{a.x, a.y, a.z, a.w, b.x, b.y, {0, 0}};
             }
+            u = checked(p, u);
             const int rows = u.ntok * p.G;
             // this lane's row: what it may see, and where its query lies
             float slope = 0.f;
@@ -224,7 +225,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 int page = 0;
                 const int my_key = key + lane * bp;
                 if (lane < nb) {
-                    page = __ldcg(table + (my_key >> p.page_shift));
+                    PLORA_CHECKED(my_key < p.max_kv, p.header) page = __ldcg(table + (my_key >> p.page_shift));
                     if ((unsigned)page >= (unsigned)p.n_pages) {   // such a page reads as zeros
                         atomicCAS(p.header, 0, PLORA_ERR_INVALID_ARG);
                         page = p.n_pages;
@@ -457,6 +458,7 @@ small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                         O.x = fmaf(f, ow.x, O.x); O.y = fmaf(f, ow.y, O.y); O.z = fmaf(f, ow.z, O.z); O.w = fmaf(f, ow.w, O.w);
                     }
                     const int tr = r / p.G, hq = (int)h.y * p.G + r % p.G;
+                    if (!row_exists(p, part < 0 ? tok0 + tr : part + tr, part >= 0)) continue;
                     if (part < 0) {
                         const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);   // nothing visible: a zero row
                         uint2 w2 = make_uint2(pack16<FP16>(O.x * inv, O.y * inv), pack16<FP16>(O.z * inv, O.w * inv));
