@@ -243,7 +243,12 @@ __device__ __forceinline__ void store(T* p, int ia, int ib, const float (&f)[2 *
     *reinterpret_cast<Vec<T, V>*>(p + ib) = b;
 }
 
-// WIDE: bases and strides are multiples of 32 bytes.
+// WIDE (interleaved pairs only): bases and strides are multiples of 32 bytes, and a chunk's two runs, which lie together, go in
+// one access.  Measured against two of 16 bytes: 16384 tokens of 64/8 heads, 64 of 128 dims, 122 and 126 us; 8192 of 32/32, bf16,
+// 77 and 80; 4096 of 32/8, fp32 in, 30.5 and 31.8.  With halves only v and what passes through have such runs, and it was no
+// faster (16384 of 32/8: 43 and 42 at 64 dims, 85 and 83 at 128).
+// Eight CTAs per SM, although the forms of 8 values then spill 8 to 20 bytes: with six, and no spills, the first takes
+// 136 us and the second 86; what counts is the loads under way (fp32 input would be some 6 % faster with six).
 template <typename TI, typename TO, int V, bool INTER, bool WIDE>
 __global__ void __launch_bounds__(256, 8) rope_kernel(const RopeParams p) {
     // the block's first chunk: one 64-bit division for the block, small ones for the threads
@@ -326,7 +331,7 @@ cudaError_t rope_go(const RopeParams& p, bool inter, cudaStream_t st) {
     // (an ordinary launch: waiting for the kernel before costs every CTA some hundred cycles, and these live for two thousand)
     const unsigned grid = (unsigned)((n + 255) / 256);
     if (inter) rope_kernel<TI, TO, V, true, WIDE><<<grid, 256, 0, st>>>(p);
-    else rope_kernel<TI, TO, V, false, WIDE><<<grid, 256, 0, st>>>(p);
+    else rope_kernel<TI, TO, V, false, false><<<grid, 256, 0, st>>>(p);
     return cudaGetLastError();
 }
 template <typename TI, typename TO>
@@ -438,10 +443,10 @@ extern "C" PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args* 
     if (((long long)p.n_tok * p.per_tok + 255) / 256 > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
     // 32-byte accesses where the runs lie together (16 values of a 16-bit type): every base and stride has to allow them
     const int W = 32 / (int)es;
-    const bool wide = V == 8 && p.q_stride % W == 0 && p.k_stride % W == 0 && p.v_stride % W == 0 && p.page_stride % 16 == 0 &&
+    const bool inter = a->layout == PLORA_ROPE_INTERLEAVED;
+    const bool wide = inter && V == 8 && p.q_stride % W == 0 && p.k_stride % W == 0 && p.v_stride % W == 0 && p.page_stride % 16 == 0 &&
                       a->head_dim % 16 == 0 && a->rot_dim % 16 == 0 && aligned(a->q, 32) && aligned(a->k, 32) && aligned(a->v, 32) &&
                       aligned(a->q_out, 32) && aligned(a->k_cache, 32) && aligned(a->v_cache, 32);
-    const bool inter = a->layout == PLORA_ROPE_INTERLEAVED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool f32 = a->in_type == PLORA_INPUT_FP32;
     cudaError_t e;
