@@ -106,8 +106,8 @@ __device__ __forceinline__ bool row_exists(const Params& p, int i, bool partial)
 
 constexpr int kSmallRows = 16;     // rows of a unit the mma.sync kernel takes
 // Requests of single tokens that the mma.sync kernel deals out by itself.  Against the plan kernel (us, self-dealt / planned; 64/8
-// heads): 1 request of some 1000 keys 11.1 / 14.5, 32: 39 / 45, 128: 106 / 107, 256: 192 / 184; 256 of some 100 keys 42 / 45,
-// of 1000 with one KV head 40 / 54.  Arrays for more (1024) cost every call 10 us and more.
+// heads): 1 request of some 1000 keys 10.8 / 14.0, 32: 38 / 44, 128: 106 / 106, 256: 193 / 185; 256 of some 100 keys 39 / 44,
+// of 1000 with one KV head 40 / 53.  Arrays for more (1024) cost every call 10 us and more.
 constexpr int kSelfRequests = 256;
 constexpr int kBigRows = 128;      // rows of a tile of the tensor-core kernel; a unit has up to two tiles
 
