@@ -272,6 +272,22 @@ __device__ __forceinline__ void item_warp(const Params& p, const Smem& sm, const
     __syncwarp();
 }
 
+// When both loaders have stopped: the copies still in flight must land before the CTA leaves (after a wait that ran out, up to
+// all of a ring may be).  A lane per stage looks at what was sent there last; only then does a phase tell the copy, for
+// the two loaders share the ring, and the one that stops first does not know which stages the other has filled again.
+template <int D>
+__device__ __forceinline__ void drain_ring(const Params& p, const Smem& sm, int lane) {
+    constexpr uint32_t kStages = Cfg<D>::kStages;
+    int last = -1;                           // (stages are numbered through, K even, V odd; a loader has filled all of its below filled[])
+#pragma unroll 1
+    for (int i = 0; i < 2 * (int)kStages; ++i) {
+        const int x = (int)sm.filled[i & 1] - 2 - (i & ~1);
+        if (lane < (int)kStages && x >= 0 && x % (int)kStages == lane) last = max(last, x);
+    }
+    if (last >= 0 && !mbar_drain(sm.kv_full + lane * 8, (last / (int)kStages) & 1, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
+    __syncwarp();
+}
+
 // ---- warps 9 and 13: keys, values ------------------------------------------------------------------------------------
 // A warp each: with pages of 16 tokens a tile is 16 boxes.  As with the MMAs, the warp stays together and an elected lane
 // issues (a copy that every lane issues for itself cost 100 to 200 cycles).
@@ -328,23 +344,9 @@ __device__ __forceinline__ void load_warp(const Params& p, const Smem& sm, const
     }
     if (lane == 0) sm.filled[kv] = it;
     __syncwarp();
+    asm volatile("bar.sync 1, 64;" ::: "memory");       // (the two loaders; their waits are bounded, so both get here)
+    if (kv == 0) drain_ring<D>(p, sm, lane);
 }
-// When both loaders have stopped: the copies still in flight must land before the CTA leaves (after a wait that ran out, up to
-// all of a ring may be).  A lane per stage looks at what was sent there last; only then does a phase tell the copy, for
-// the two loaders share the ring, and the one that stops first does not know which stages the other has filled again.
-template <int D>
-__device__ __forceinline__ void drain_ring(const Params& p, const Smem& sm, int lane) {
-    constexpr uint32_t kStages = Cfg<D>::kStages;
-    int last = -1;                           // (stages are numbered through, K even, V odd; a loader has filled all of its below filled[])
-#pragma unroll 1
-    for (int i = 0; i < 2 * (int)kStages; ++i) {
-        const int x = (int)sm.filled[i & 1] - 2 - (i & ~1);
-        if (lane < (int)kStages && x >= 0 && x % (int)kStages == lane) last = max(last, x);
-    }
-    if (last >= 0 && !mbar_drain(sm.kv_full + lane * 8, (last / (int)kStages) & 1, wait_limit(p.header))) atomicCAS(p.header, 0, PLORA_ERR_TIMEOUT);
-    __syncwarp();
-}
-
 // ---- warp 8: the products ---------------------------------------------------------------------------------------
 // The warp stays together and one elected lane issues: the MMA's operands are uniform registers, and under a plain
 // `lane == 0` the compiler cannot know that a single lane is active (an MMA then cost the issuer about 100 cycles, more
@@ -750,7 +752,6 @@ big_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == kKeyWarp) drain_ring<D>(p, sm, lane);
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
