@@ -535,8 +535,8 @@ PLORA_API plora_status plora_rope_cache(const plora_rope_cache_args *args, void 
  *            The result does not depend on the grouping beyond rounding.  n_groups = 0: none.
  *            tok_start and group_start have to ascend (equal entries: a request without tokens, a group without requests); if
  *            one does not, nothing is computed and the status word gets PLORA_ERR_INVALID_ARG.  n_groups <= n_req.
- * type       PLORA_INPUT_BF16 / FP16 of q, K, V and out; products and sums in fp32, weights rounded to the type for the
- *            second product.
+ * type       PLORA_INPUT_BF16 / FP16 of q, K, V and out; products and sums in fp32.  Weights are rounded to the type for the
+ *            second product; with up to 16 query rows per KV head and unit (single tokens) they keep 16 bits or more.
  * q [n_tok][n_q_heads][head_dim] (q_stride elements between tokens, 0: packed), out packed; query head h reads KV
  * head h / (n_q_heads / n_kv_heads).  head_dim 64 or 128; page_size 16, 32, 64 or 128; at most 128 query heads per KV
  * head.  q, K, V and out 16-byte aligned, strides multiples of 8.  Cache slots at or beyond kv_len may hold anything; below

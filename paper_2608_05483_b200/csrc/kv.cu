@@ -247,8 +247,8 @@ __device__ __forceinline__ void store(T* p, int ia, int ib, const float (&f)[2 *
 // one access.  Measured against two of 16 bytes: 16384 tokens of 64/8 heads, 64 of 128 dims, 122 and 126 us; 8192 of 32/32, bf16,
 // 77 and 80; 4096 of 32/8, fp32 in, 30.5 and 31.8.  With halves only v and what passes through have such runs, and it was no
 // faster (16384 of 32/8: 43 and 42 at 64 dims, 85 and 83 at 128).
-// Eight CTAs per SM, although the forms of 8 values then spill 8 to 20 bytes: with six, and no spills, the first takes
-// 136 us and the second 86; what counts is the loads under way (fp32 input would be some 6 % faster with six).
+// Eight CTAs per SM, although eight of the twelve forms of 8 values then spill 8 to 20 bytes: with six and no spills the first
+// takes 136 us and the second 86; what counts is the loads under way.  (Interleaved fp32 input would be some 6 % faster.)
 template <typename TI, typename TO, int V, bool INTER, bool WIDE>
 __global__ void __launch_bounds__(256, 8) rope_kernel(const RopeParams p) {
     // the block's first chunk: one 64-bit division for the block, small ones for the threads

@@ -6,7 +6,7 @@
 // piece, into 128-byte-swizzled rows) through a ring; four consumer warps take 16 tokens of every
 // tile each: S = Q K^T and O += P V by mma.sync with the unit's rows as the 16-row operand, an online
 // softmax per warp in 32 bits.  (The legacy tensor instruction fits: its operands stay in registers, and at
-// 16 rows the tensor pipe is idle nine tenths of the time anyway.)  At the end of an item the warps' (m, l, o)
+// 16 rows the tensor pipe is idle four fifths of the time anyway.)  At the end of an item the warps' (m, l, o)
 // meet in shared memory.
 // The weights P enter the second product in two parts of the input type, the rounded value and the rest (16 bits of a bf16
 // weight, 22 of a half one, so that the output's own rounding is what is left of the error, as in plora_attn_decode).  With at
