@@ -1,4 +1,4 @@
-"""Attention over the paged cache at the edges of its plan: lists that run full, ranges and numbers at their limits."""
+"""The paged cache's calls at their edges: plans of any size, ranges and numbers at their limits, accuracy, streams, empty steps."""
 import pytest
 import torch
 
