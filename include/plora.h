@@ -565,6 +565,82 @@ PLORA_API size_t plora_attn_paged_workspace_bytes(int32_t n_tok, int32_t n_req, 
                                                   int32_t head_dim, int32_t page_size, int32_t max_blocks);
 PLORA_API plora_status plora_attn_paged(const plora_paged_attn *args, void *stream);
 
+/* ---- A layer's base projections in 8 bits -----------------------------------------------------------------
+ * (No counterpart in the paper, which takes the base model's products as given.)  These calls make the fp32 y that
+ * plora_lora_delta adds to, and what stands between: norm, activation, and their 8-bit results.
+ *
+ * An 8-bit matrix is a matrix of e4m3 values q (largest 448) with fp32 scales; it stands for s * q.
+ *   activations  q [rows][cols] (rows `stride` bytes apart), scale [rows][ceil(cols / 128)]: one per 128 columns of a row
+ *   weights      q [n][k], scale [ceil(n / 128)][ceil(k / 128)]: one per 128 x 128; n is d_out, k is d_in
+ * q is 16-byte aligned, its stride a multiple of 16 (0: cols rounded up to 16); bytes between the columns' end and the stride
+ * are neither read as values nor written.  Scales are packed.  The calls below that make 8-bit matrices take
+ * s = max(max|v| / 448, 2^-126) over the block and round v / s to nearest even (v / s is good to a few 2^-24; a NaN or an infinity
+ * in a block makes its scale one).
+ *
+ * plora_rms_norm:  h = x + residual;  v = h * rsqrt(mean(h^2) + eps) * (weight + offset)  per row of d columns, in fp32.
+ *   x                       in_type: PLORA_INPUT_FP32 (the deltas' y), or the same as type
+ *   weight                  [d], weight_type fp32 or type; NULL: ones
+ *   residual, residual_out  residual_type fp32 or type; both or neither.  residual_out = h, rounded to residual_type; may be
+ *                           residual itself (with the same stride).  v is made of the h that is not rounded.
+ *   y                       v rounded to type (bf16 or IEEE half), or NULL; may be x itself if in_type == type
+ *   q, scale                v as an 8-bit matrix, or both NULL
+ * At least one of y, q, residual_out.  d <= 32768.  Strides count elements (q's: bytes); 0 means packed.  Any strides and
+ * alignments of whole elements work (q excepted); where all rows are 16-byte aligned (fp32: 32) and d is a multiple of 8
+ * the accesses are wide.  The first 16 rows or 16000 give the same bits for a row. */
+typedef struct {
+    int32_t in_type, type, weight_type, residual_type, n, d;
+    int64_t x_stride, residual_stride, residual_out_stride, y_stride, q_stride;
+    const void *x, *weight, *residual;
+    void *residual_out, *y, *q;
+    float *scale;
+    float eps, offset;
+} plora_rms_norm_args;
+PLORA_API plora_status plora_rms_norm(const plora_rms_norm_args *args, void *stream);
+
+/* v = act(gate) * up, or act(gate) if up is NULL, per element in fp32; y, q and scale as above.
+ * SILU: v / (1 + e^-v).  GELU: its tanh form, v / 2 (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))).  NONE: v itself (with up NULL: the
+ * 8-bit form of what is already there, the attention's output for instance).  Results of SILU and GELU below 2^-119 of up may be zero.  gate and up have one type and may be parts of one
+ * fused row. */
+#define PLORA_ACT_NONE 0
+#define PLORA_ACT_SILU 1
+#define PLORA_ACT_GELU 2
+typedef struct {
+    int32_t in_type, type, act, n, d;
+    int64_t gate_stride, up_stride, y_stride, q_stride;
+    const void *gate, *up;
+    void *y, *q;
+    float *scale;
+} plora_gated_act_args;
+PLORA_API plora_status plora_gated_act(const plora_gated_act_args *args, void *stream);
+
+/* A weight [n][k] of type bf16, fp16 or fp32 (rows w_stride elements apart, 0: packed) as an 8-bit matrix: a set-up call. */
+PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32_t n, int32_t k, int64_t w_stride, void *q_dev,
+                                          int64_t q_stride, float *scale_dev, void *stream);
+
+/* out_i [m][n_i] = x w_i^T for the 8-bit activations x [m][k] and 1 to 4 8-bit weights w_i [n_i][k] that share them (q, k and v;
+ * gate and up), in one launch:
+ *     out[r][c] = sum_b x_scale[r][b] w_scale[c / 128][b] sum_{k in block b} x[r][k] w[c][k]
+ * Sums in fp32, rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
+ * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; 32-byte aligned
+ * rows are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1.
+ * The weights are read before the kernel in front has completed if that kernel is one of this library's: they have to be complete
+ * before it begins (weights made by plora_quant_weight, copies or any other library's kernels always are).
+ * The kernel takes up to all 512 tensor-memory columns of an SM; as with plora_lora_delta's tensor-core path, do not run it
+ * beside a kernel that holds tensor memory for its whole lifetime and itself waits for this call.
+ * status  device int32 or NULL: a sticky word that gets PLORA_ERR_TIMEOUT if a bounded device-side wait ran out. */
+typedef struct {
+    int32_t out_type, m, k, n_weights;
+    int32_t n[4];
+    int64_t x_stride, w_stride[4], out_stride[4];
+    const void *x;
+    const float *x_scale;
+    const void *w[4];
+    const float *w_scale[4];
+    void *out[4];
+    int32_t *status;
+} plora_gemm_fp8_args;
+PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

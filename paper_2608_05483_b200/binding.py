@@ -50,11 +50,13 @@ EXPORTS = (
     "plora_cost_model", "plora_attn_workspace_bytes", "plora_attn_decode", "plora_attn_status", "plora_attn_set_debug",
     "plora_set_wait_limit", "plora_set_test_hook", "plora_set_inputs_resident", "plora_stream_read",
     "plora_kv_plan", "plora_rope_table", "plora_rope_cache", "plora_attn_paged_workspace_bytes", "plora_attn_paged",
+    "plora_rms_norm", "plora_gated_act", "plora_quant_weight", "plora_gemm_fp8",
 )
 
 INPUT_BF16, INPUT_FP16, INPUT_FP32 = 0, 1, 2
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_NONE, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
+ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
 
 HOOK_NONE, HOOK_WITHHOLD_RELEASE, HOOK_MAX_CYCLES = 0, 1, 1 << 24
 
@@ -99,6 +101,26 @@ class PagedAttn(ctypes.Structure):
                                                   "prefix_len", "key_lo", "key_hi", "slopes")]
                 + [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("out", ctypes.c_void_p),
                    ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)])
+
+
+class RmsNormArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("in_type", "type", "weight_type", "residual_type", "n", "d")]
+                + [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "y_stride", "q_stride")]
+                + [(n, ctypes.c_void_p) for n in ("x", "weight", "residual", "residual_out", "y", "q", "scale")]
+                + [("eps", ctypes.c_float), ("offset", ctypes.c_float)])
+
+
+class GatedActArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("in_type", "type", "act", "n", "d")]
+                + [(n, ctypes.c_int64) for n in ("gate_stride", "up_stride", "y_stride", "q_stride")]
+                + [(n, ctypes.c_void_p) for n in ("gate", "up", "y", "q", "scale")])
+
+
+class GemmFp8Args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("out_type", "m", "k", "n_weights")]
+                + [("n", ctypes.c_int32 * 4), ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64 * 4),
+                   ("out_stride", ctypes.c_int64 * 4), ("x", ctypes.c_void_p), ("x_scale", ctypes.c_void_p), ("w", ctypes.c_void_p * 4),
+                   ("w_scale", ctypes.c_void_p * 4), ("out", ctypes.c_void_p * 4), ("status", ctypes.c_void_p)])
 
 
 class PloraError(RuntimeError):
@@ -172,6 +194,10 @@ def load(build_if_missing: bool = True):
         "plora_rope_cache": (i32, [vp, vp]),
         "plora_attn_paged_workspace_bytes": (ctypes.c_size_t, [i32] * 7),
         "plora_attn_paged": (i32, [vp, vp]),
+        "plora_rms_norm": (i32, [vp, vp]),
+        "plora_gated_act": (i32, [vp, vp]),
+        "plora_quant_weight": (i32, [vp, i32, i32, i32, i64, vp, i64, vp, vp]),
+        "plora_gemm_fp8": (i32, [vp, vp]),
     }
     for name in EXPORTS:
         fn = getattr(lib, name)  # AttributeError here = the library does not export what the header declares
@@ -249,7 +275,8 @@ def plora_stream_read(buf_ptr, nbytes: int, sink_ptr, sink_bytes: int, stream=0)
 def _new_on(stream, make, *size, **kw):
     """A tensor made on the stream that the call runs on: zeroed before the kernels read it, and its memory handed on only
     behind them."""
-    import torch
+    if stream is None:
+        return make(*size, **kw)
     with torch.cuda.stream(stream):
         return make(*size, **kw)
 
@@ -499,6 +526,236 @@ def attn_paged(q, k_cache, v_cache, block_table, kv_len, scale: float, tok_start
     if rc != OK:
         raise PloraError(rc, "plora_attn_paged")
     return out, workspace
+
+
+# ---- a layer's base projections in 8 bits -------------------------------------------------
+def plora_rms_norm(args: RmsNormArgs, stream=0):
+    return load().plora_rms_norm(ctypes.byref(args), stream)
+
+
+def plora_gated_act(args: GatedActArgs, stream=0):
+    return load().plora_gated_act(ctypes.byref(args), stream)
+
+
+def plora_quant_weight(w_ptr, type_, n, k, w_stride, q_ptr, q_stride, scale_ptr, stream=0):
+    return load().plora_quant_weight(w_ptr, type_, n, k, w_stride, q_ptr, q_stride, scale_ptr, stream)
+
+
+def plora_gemm_fp8(args: GemmFp8Args, stream=0):
+    return load().plora_gemm_fp8(ctypes.byref(args), stream)
+
+
+class Act8(NamedTuple):
+    """What rms_norm and gated_act write: y [n, d] in 16 bits, q [n, d] e4m3 with scale [n, ceil(d / 128)], the residual sum (each
+    None where it was not asked for)."""
+    y: Any
+    q: Any
+    scale: Any
+    residual: Any = None
+
+
+# (packed as RmsNormArgs, GatedActArgs and GemmFp8Args are laid out)
+_NORM_PACK = struct.Struct("@6i5q7P2f")
+_ACT_PACK = struct.Struct("@5i4x4q5P")
+_GEMM_PACK = struct.Struct("@8i9q15P")
+
+
+def _type_of(name, t) -> int:
+    if t.dtype is torch.bfloat16:
+        return INPUT_BF16
+    if t.dtype is torch.float32:
+        return INPUT_FP32
+    if t.dtype is torch.float16:
+        return INPUT_FP16
+    _bad(f"{name}: float32, bfloat16 or float16 expected, got {t.dtype}")
+
+
+def _rows(name, t, n: int, d: int, dev: int) -> int:
+    """Elements between the rows of a CUDA tensor [n, d] whose rows are packed."""
+    if t.shape != (n, d) or not t.is_cuda or t.get_device() != dev:
+        _bad(f"{name}: CUDA tensor [{n}, {d}] on the inputs' device expected, got {list(t.shape)} on {t.device}")
+    st, one = t.stride()
+    if one != 1 and d > 1:
+        _bad(f"{name}: packed rows expected")
+    if n < 2:
+        return d
+    if st < d:       # (the C structures read 0 as packed; rows that overlap are not rows)
+        _bad(f"{name}: a tensor that is expanded along its rows is not supported")
+    return st
+
+
+def _q_rows(name, q, n: int, d: int, dev: int) -> int:
+    """Bytes between the rows of an e4m3 CUDA tensor [n, d]."""
+    if q.dtype is not torch.float8_e4m3fn:
+        _bad(f"{name}: float8_e4m3fn expected, got {q.dtype}")
+    st = _rows(name, q, n, d, dev)
+    if n < 2:
+        return -(-d // 16) * 16
+    if st % 16:
+        _bad(f"{name}: rows have to lie a multiple of 16 bytes apart")
+    return st
+
+
+def _scales(name, t, rows: int, cols: int, dev: int) -> int:
+    if t.dtype is not torch.float32 or t.shape != (rows, cols) or not t.is_cuda or not t.is_contiguous() or t.get_device() != dev:
+        _bad(f"{name}: packed float32 CUDA tensor {[rows, cols]} on the inputs' device expected, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _q_empty(stream, n: int, d: int, device):
+    """An 8-bit matrix's buffers: rows a multiple of 16 bytes apart."""
+    width = -(-d // 16) * 16
+    q = _new_on(stream, torch.empty, (n, width), dtype=torch.float8_e4m3fn, device=device)
+    scale = _new_on(stream, torch.empty, (n, -(-d // 128)), dtype=torch.float32, device=device)
+    return (q if width == d else q[:, :d]), scale
+
+
+def _call_on(dev: int, fn, args, stream, t) -> int:
+    """Makes the call with the inputs' device as the current one."""
+    if dev == torch.cuda.current_device():
+        return fn(args, _raw_stream(stream, t))
+    with torch.cuda.device(dev):
+        return fn(args, _raw_stream(stream, t))
+
+
+def _outputs(n, d, dev, like, type16, out_type, fp8, y, q, scale, stream):
+    """(y, q, scale, the type of y, its code): the caller's buffers, or new ones where they are asked for."""
+    if (q is None) != (scale is None):
+        _bad("q and scale go together")
+    if y is not None:
+        out_type = y.dtype
+    elif out_type is not None:
+        y = _new_on(stream, torch.empty, (n, d), dtype=out_type, device=like.device)
+    if q is None and fp8:
+        q, scale = _q_empty(stream, n, d, like.device)
+    if out_type is None:
+        out_type = type16 or torch.bfloat16
+    if out_type is not torch.bfloat16 and out_type is not torch.float16:
+        _bad(f"y: bfloat16 or float16 expected, got {out_type}")
+    if type16 is not None and out_type is not type16:
+        _bad(f"y: the inputs' type, {type16}, expected, got {out_type}")
+    return y, q, scale, INPUT_BF16 if out_type is torch.bfloat16 else INPUT_FP16
+
+
+def rms_norm(x, weight=None, eps: float = 1e-5, residual=None, residual_out=None, offset: float = 0.0, out_type=None, fp8: bool = False,
+             y=None, q=None, scale=None, stream=None) -> Act8:
+    """Root-mean-square norm of the rows of x [n, d] (plora_rms_norm), x + residual first if there is a residual: the sum goes to
+    residual_out (None: to residual itself).  x is fp32, or of the 16-bit type; weight [d] of either.
+    Outputs: y in 16 bits (out_type=torch.bfloat16 / float16, or a buffer) and an 8-bit matrix (fp8=True, or buffers q and scale)."""
+    n, d = x.shape
+    dev = x.get_device()
+    in_type = _type_of("x", x)
+    type16 = None if in_type == INPUT_FP32 else x.dtype
+    for t in (weight, residual):
+        if type16 is None and t is not None and t.dtype is not torch.float32:
+            type16 = t.dtype
+    if type16 is None and y is None and out_type is None and q is None and not fp8 and residual is None:
+        _bad("nothing to write: neither y, q nor a residual")
+    y, q, scale, kind = _outputs(n, d, dev, x, type16, out_type, fp8, y, q, scale, stream)
+    wt = rt = kind
+    w_at = 0
+    if weight is not None:
+        wt = _type_of("weight", weight)
+        if weight.shape != (d,) or not weight.is_cuda or not weight.is_contiguous() or weight.get_device() != dev:
+            _bad(f"weight: packed CUDA tensor [{d}] on x's device expected")
+        if wt != kind and wt != INPUT_FP32:
+            _bad("weight: float32 or the 16-bit type of the other tensors expected")
+        w_at = weight.data_ptr()
+    rs = ros = r_at = ro_at = 0
+    if residual is not None:
+        rt = _type_of("residual", residual)
+        if rt != kind and rt != INPUT_FP32:
+            _bad("residual: float32 or the 16-bit type of the other tensors expected")
+        if residual_out is None:
+            residual_out = residual
+        elif residual_out.dtype is not residual.dtype:
+            _bad("residual_out: residual's type expected")
+        rs, ros = _rows("residual", residual, n, d, dev), _rows("residual_out", residual_out, n, d, dev)
+        r_at, ro_at = residual.data_ptr(), residual_out.data_ptr()
+    elif residual_out is not None:
+        _bad("residual_out without a residual")
+    a = _NORM_PACK.pack(in_type, kind, wt, rt, n, d, _rows("x", x, n, d, dev), rs, ros, 0 if y is None else _rows("y", y, n, d, dev),
+                        0 if q is None else _q_rows("q", q, n, d, dev), x.data_ptr(), w_at, r_at, ro_at, 0 if y is None else y.data_ptr(),
+                        0 if q is None else q.data_ptr(), 0 if q is None else _scales("scale", scale, n, -(-d // 128), dev), eps, offset)
+    rc = _call_on(dev, load().plora_rms_norm, a, stream, x)
+    if rc != OK:
+        raise PloraError(rc, "plora_rms_norm")
+    return Act8(y, q, scale, residual_out)
+
+
+_ACTS = {"none": ACT_NONE, "silu": ACT_SILU, "gelu": ACT_GELU}
+
+
+def gated_act(gate, up=None, act: str = "silu", out_type=None, fp8: bool = False, y=None, q=None, scale=None, stream=None) -> Act8:
+    """act(gate) * up, or act(gate), for gate and up [n, d] (plora_gated_act); outputs as of rms_norm.  act: "silu", "gelu" (tanh form) or
+    "none": with up=None the 8-bit form of a matrix."""
+    if act not in _ACTS:
+        _bad(f"act: one of {sorted(_ACTS)} expected, got {act!r}")
+    n, d = gate.shape
+    dev = gate.get_device()
+    in_type = _type_of("gate", gate)
+    if up is not None and up.dtype is not gate.dtype:
+        _bad("gate and up: one type expected")
+    y, q, scale, kind = _outputs(n, d, dev, gate, None if in_type == INPUT_FP32 else gate.dtype, out_type, fp8, y, q, scale, stream)
+    if y is None and q is None:
+        _bad("nothing to write: neither y nor q")
+    a = _ACT_PACK.pack(in_type, kind, _ACTS[act], n, d, _rows("gate", gate, n, d, dev), 0 if up is None else _rows("up", up, n, d, dev),
+                       0 if y is None else _rows("y", y, n, d, dev), 0 if q is None else _q_rows("q", q, n, d, dev), gate.data_ptr(),
+                       0 if up is None else up.data_ptr(), 0 if y is None else y.data_ptr(), 0 if q is None else q.data_ptr(),
+                       0 if q is None else _scales("scale", scale, n, -(-d // 128), dev))
+    rc = _call_on(dev, load().plora_gated_act, a, stream, gate)
+    if rc != OK:
+        raise PloraError(rc, "plora_gated_act")
+    return Act8(y, q, scale)
+
+
+def quant_weight(w, stream=None):
+    """A weight [n, k] (n: outputs, k: inputs) as an 8-bit matrix (q [n, k] e4m3, scale [ceil(n / 128), ceil(k / 128)]): a set-up call
+    (plora_quant_weight)."""
+    n, k = w.shape
+    dev = w.get_device()
+    kind, st = _type_of("w", w), _rows("w", w, n, k, dev)
+    width = -(-k // 16) * 16
+    q = _new_on(stream, torch.empty, (n, width), dtype=torch.float8_e4m3fn, device=w.device)[:, :k]
+    scale = _new_on(stream, torch.empty, (-(-n // 128), -(-k // 128)), dtype=torch.float32, device=w.device)
+    with torch.cuda.device(dev):
+        _check(plora_quant_weight(w.data_ptr(), kind, n, k, st, q.data_ptr(), width, scale.data_ptr(), _raw_stream(stream, w)),
+               "plora_quant_weight")
+    return q, scale
+
+
+def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, stream=None):
+    """x w^T for an 8-bit matrix x [m, k] with x_scale and an 8-bit weight w [n, k] with w_scale, or up to four of them (lists) that
+    share x, in one launch (plora_gemm_fp8).  Returns [m, n] (a list of them for lists): fp32, or out_type, or the buffers `out`."""
+    many = isinstance(w, (list, tuple))
+    ws, scales = (w, w_scale) if many else ((w,), (w_scale,))
+    count = len(ws)
+    if count < 1 or count > 4 or len(scales) != count:
+        _bad("w, w_scale: one to four weights, each with its scales, expected")
+    m, k = x.shape
+    dev = x.get_device()
+    blocks = -(-k // 128)
+    if out is None:
+        kind = out_type or torch.float32
+        outs = [_new_on(stream, torch.empty, (m, t.shape[0]), dtype=kind, device=x.device) for t in ws]
+    else:
+        outs = out if many else (out,)
+        if len(outs) != count:
+            _bad("out: a buffer for each weight expected")
+    ns, strides, out_strides, at, s_at, o_at = [0] * 4, [0] * 4, [0] * 4, [0] * 4, [0] * 4, [0] * 4
+    kind = outs[0].dtype
+    for i, (t, s, o) in enumerate(zip(ws, scales, outs)):
+        n = t.shape[0]
+        if o.dtype is not kind:
+            _bad("out: one type expected")
+        ns[i], strides[i], out_strides[i] = n, _q_rows("w", t, n, k, dev), _rows("out", o, m, n, dev)
+        at[i], s_at[i], o_at[i] = t.data_ptr(), _scales("w_scale", s, -(-n // 128), blocks, dev), o.data_ptr()
+    a = _GEMM_PACK.pack(_type_of("out", outs[0]), m, k, count, *ns, _q_rows("x", x, m, k, dev), *strides, *out_strides, x.data_ptr(),
+                        _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, _opt_ints("status", status, (1,)))
+    rc = _call_on(dev, load().plora_gemm_fp8, a, stream, x)
+    if rc != OK:
+        raise PloraError(rc, "plora_gemm_fp8")
+    return list(outs) if many else outs[0]
 
 
 def plora_pool_slab_bytes(desc: PoolDesc) -> int:

@@ -256,6 +256,12 @@ struct Device {
     int id, sms;
 };
 
+// The driver's call that makes tensor maps (nullptr: there is none).
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled();
+
 // ---- launches -----------------------------------------------------------------------------------------
 cudaError_t launch_small(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Params& p, int head_dim, bool fp16, bool self,
                          Device dev, cudaStream_t st);
