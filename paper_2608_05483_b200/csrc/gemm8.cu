@@ -6,7 +6,8 @@
 // next accumulator.  (The tensor cores' sum over a block of 128 is exact to fp32 rounding here: measured error 0 against 64 bits.)
 //
 // Roles: warps 0-7 scale and add, a row per thread and half of the tile's columns per warpgroup; warp 8 loads (a box of x and one
-// of w per block of K, 128-byte rows, swizzled); warp 9 issues the products; warps 10 and 11 only give their registers away.
+// of w per block of K, 128-byte rows, swizzled); warp 9 issues the products; warps 10 and 11 stage the scales' products, some blocks ahead (loaded
+// by the adding warps themselves, a line per row, they cost those 140 of 870 cycles per block).
 #include "w8.cuh"
 
 namespace plora {
@@ -22,9 +23,11 @@ using paged::pack16;
 using paged::smem_u32;
 
 constexpr int kMaxWeights = 4;
-constexpr int kThreads = 384, kAddWarps = 8, kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 384, kAddWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kScaleWarp = 10;      // (two of the last)
 constexpr int kRows = 128;                // rows of x per CTA
 constexpr int kRowBytes = 128;            // one block of K
+constexpr int kScaleRun = 4;              // blocks of K whose scales are staged together
+constexpr int kScaleBytes = kScaleRun * 2 * kRows * 4;
 constexpr long long kWaitCycles = 4000000000ll;      // limit of a wait: about two seconds of SM clock
 
 // CG: CTAs that share a tile (cta_group); BN: columns of the tile.
@@ -34,8 +37,9 @@ struct Cfg {
     // one CTA per SM in pairs, two otherwise
     static constexpr int kStages = CG == 2 ? (BN == 256 ? 6 : 8) : (BN == 128 ? 3 : 4);
     static constexpr int kAccs = CG == 2 ? 512 / BN : 256 / BN, kTmemCols = kAccs * BN;
-    static constexpr int kBars = 2 * kStages + 2 * kAccs + 1;
-    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kBars * 8 + 16;
+    static constexpr int kScaleSlots = CG == 2 ? 4 : 2;       // such runs
+    static constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kScaleSlots + 1;
+    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kScaleSlots * kScaleBytes + kBars * 8 + 16;
     static constexpr int kCols = BN / 2;  // columns of a thread
     static constexpr int kRead = BN == 256 ? 16 : 32;     // columns read at a time (two such buffers beside the sums)
     static constexpr int kPitch = BN + 1; // floats between the rows of a partial tile in shared memory
@@ -60,7 +64,7 @@ struct Maps {
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // K-major operand of 128-byte rows, 128-byte swizzle: groups of 8 rows lie 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr) {
+__device__ __forceinline__ constexpr uint64_t smem_desc(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3fffu) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 // fp32 accumulate, e4m3 operands, both K-major.
@@ -141,8 +145,10 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {     /
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// (Hands nothing over in memory, only the right to tensor memory, whose reads are complete: a release at cluster scope cost the
+// warps that add some 800 cycles per block of K.)
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ float ld_cluster(uint32_t a) {
     float v;
@@ -157,6 +163,8 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
     return p != 0;
 }
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void st_global32(void* p, const uint32_t* w) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
                  "r"(w[5]), "r"(w[6]), "r"(w[7])
@@ -218,31 +226,35 @@ __device__ __forceinline__ Share share_of(const Params& p, uint32_t rank) {
 }
 
 struct Smem {
-    uint32_t ring, full, empty, acc_full, acc_empty, done;
+    uint32_t ring, full, empty, acc_full, acc_empty, scale_full, scale_empty, done;
+    float* scales;       // [run][block][half of the columns][row]
     uint32_t* tmem_slot;
     WaitCtl wc;
 };
 
+// Warps 8 and 9 stay together and an elected lane issues: copies and products take uniform registers, and in a branch of a single
+// lane each of them costs 100 cycles and more (the first form of this kernel: 1900 cycles per block of K instead of 512).
 template <int CG, int BN>
 __device__ __forceinline__ void load_warp(const Params& p, const Maps& maps, const Smem& sm, uint32_t rank) {
     using C = Cfg<CG, BN>;
+    const unsigned all = 0xffffffffu;
     const Share sh = share_of<CG>(p, rank);
-    const uint32_t lead = CG == 2 ? 0 : rank;
     const uint32_t bytes = CG * (uint32_t)(p.x_rows * kRowBytes + C::kBBytes);
+    const uint32_t ring = uniform(sm.ring), full = uniform(sm.full), counts = uniform(CG == 2 ? in_cta(sm.full, 0) : sm.full);
     uint32_t it = 0, early = 0;
     bool stopped = false;
     // The weights of the first stages are fetched before the kernel in front has completed: no kernel of the library that lets
     // the next one start early writes weights.
     auto begin = [&](uint32_t s, const Tile& t, int b) {
-        const uint32_t bar = sm.full + s * 8;
-        if (CG == 1 || rank == 0) mbar_arrive_expect_tx(bar, bytes);
-        tma_box<CG>(sm.ring + s * C::kStageBytes + C::kABytes, &maps.w[t.w], b * kRowBytes, t.nt * BN + (CG == 2 ? (int)rank * (BN / 2) : 0),
-                    CG == 2 ? in_cta(bar, lead) : bar);
+        if (elect_one()) {
+            if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full + s * 8, bytes);
+            tma_box<CG>(ring + s * C::kStageBytes + C::kABytes, &maps.w[t.w], b * kRowBytes, t.nt * BN + (CG == 2 ? (int)rank * (BN / 2) : 0),
+                        counts + s * 8);
+        }
     };
     auto finish = [&](uint32_t s, const Tile& t, int b) {
-        const uint32_t bar = sm.full + s * 8;
-        tma_box<CG>(sm.ring + s * C::kStageBytes, &maps.x, b * kRowBytes, (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows,
-                    CG == 2 ? in_cta(bar, lead) : bar);
+        if (elect_one())
+            tma_box<CG>(ring + s * C::kStageBytes, &maps.x, b * kRowBytes, (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows, counts + s * 8);
     };
     if (sh.first < p.tiles) {
         const Tile t = tile_of(p, sh.first);
@@ -256,7 +268,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Maps& maps, con
         for (int b = sh.b0; b < sh.b1; ++b, ++it) {
             const uint32_t s = it % C::kStages;
             if (it >= early) {
-                if (!wait(sm.empty + s * 8, ((it / C::kStages) & 1) ^ 1, sm.wc)) {
+                if (!__all_sync(all, wait(sm.empty + s * 8, ((it / C::kStages) & 1) ^ 1, sm.wc))) {
                     stopped = true;
                     break;
                 }
@@ -280,8 +292,12 @@ __device__ __forceinline__ void load_warp(const Params& p, const Maps& maps, con
 template <int CG, int BN>
 __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32_t tmem, uint32_t rank) {
     using C = Cfg<CG, BN>;
+    const unsigned all = 0xffffffffu;
     const Share sh = share_of<CG>(p, rank);
     constexpr uint32_t idesc = instr_desc(CG * kRows, BN);
+    constexpr uint32_t kHi = (uint32_t)(smem_desc(0) >> 32), kLo = (uint32_t)smem_desc(0);
+    const uint32_t ring = uniform(sm.ring >> 4), empty = uniform(sm.empty), acc_full = uniform(sm.acc_full);
+    tmem = uniform(tmem);
     uint32_t it = 0;
     bool stopped = false;
 #pragma unroll 1
@@ -289,20 +305,23 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
 #pragma unroll 1
         for (int b = sh.b0; b < sh.b1; ++b, ++it) {
             const uint32_t s = it % C::kStages, a = it % C::kAccs;
-            if (!wait(sm.acc_empty + a * 8, ((it / C::kAccs) & 1) ^ 1, sm.wc) || !wait(sm.full + s * 8, (it / C::kStages) & 1, sm.wc)) {
+            if (!__all_sync(all, wait(sm.acc_empty + a * 8, ((it / C::kAccs) & 1) ^ 1, sm.wc)) ||
+                !__all_sync(all, wait(sm.full + s * 8, (it / C::kStages) & 1, sm.wc))) {
                 stopped = true;
                 break;
             }
             tc_fence_after();
-            const uint64_t da = smem_desc(sm.ring + s * C::kStageBytes), db = smem_desc(sm.ring + s * C::kStageBytes + C::kABytes);
+            const uint32_t da = (ring + s * (C::kStageBytes >> 4)) | kLo, db = da + (C::kABytes >> 4);
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma<CG>(tmem + a * BN, da + 2 * k, db + 2 * k, idesc, k > 0);
-            umma_commit<CG, true>(sm.empty + s * 8);
-            umma_commit<CG, true>(sm.acc_full + a * 8);
+                for (int k = 0; k < 4; ++k) umma<CG>(tmem + a * BN, desc_of(da + 2 * k, kHi), desc_of(db + 2 * k, kHi), idesc, k > 0);
+                umma_commit<CG, true>(empty + s * 8);
+                umma_commit<CG, true>(acc_full + a * 8);
+            }
         }
     }
     // no product is under way when tensor memory is given back
-    umma_commit<CG, false>(sm.done);
+    if (elect_one()) umma_commit<CG, false>(sm.done);
     if (!paged::mbar_drain(sm.done, 0, kWaitCycles) && p.status) atomicCAS(p.status, 0, PLORA_ERR_TIMEOUT);
 }
 
@@ -312,53 +331,89 @@ __device__ __forceinline__ void store_one(void* out, long long at, float v) {
     else static_cast<uint16_t*>(out)[at] = (uint16_t)pack16<KIND == PLORA_INPUT_FP16>(v, 0.f);
 }
 
-// Scales and adds the accumulators of one tile: the row of this thread, kCols columns from `col` on.
+// Warps 10 and 11: sx sw of each row, block and half of the tile's columns (a half lies in one block of w's rows).
 template <int CG, int BN>
-__device__ __forceinline__ bool add_tile(const Params& p, const Smem& sm, uint32_t tmem, const Share& sh, const Tile& t, int row, int col,
-                                         int warp, int lane, uint32_t& it, float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
+__device__ __forceinline__ void scale_warps(const Params& p, const Smem& sm, uint32_t rank) {
     using C = Cfg<CG, BN>;
-    const bool any = row - lane < p.m;        // a row of this warp exists
-    const float* xs = p.x_scale + (size_t)min(row, p.m - 1) * p.blocks;
-    const float* ws = p.w_scale[t.w] + (size_t)(min(col, p.n[t.w] - 1) / kBlock) * p.blocks;
+    const Share sh = share_of<CG>(p, rank);
+    const int lane = threadIdx.x & 31, r0 = threadIdx.x - kScaleWarp * 32;
+    uint32_t it = 0;
+    paged::grid_wait();
+#pragma unroll 1
+    for (int i = sh.first; i < p.tiles; i += sh.step) {
+        const Tile t = tile_of(p, i);
+        const int row0 = (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows, last = (p.n[t.w] - 1) / kBlock;
+        const float *x0 = p.x_scale + (size_t)min(row0 + r0, p.m - 1) * p.blocks, *x1 = p.x_scale + (size_t)min(row0 + r0 + 64, p.m - 1) * p.blocks;
+        const float *w0 = p.w_scale[t.w] + (size_t)min(t.nt * BN / kBlock, last) * p.blocks;
+        const float *w1 = p.w_scale[t.w] + (size_t)min((t.nt * BN + C::kCols) / kBlock, last) * p.blocks;
+#pragma unroll 1
+        for (int b = sh.b0; b < sh.b1; b += kScaleRun, ++it) {
+            const uint32_t slot = it % C::kScaleSlots;
+            float x[2][kScaleRun], w[2][kScaleRun];
+#pragma unroll
+            for (int j = 0; j < kScaleRun; ++j) {
+                const int at = min(b + j, sh.b1 - 1);
+                x[0][j] = x0[at]; x[1][j] = x1[at];
+                w[0][j] = w0[at]; w[1][j] = w1[at];
+            }
+            if (!__all_sync(0xffffffffu, wait(sm.scale_empty + slot * 8, ((it / C::kScaleSlots) & 1) ^ 1, sm.wc))) return;
+            float* s = sm.scales + slot * (kScaleBytes / 4) + r0;
+#pragma unroll
+            for (int j = 0; j < kScaleRun; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    s[(j * 2 + h) * kRows] = x[0][j] * w[h][j];
+                    s[(j * 2 + h) * kRows + 64] = x[1][j] * w[h][j];
+                }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sm.scale_full + slot * 8);
+        }
+    }
+}
+
+// Scales and adds the accumulators of one tile: row (warp & 3) * 32 + lane of the CTA's, half warp >> 2 of the columns.
+template <int CG, int BN>
+__device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t tmem, const Share& sh, bool any, int warp, int lane, uint32_t& it, uint32_t& run,
+                                         float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
+    using C = Cfg<CG, BN>;
     const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + (warp >> 2) * C::kCols;
+    const float* scales = sm.scales + (warp >> 2) * kRows + (warp & 3) * 32 + lane;
 #pragma unroll
     for (int i = 0; i < C::kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
-    float sx = 0.f, sw = 0.f;
-    if (sh.b0 < sh.b1) {
-        sx = xs[sh.b0];
-        sw = ws[sh.b0];
-    }
 #pragma unroll 1
-    for (int b = sh.b0; b < sh.b1; ++b, ++it) {
-        const uint32_t a = it % C::kAccs;
-        const float f = sx * sw;
-        const int next = min(b + 1, sh.b1 - 1);
-        sx = xs[next];
-        sw = ws[next];
-        if (!__all_sync(0xffffffffu, wait(sm.acc_full + a * 8, (it / C::kAccs) & 1, sm.wc))) return false;
-        tc_fence_after();
-        if (any) {
-            const float2 f2 = make_float2(f, f);
-            uint32_t buf[2][C::kRead];
-            tmem_ld<C::kRead>(from + a * BN, buf[0]);
+    for (int left = sh.b1 - sh.b0; left > 0; left -= kScaleRun, ++run) {
+        const uint32_t slot = run % C::kScaleSlots;
+        if (!__all_sync(0xffffffffu, wait(sm.scale_full + slot * 8, (run / C::kScaleSlots) & 1, sm.wc))) return false;
+#pragma unroll 1
+        for (int j = 0; j < min(left, kScaleRun); ++j, ++it) {
+            const uint32_t a = it % C::kAccs;
+            const float f = scales[slot * (kScaleBytes / 4) + j * 2 * kRows];
+            if (!__all_sync(0xffffffffu, wait(sm.acc_full + a * 8, (it / C::kAccs) & 1, sm.wc))) return false;
+            tc_fence_after();
+            if (any) {        // (a row of this warp exists)
+                const float2 f2 = make_float2(f, f);
+                uint32_t buf[2][C::kRead];
+                tmem_ld<C::kRead>(from + a * BN, buf[0]);
 #pragma unroll
-            for (int c = 0; c < C::kCols / C::kRead; ++c) {
-                tmem_ld_wait();
-                if (c + 1 < C::kCols / C::kRead) tmem_ld<C::kRead>(from + a * BN + (c + 1) * C::kRead, buf[(c + 1) & 1]);
-                const float* v = reinterpret_cast<const float*>(buf[c & 1]);
+                for (int c = 0; c < C::kCols / C::kRead; ++c) {
+                    tmem_ld_wait();
+                    if (c + 1 < C::kCols / C::kRead) tmem_ld<C::kRead>(from + a * BN + (c + 1) * C::kRead, buf[(c + 1) & 1]);
+                    const float* v = reinterpret_cast<const float*>(buf[c & 1]);
 #pragma unroll
-                for (int i = 0; i < C::kRead / 2; ++i) {
-                    float2& o = acc[c * (C::kRead / 2) + i];
-                    o = __ffma2_rn(make_float2(v[2 * i], v[2 * i + 1]), f2, o);
+                    for (int i = 0; i < C::kRead / 2; ++i) {
+                        float2& o = acc[c * (C::kRead / 2) + i];
+                        o = __ffma2_rn(make_float2(v[2 * i], v[2 * i + 1]), f2, o);
+                    }
                 }
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2) arrive_cluster(in_cta(sm.acc_empty + a * 8, 0));
+                else mbar_arrive(sm.acc_empty + a * 8);
+            }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-            if (CG == 2) arrive_cluster(in_cta(sm.acc_empty + a * 8, 0));
-            else mbar_arrive(sm.acc_empty + a * 8);
-        }
+        if (lane == 0) mbar_arrive(sm.scale_empty + slot * 8);
     }
     return true;
 }
@@ -392,14 +447,17 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
     using C = Cfg<CG, BN>;
     extern __shared__ uint8_t raw[];
     uint8_t* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    uint8_t* bars = base + C::kStages * C::kStageBytes;
+    uint8_t* bars = base + C::kStages * C::kStageBytes + C::kScaleSlots * kScaleBytes;
     Smem sm;
     sm.ring = smem_u32(base);
     sm.full = smem_u32(bars);
     sm.empty = sm.full + C::kStages * 8;
     sm.acc_full = sm.empty + C::kStages * 8;
     sm.acc_empty = sm.acc_full + C::kAccs * 8;
-    sm.done = sm.acc_empty + C::kAccs * 8;
+    sm.scale_full = sm.acc_empty + C::kAccs * 8;
+    sm.scale_empty = sm.scale_full + C::kScaleSlots * 8;
+    sm.done = sm.scale_empty + C::kScaleSlots * 8;
+    sm.scales = reinterpret_cast<float*>(base + C::kStages * C::kStageBytes);
     sm.tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars * 8);
     sm.wc.abort_flag = reinterpret_cast<volatile int*>(bars + C::kBars * 8 + 8);
     sm.wc.status = p.status;
@@ -413,6 +471,10 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
         for (int a = 0; a < C::kAccs; ++a) {
             mbar_init(sm.acc_full + a * 8, 1);
             mbar_init(sm.acc_empty + a * 8, kAddWarps * CG);
+        }
+        for (int r = 0; r < C::kScaleSlots; ++r) {
+            mbar_init(sm.scale_full + r * 8, 2);
+            mbar_init(sm.scale_empty + r * 8, kAddWarps);
         }
         mbar_init(sm.done, 1);
         sm.wc.abort_flag[0] = 0;
@@ -442,13 +504,13 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
         paged::grid_wait();
         if (threadIdx.x == 0) paged::grid_launch_dependents();     // (what the kernel in front wrote is complete by now)
         const int r = (CG == 2 ? (int)rank * kRows : 0) + (warp & 3) * 32 + lane, c = (warp >> 2) * C::kCols;
-        uint32_t it = 0;
+        uint32_t it = 0, run = 0;
         float2 acc[C::kCols / 2];
 #pragma unroll 1
         for (int i = sh.first; i < p.tiles; i += sh.step) {
             const Tile t = tile_of(p, i);
             const int row = t.mt * CG * kRows + r, col = t.nt * BN + c;
-            if (!add_tile<CG, BN>(p, sm, tmem, sh, t, row, col, warp, lane, it, acc)) break;
+            if (!add_tile<CG, BN>(sm, tmem, sh, row - lane < p.m, warp, lane, it, run, acc)) break;
             if (CG == 2 || p.splits == 1) {
                 store_tile<CG, BN, KIND>(p, t, row, col, acc);
             } else if (row < p.m) {       // all products are complete: the ring is free for the partial tile
@@ -462,8 +524,9 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
         }
     } else {
         if (CG == 2 && BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (warp == kLoadWarp && elect_one()) load_warp<CG, BN>(p, maps, sm, rank);
-        else if (warp == kMmaWarp && (CG == 1 || rank == 0) && elect_one()) mma_warp<CG, BN>(p, sm, tmem, rank);
+        if (warp == kLoadWarp) load_warp<CG, BN>(p, maps, sm, rank);
+        else if (warp == kMmaWarp && (CG == 1 || rank == 0)) mma_warp<CG, BN>(p, sm, tmem, rank);
+        else if (warp >= kScaleWarp) scale_warps<CG, BN>(p, sm, rank);
         __syncwarp();
     }
     tc_fence_before();
