@@ -16,6 +16,7 @@ namespace w8 {
 namespace {
 
 constexpr float kTop = 448.f, kLeast = 1.17549435e-38f;   // largest e4m3 value; 2^-126
+constexpr int kRingMost = 224 * 1024;   // shared memory that the rings of an SM's CTAs may take together
 constexpr int kMaxNorm = 32768;     // columns of a row that a CTA of 1024 threads holds
 
 enum Kind { kNone = -1, kBf16 = PLORA_INPUT_BF16, kFp16 = PLORA_INPUT_FP16, kFp32 = PLORA_INPUT_FP32 };
@@ -30,58 +31,75 @@ __device__ __forceinline__ void from_f(float v, float& o) { o = v; }
 __device__ __forceinline__ void from_f(float v, __nv_bfloat16& o) { o = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void from_f(float v, __half& o) { o = __float2half_rn(v); }
 
-template <int BYTES> struct Words { uint32_t w[BYTES / 4]; };
-__device__ __forceinline__ void ld_words(const void* p, Words<16>& r) {
+// ---- eight columns of a row -----------------------------------------------------------------------------------------
+typedef float2 Eight[4];
+__device__ __forceinline__ uint32_t word_of(__nv_bfloat16, float2 v) { return paged::pack16<false>(v.x, v.y); }
+__device__ __forceinline__ uint32_t word_of(__half, float2 v) { return paged::pack16<true>(v.x, v.y); }
+__device__ __forceinline__ float2 pair_of(__nv_bfloat16, uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float2 pair_of(__half, uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+
+__device__ __forceinline__ void unpack8(float, const uint32_t (&w)[8], Eight& f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(T t, const uint32_t (&w)[4], Eight& f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = pair_of(t, w[i]);
+}
+__device__ __forceinline__ void ld_words(const void* p, uint32_t (&w)[4]) {
     const uint4 v = *static_cast<const uint4*>(p);
-    r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
 }
-__device__ __forceinline__ void ld_words(const void* p, Words<32>& r) {
+__device__ __forceinline__ void ld_words(const void* p, uint32_t (&w)[8]) {
     asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(p));
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
 }
-__device__ __forceinline__ void st_words(void* p, const Words<16>& r) { *static_cast<uint4*>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]); }
-__device__ __forceinline__ void st_words(void* p, const Words<32>& r) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]),
-                 "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7]) : "memory");
-}
-// Eight columns of a row.  VEC: the whole chunk lies inside the row, aligned; otherwise element by element, zeros beyond `left`.
+// VEC: the whole chunk lies inside the row, aligned to its own size; otherwise element by element, zeros beyond `left`.
 template <bool VEC, typename T>
-__device__ __forceinline__ void load8(const T* p, int left, float (&f)[8]) {
+__device__ __forceinline__ void load8(const T* p, int left, Eight& f) {
     if (VEC) {
-        Words<8 * sizeof(T)> w;
+        uint32_t w[2 * sizeof(T)];
         ld_words(p, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = to_f(reinterpret_cast<const T*>(w.w)[i]);
+        unpack8(T(), w, f);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = i < left ? to_f(p[i]) : 0.f;
+        for (int i = 0; i < 4; ++i) f[i] = make_float2(2 * i < left ? to_f(p[2 * i]) : 0.f, 2 * i + 1 < left ? to_f(p[2 * i + 1]) : 0.f);
     }
+}
+__device__ __forceinline__ void put8(float* p, const Eight& f) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(__float_as_uint(f[0].x)), "r"(__float_as_uint(f[0].y)),
+                 "r"(__float_as_uint(f[1].x)), "r"(__float_as_uint(f[1].y)), "r"(__float_as_uint(f[2].x)), "r"(__float_as_uint(f[2].y)),
+                 "r"(__float_as_uint(f[3].x)), "r"(__float_as_uint(f[3].y)) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void put8(T* p, const Eight& f) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(word_of(T(), f[0]), word_of(T(), f[1]), word_of(T(), f[2]), word_of(T(), f[3]));
 }
 template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T* p, int left, const float (&f)[8]) {
+__device__ __forceinline__ void store8(T* p, int left, const Eight& f) {
     if (VEC) {
-        Words<8 * sizeof(T)> w;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) from_f(f[i], reinterpret_cast<T*>(w.w)[i]);
-        st_words(p, w);
+        put8(p, f);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < left) from_f(f[i], p[i]);
+        for (int i = 0; i < 4; ++i) {
+            if (2 * i < left) from_f(f[i].x, p[2 * i]);
+            if (2 * i + 1 < left) from_f(f[i].y, p[2 * i + 1]);
+        }
     }
 }
-// Two e4m3 values in 16 bits, lo in the lower byte; to nearest even, finite values beyond the range to the largest.
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+// Two e4m3 values in 16 bits, the first in the lower byte; to nearest even, finite values beyond the range to the largest.
+__device__ __forceinline__ uint32_t e4m3x2(float2 v) {
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(v.y), "f"(v.x));
     return r;
 }
 template <bool VEC>
-__device__ __forceinline__ void store_q8(uint8_t* p, int left, const float (&f)[8], float inv) {
+__device__ __forceinline__ void store_q8(uint8_t* p, int left, const Eight& f, float inv) {
+    const float2 inv2 = make_float2(inv, inv);
     uint32_t w[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        w[i] = e4m3x2(f[4 * i] * inv, f[4 * i + 1] * inv) | e4m3x2(f[4 * i + 2] * inv, f[4 * i + 3] * inv) << 16;
+    for (int i = 0; i < 2; ++i) w[i] = e4m3x2(__fmul2_rn(f[2 * i], inv2)) | e4m3x2(__fmul2_rn(f[2 * i + 1], inv2)) << 16;
     if (VEC) {
         *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     } else {
@@ -90,29 +108,60 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int left, const float (&f)[
             if (i < left) p[i] = (uint8_t)(w[i >> 2] >> 8 * (i & 3));
     }
 }
-// The scale of a block from its largest magnitude; 1 / s is within two roundings of the true reciprocal.  (A NaN gives NaN.)
+// The scale of a block from its largest magnitude, and its reciprocal by the special-function unit: v / s is good to some 2^-22.
 __device__ __forceinline__ float scale_of(float top, float& inv) {
-    const float s = top / kTop;
-    const bool least = s < kLeast;
-    inv = least ? 1.f / kLeast : kTop / top;
-    return least ? kLeast : s;
+    float s = top * (1.f / kTop);
+    s = s < kLeast ? kLeast : s;             // (a NaN stays one)
+    inv = paged::rcp(s);
+    return s;
 }
-__device__ __forceinline__ float max8(const float (&f)[8]) {
-    float m = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = f[i] != f[i] ? f[i] : m < fabsf(f[i]) ? fabsf(f[i]) : m;
+// Largest magnitude; a NaN stays one.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
     return m;
 }
-// max that keeps a NaN, over the 16 lanes of a block
-__device__ __forceinline__ float max16(float m) {
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) {
-        const float o = __shfl_xor_sync(0xffffffffu, m, d);
-        m = o != o || o > m ? o : m;
-    }
-    return m;
+__device__ __forceinline__ float max8(const Eight& f) {
+    return max_abs(max_abs(f[0].x, f[0].y, f[1].x), max_abs(f[1].y, f[2].x, f[2].y), max_abs(f[3].x, f[3].y, 0.f));
 }
 
+// ---- a thread's part of a row ---------------------------------------------------------------------------------------
+// Four lanes have a block of 128 columns, each four chunks of 8 columns that lie 32 columns apart: every access of the four is 64
+// bytes (32 of the 8-bit output) in one piece, and a block's maximum is two shuffles for 32 values.  (With 16 lanes per block and a
+// chunk each, instruction issue bounded these kernels: 24 instructions per value.)
+constexpr int kChunks = 4;
+typedef Eight Part[kChunks];
+__device__ __forceinline__ int column_of(int t, int i) { return (t >> 2) * kBlock + i * 32 + (t & 3) * 8; }
+
+// y, q and scale of the row's values v (thread t of the row).  All lanes of the warp call it.
+template <int KY, bool VEC>
+__device__ __forceinline__ void write_part(void* y, long long y_stride, uint8_t* q, long long q_stride, float* scale, int blocks, int d, long long row,
+                                           int t, bool live, const Part& v) {
+    typedef typename TypeOf<KY>::type TY;
+    if (y && live) {
+        TY* out = static_cast<TY*>(y) + row * y_stride;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = column_of(t, i);
+            if (c < d) store8<VEC>(out + c, d - c, v[i]);
+        }
+    }
+    if (!q) return;
+    float m = max_abs(max8(v[0]), max8(v[1]), max_abs(max8(v[2]), max8(v[3]), 0.f)), inv;
+    m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 1), 0.f);
+    m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 2), 0.f);
+    const float s = scale_of(m, inv);
+    if (!live) return;
+    uint8_t* out = q + row * q_stride;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = column_of(t, i);
+        if (c < d) store_q8<VEC>(out + c, d - c, v[i], inv);
+    }
+    if ((t & 3) == 0 && (t >> 2) < blocks) scale[row * blocks + (t >> 2)] = s;
+}
+
+// ---- norm ------------------------------------------------------------------------------------------------------------
 struct NormParams {
     const void *x, *weight, *res;
     void *res_out, *y;
@@ -120,100 +169,198 @@ struct NormParams {
     float* scale;
     long long x_stride, res_stride, res_out_stride, y_stride, q_stride;
     int32_t n, d, blocks, weight_f32;
+    int32_t lanes;               // of a row, where a warp has whole rows: a power of two
     float eps, offset;
 };
 
-// ROWS rows per CTA, blockDim.x / ROWS threads each (ROWS > 1: a warp), NC chunks of 8 columns per thread; at most MAXT threads.
-template <int KX, int KR, int KY, int NC, int ROWS, int MAXT, bool VEC>
-__global__ void __launch_bounds__(MAXT) norm_kernel(const NormParams p) {
-    typedef typename TypeOf<KX>::type TX;
-    typedef typename TypeOf<KR>::type TR;
-    typedef typename TypeOf<KY>::type TY;
-    __shared__ float part[32];
-    const int T = ROWS > 1 ? 32 : blockDim.x, t = ROWS > 1 ? threadIdx.x & 31 : threadIdx.x;
-    const long long row = (long long)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x >> 5 : 0);
-    paged::grid_wait();
-    paged::grid_launch_dependents();
-    if (ROWS > 1 && row >= p.n) return;
-    float h[NC][8];
-    const TX* x = static_cast<const TX*>(p.x) + row * p.x_stride;
+// The sum of squares over the row's threads.
+template <bool CTA>
+__device__ __forceinline__ float row_sum(const Part& h, float* part, int t, int lanes) {
+    float2 s[kChunks];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int c = (i * T + t) * 8, left = p.d - c;
-        if (left > 0) load8<VEC>(x + c, left, h[i]);
-        else
+    for (int i = 0; i < kChunks; ++i) {
+        s[i] = __fmul2_rn(h[i][0], h[i][0]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] = 0.f;
+        for (int e = 1; e < 4; ++e) s[i] = __ffma2_rn(h[i][e], h[i][e], s[i]);
     }
-    if (KR != kNone) {
-        const TR* res = static_cast<const TR*>(p.res) + row * p.res_stride;
-        float r[NC][8];
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int c = (i * T + t) * 8, left = p.d - c;
-            if (left > 0) load8<VEC>(res + c, left, r[i]);
-        }
-        TR* out = static_cast<TR*>(p.res_out) + row * p.res_out_stride;
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int c = (i * T + t) * 8, left = p.d - c;
-            if (left > 0) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[i][e] += r[i][e];
-                store8<VEC>(out + c, left, h[i]);
-            }
-        }
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(h[i][e], h[i][e], s);
-        sum += s;
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (ROWS == 1) {
+    const float2 two = __fadd2_rn(__fadd2_rn(s[0], s[1]), __fadd2_rn(s[2], s[3]));
+    float sum = two.x + two.y;
+    for (int d = lanes / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (CTA) {
+        const int warps = blockDim.x / 32;
         if ((t & 31) == 0) part[t >> 5] = sum;
         __syncthreads();
-        sum = (t & 31) < T / 32 ? part[t & 31] : 0.f;
+        sum = (t & 31) < warps ? part[t & 31] : 0.f;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     }
+    return sum;
+}
+// v = h * rsqrt(mean + eps) * (weight + offset)
+__device__ __forceinline__ void scale8(Eight& h, const Eight& w, float f, float offset) {
+    const float2 f2 = make_float2(f, f), o2 = make_float2(offset, offset);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __fmul2_rn(h[e], __fmul2_rn(f2, __fadd2_rn(w[e], o2)));
+}
+template <int KY, bool VEC>
+__device__ __forceinline__ void weigh(const NormParams& p, Part& h, float sum, int t) {
+    typedef typename TypeOf<KY>::type TY;
     const float f = __frsqrt_rn(sum / (float)p.d + p.eps);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int c = (i * T + t) * 8, left = p.d - c;
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = column_of(t, i), left = p.d - c;
         if (left > 0) {
-            float w[8];
+            Eight w;
             if (!p.weight) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = 1.f;
+                for (int e = 0; e < 4; ++e) w[e] = make_float2(1.f, 1.f);
             } else if (p.weight_f32) {
                 load8<VEC>(static_cast<const float*>(p.weight) + c, left, w);
             } else {
                 load8<VEC>(static_cast<const TY*>(p.weight) + c, left, w);
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] *= f * (w[e] + p.offset);
-            if (p.y) store8<VEC>(static_cast<TY*>(p.y) + row * p.y_stride + c, left, h[i]);
+            scale8(h[i], w, f, p.offset);
             if (!VEC)       // (what lies beyond the row takes no part in a block's maximum)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[i][e] = e < left ? h[i][e] : 0.f;
+                for (int e = 0; e < 4; ++e) h[i][e] = make_float2(2 * e < left ? h[i][e].x : 0.f, 2 * e + 1 < left ? h[i][e].y : 0.f);
         }
-    }
-    if (!p.q) return;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int c = (i * T + t) * 8, left = p.d - c;
-        float inv;
-        const float s = scale_of(max16(max8(h[i])), inv);
-        if (left > 0) store_q8<VEC>(p.q + row * p.q_stride + c, left, h[i], inv);
-        if ((t & 15) == 0 && left > 0) p.scale[row * p.blocks + c / kBlock] = s;
     }
 }
 
+// CTA: a row per CTA; otherwise p.lanes lanes per row, and several rows per warp where a row has fewer than 32.
+template <int KX, int KR, int KY, bool CTA, bool VEC>
+__global__ void __launch_bounds__(CTA ? 1024 : 256) norm_kernel(const NormParams p) {
+    typedef typename TypeOf<KX>::type TX;
+    typedef typename TypeOf<KR>::type TR;
+    __shared__ float part[32];
+    const int lanes = CTA ? 32 : p.lanes, t = CTA ? threadIdx.x : threadIdx.x & (lanes - 1);
+    const long long row = CTA ? blockIdx.x : ((long long)blockIdx.x * blockDim.x + threadIdx.x) / lanes;
+    const bool live = row < p.n;
+    paged::grid_wait();
+    paged::grid_launch_dependents();
+    Part h;
+    const TX* x = static_cast<const TX*>(p.x) + row * p.x_stride;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = column_of(t, i), left = p.d - c;
+        if (live && left > 0) load8<VEC>(x + c, left, h[i]);
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[i][e] = make_float2(0.f, 0.f);
+    }
+    if (KR != kNone && live) {
+        const TR* res = static_cast<const TR*>(p.res) + row * p.res_stride;
+        Part r;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = column_of(t, i), left = p.d - c;
+            if (left > 0) load8<VEC>(res + c, left, r[i]);
+        }
+        TR* out = static_cast<TR*>(p.res_out) + row * p.res_out_stride;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = column_of(t, i), left = p.d - c;
+            if (left > 0) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[i][e] = __fadd2_rn(h[i][e], r[i][e]);
+                store8<VEC>(out + c, left, h[i]);
+            }
+        }
+    }
+    weigh<KY, VEC>(p, h, row_sum<CTA>(h, part, t, lanes), t);
+    write_part<KY, VEC>(p.y, p.y_stride, p.q, p.q_stride, p.scale, p.blocks, p.d, row, t, live, h);
+}
+
+// A thread's columns on their way to its own place in shared memory: copies that the thread waits for itself, so that many are
+// under way without registers, barriers or other threads.  Places lie 16 bytes apart between the threads.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+template <typename T>
+__device__ __forceinline__ void fetch8(uint32_t dst, int threads, const T* src) {
+    copy16(dst, src);
+    if (sizeof(T) == 4) copy16(dst + threads * 16, reinterpret_cast<const char*>(src) + 16);
+}
+template <typename T>
+__device__ __forceinline__ void take8(uint32_t from, int threads, Eight& f) {
+    uint32_t w[2 * sizeof(T)];
+    const uint4 a = paged::lds128(from);
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+    if (sizeof(T) == 4) {
+        constexpr int k = sizeof(T) == 4 ? 4 : 0;
+        const uint4 b = paged::lds128(from + threads * 16);
+        w[k] = b.x; w[k + 1] = b.y; w[k + 2] = b.z; w[k + 3] = b.w;
+    }
+    unpack8(T(), w, f);
+}
+
+// Long rows, aligned, dealt out to CTAs that stay: a row's columns are under way while the kRing - 1 rows before it are worked on.
+// (Arithmetic and its order are those of norm_kernel: a row's result does not depend on the rows beside it.)
+constexpr int kRing = 3;
+template <int KX, int KR, int KY, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) norm_ring_kernel(const NormParams p) {
+    typedef typename TypeOf<KX>::type TX;
+    typedef typename TypeOf<KR>::type TR;
+    constexpr int kX = 8 * sizeof(TX), kR = KR == kNone ? 0 : 8 * sizeof(TR);
+    extern __shared__ uint4 ring[];
+    __shared__ float part[2][32];
+    const int T = blockDim.x, t = threadIdx.x;
+    const uint32_t mine = paged::smem_u32(ring) + t * 16;
+    auto place = [&](uint32_t stage, int i, bool res) { return mine + ((stage * kChunks + i) * (kX + kR) + (res ? kX : 0)) * T; };
+    auto fetch = [&](uint32_t stage, long long row) {
+        if (row < p.n) {
+            const TX* x = static_cast<const TX*>(p.x) + row * p.x_stride;
+            const TR* res = static_cast<const TR*>(p.res) + row * p.res_stride;
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) {
+                const int c = column_of(t, i);
+                if (c < p.d) {
+                    fetch8(place(stage, i, false), T, x + c);
+                    if (KR != kNone) fetch8(place(stage, i, true), T, res + c);
+                }
+            }
+        }
+        copies_group();
+    };
+    paged::grid_wait();
+    paged::grid_launch_dependents();
+#pragma unroll
+    for (int s = 0; s < kRing; ++s) fetch(s, blockIdx.x + (long long)s * gridDim.x);
+    uint32_t stage = 0, odd = 0;
+#pragma unroll 1
+    for (long long row = blockIdx.x; row < p.n; row += gridDim.x, odd ^= 1) {
+        copies_wait<kRing - 1>();
+        Part h;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = column_of(t, i);
+            if (c < p.d) {
+                take8<TX>(place(stage, i, false), T, h[i]);
+                if (KR != kNone) {
+                    Eight r;
+                    take8<TR>(place(stage, i, true), T, r);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[i][e] = __fadd2_rn(h[i][e], r[e]);
+                    store8<true>(static_cast<TR*>(p.res_out) + row * p.res_out_stride + c, 8, h[i]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[i][e] = make_float2(0.f, 0.f);
+            }
+        }
+        // (two rows' partial sums lie apart: a warp may be a row ahead of the others)
+        const float sum = row_sum<true>(h, part[odd], t, 32);
+        fetch(stage, row + (long long)kRing * gridDim.x);
+        stage = stage + 1 == kRing ? 0 : stage + 1;
+        weigh<KY, true>(p, h, sum, t);
+        write_part<KY, true>(p.y, p.y_stride, p.q, p.q_stride, p.scale, p.blocks, p.d, row, t, true, h);
+    }
+}
+
+// ---- activation --------------------------------------------------------------------------------------------------------
 struct ActParams {
     const void *gate, *up;
     void* y;
@@ -222,45 +369,44 @@ struct ActParams {
     long long gate_stride, up_stride, y_stride, q_stride;
     int32_t n, d, blocks;
 };
-// sigmoid(2 z) v is v / (1 + e^-2z): silu for 2 z = v, and gelu's tanh form, v / 2 (1 + tanh z), for z = sqrt(2 / pi) (v + 0.044715 v^3)
+// sigmoid(2 z) v is v / (1 + e^-2z): silu for 2 z = v, and gelu's tanh form, v / 2 (1 + tanh z), for z = sqrt(2 / pi) (v + 0.044715 v^3).
+// The exponential and the reciprocal are the special-function unit's: good to a few 2^-23, and to 2^-23 of the exponent.
 template <int ACT>
 __device__ __forceinline__ float act_of(float v) {
     if (ACT == PLORA_ACT_NONE) return v;
     const float z2 = ACT == PLORA_ACT_SILU ? v : 1.5957691216057308f * fmaf(0.044715f * v * v, v, v);
-    return __fdividef(v, 1.f + expf(-z2));
+    return v * paged::rcp(1.f + paged::ex2(z2 * -1.4426950408889634f));
 }
-// 16 lanes have a block of 128 columns of a row.
 template <int KX, int KY, int ACT, bool GATED, bool VEC>
-__global__ void __launch_bounds__(256) act_kernel(const ActParams p) {
+__global__ void __launch_bounds__(256, 3) act_kernel(const ActParams p) {
     typedef typename TypeOf<KX>::type TX;
-    typedef typename TypeOf<KY>::type TY;
     paged::grid_wait();
     paged::grid_launch_dependents();
-    const unsigned g = (blockIdx.x * 256u + threadIdx.x) >> 4;
+    const unsigned g = (blockIdx.x * 256u + threadIdx.x) >> 2;
     const unsigned row = g / (unsigned)p.blocks, b = g - row * (unsigned)p.blocks;
-    const int c = (int)b * kBlock + (int)(threadIdx.x & 15) * 8, left = row < (unsigned)p.n ? p.d - c : 0;
-    float v[8];
+    const int t = (int)b * 4 + (threadIdx.x & 3);
+    const bool live = row < (unsigned)p.n;
+    Part v, u;
+    const TX *gate = static_cast<const TX*>(p.gate) + row * p.gate_stride, *up = static_cast<const TX*>(p.up) + row * p.up_stride;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    if (left > 0) {
-        float u[8];
-        load8<VEC>(static_cast<const TX*>(p.gate) + row * p.gate_stride + c, left, v);
-        if (GATED) load8<VEC>(static_cast<const TX*>(p.up) + row * p.up_stride + c, left, u);
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = column_of(t, i), left = p.d - c;
+        if (live && left > 0) {
+            load8<VEC>(gate + c, left, v[i]);
+            if (GATED) load8<VEC>(up + c, left, u[i]);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[e] = act_of<ACT>(v[e]);
-            if (GATED) v[e] *= u[e];
-            if (!VEC) v[e] = e < left ? v[e] : 0.f;
+            for (int e = 0; e < 4; ++e) v[i][e] = u[i][e] = make_float2(0.f, 0.f);
         }
-        if (p.y) store8<VEC>(static_cast<TY*>(p.y) + row * p.y_stride + c, left, v);
     }
-    if (!p.q) return;
-    float inv;
-    const float s = scale_of(max16(max8(v)), inv);
-    if (left > 0) {
-        store_q8<VEC>(p.q + row * p.q_stride + c, left, v, inv);
-        if ((threadIdx.x & 15) == 0) p.scale[(size_t)row * p.blocks + b] = s;
-    }
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {      // (zeros stay zeros)
+            v[i][e] = make_float2(act_of<ACT>(v[i][e].x), act_of<ACT>(v[i][e].y));
+            if (GATED) v[i][e] = __fmul2_rn(v[i][e], u[i][e]);
+        }
+    write_part<KY, VEC>(p.y, p.y_stride, p.q, p.q_stride, p.scale, p.blocks, p.d, row, t, live, v);
 }
 
 struct WeightParams {
@@ -277,27 +423,23 @@ __global__ void __launch_bounds__(1024) weight_kernel(const WeightParams p) {
     typedef typename TypeOf<KX>::type TX;
     __shared__ float part[32];
     const int r0 = blockIdx.y * kBlock + (threadIdx.x >> 4), c = blockIdx.x * kBlock + (threadIdx.x & 15) * 8, left = p.k - c;
-    float v[2][8], m = 0.f;
+    Eight v[2];
+    float m = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int r = r0 + 64 * i;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+        for (int e = 0; e < 4; ++e) v[i][e] = make_float2(0.f, 0.f);
         if (r < p.n && left > 0) load8<VEC>(static_cast<const TX*>(p.w) + r * p.w_stride + c, left, v[i]);
-        const float o = max8(v[i]);
-        m = o != o || o > m ? o : m;
+        m = max_abs(m, max8(v[i]), 0.f);
     }
-    m = max16(m);
-    const float o = __shfl_xor_sync(0xffffffffu, m, 16);
-    m = o != o || o > m ? o : m;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, d), 0.f);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
     __syncthreads();
     m = part[0];
 #pragma unroll
-    for (int i = 1; i < 32; ++i) {
-        const float o = part[i];
-        m = o != o || o > m ? o : m;
-    }
+    for (int i = 1; i < 32; ++i) m = max_abs(m, part[i], 0.f);
     float inv;
     const float s = scale_of(m, inv);
     if (threadIdx.x == 0) p.scale[(size_t)blockIdx.y * p.blocks + blockIdx.x] = s;
@@ -309,8 +451,8 @@ __global__ void __launch_bounds__(1024) weight_kernel(const WeightParams p) {
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------
-cudaError_t launch(const void* kern, dim3 grid, unsigned block, cudaStream_t st, void** args) {
-    const cudaError_t e = paged::launch_pdl(kern, grid, dim3(block), 0, st, args);
+cudaError_t launch(const void* kern, dim3 grid, unsigned block, cudaStream_t st, void** args, size_t smem = 0) {
+    const cudaError_t e = paged::launch_pdl(kern, grid, dim3(block), smem, st, args);
     if (e != cudaSuccess) (void)cudaGetLastError();      // reported by the caller; a later call must not find it
     return e;
 }
@@ -331,39 +473,44 @@ Rows rows_of(const void* p, int kind, long long& stride, long long d) {
 }
 
 template <int KX, int KR, int KY, bool VEC>
-cudaError_t norm_go(const NormParams& p, int sms, cudaStream_t st) {
-    // A warp per row up to 1024 columns.  Beyond, a CTA per row: four chunks per thread where there are rows enough to fill the
-    // SMs (bytes under way), one where a row's latency is all there is.
-    const int chunks = (p.d + 7) / 8;
-    void* args[] = {const_cast<NormParams*>(&p)};
-    if (chunks <= 128) {
-        const dim3 grid((unsigned)((p.n + 7) / 8));
-        if (chunks <= 32) return launch((const void*)norm_kernel<KX, KR, KY, 1, 8, 256, VEC>, grid, 256, st, args);
-        return launch((const void*)norm_kernel<KX, KR, KY, 4, 8, 256, VEC>, grid, 256, st, args);
+cudaError_t norm_go(NormParams p, paged::Device dev, cudaStream_t st) {
+    // Up to 1024 columns a row has 4 lanes per block, rounded up to a power of two; beyond, a CTA.  (Chosen by the columns alone:
+    // rows sum alike in any batch.)
+    void* args[] = {&p};
+    if (p.blocks <= 8) {
+        for (p.lanes = 4; p.lanes < 4 * p.blocks; p.lanes *= 2) {}
+        const long long threads = (long long)p.n * p.lanes;
+        return launch((const void*)norm_kernel<KX, KR, KY, false, VEC>, dim3((unsigned)((threads + 255) / 256)), 256, st, args);
     }
-    auto threads = [&](int nc) { return (unsigned)((chunks + nc * 32 - 1) / (nc * 32) * 32); };
-    if (p.n <= 2 * sms && chunks <= 1024) return launch((const void*)norm_kernel<KX, KR, KY, 1, 1, 1024, VEC>, dim3(p.n), threads(1), st, args);
-    if (chunks <= 1024) return launch((const void*)norm_kernel<KX, KR, KY, 4, 1, 256, VEC>, dim3(p.n), threads(4), st, args);
-    return launch((const void*)norm_kernel<KX, KR, KY, 4, 1, 1024, VEC>, dim3(p.n), threads(4), st, args);
+    const unsigned threads = (unsigned)((p.blocks * 4 + 31) / 32 * 32);
+    const size_t ring = (size_t)kRing * kChunks * 8 * (size_of(KX) + (KR == kNone ? 0 : size_of(KR))) * threads;
+    if (!VEC || ring + 1280 > kRingMost) return launch((const void*)norm_kernel<KX, KR, KY, true, VEC>, dim3(p.n), threads, st, args);
+    const bool wide = threads > 256;
+    const void* kern = wide ? (const void*)norm_ring_kernel<KX, KR, KY, 1024> : (const void*)norm_ring_kernel<KX, KR, KY, 256>;
+    static paged::Configured configured[2];
+    const cudaError_t e = configured[wide].ensure(kern, kRingMost, dev.id);
+    if (e != cudaSuccess) return e;
+    const long long fit = kRingMost / (ring + 1280), most = wide ? 1 : 768 / threads, ctas = (fit < most ? fit : most) * dev.sms;
+    return launch(kern, dim3((unsigned)(p.n < ctas ? p.n : ctas)), threads, st, args, ring);
 }
 template <int KX, int KY>
-cudaError_t norm_res(const NormParams& p, int res, bool vec, int sms, cudaStream_t st) {
-    if (!p.res) return vec ? norm_go<KX, kNone, KY, true>(p, sms, st) : norm_go<KX, kNone, KY, false>(p, sms, st);
-    if (res == kFp32) return vec ? norm_go<KX, kFp32, KY, true>(p, sms, st) : norm_go<KX, kFp32, KY, false>(p, sms, st);
-    return vec ? norm_go<KX, KY, KY, true>(p, sms, st) : norm_go<KX, KY, KY, false>(p, sms, st);
+cudaError_t norm_res(const NormParams& p, int res, bool vec, paged::Device dev, cudaStream_t st) {
+    if (!p.res) return vec ? norm_go<KX, kNone, KY, true>(p, dev, st) : norm_go<KX, kNone, KY, false>(p, dev, st);
+    if (res == kFp32) return vec ? norm_go<KX, kFp32, KY, true>(p, dev, st) : norm_go<KX, kFp32, KY, false>(p, dev, st);
+    return vec ? norm_go<KX, KY, KY, true>(p, dev, st) : norm_go<KX, KY, KY, false>(p, dev, st);
 }
 template <int KX, int KY, int ACT>
-cudaError_t act_go(const ActParams& p, bool vec, unsigned grid, cudaStream_t st) {
+cudaError_t act_go(const ActParams& p, bool vec, cudaStream_t st) {
     void* args[] = {const_cast<ActParams*>(&p)};
     const void* k = p.up ? (vec ? (const void*)act_kernel<KX, KY, ACT, true, true> : (const void*)act_kernel<KX, KY, ACT, true, false>)
                          : (vec ? (const void*)act_kernel<KX, KY, ACT, false, true> : (const void*)act_kernel<KX, KY, ACT, false, false>);
-    return launch(k, dim3(grid), 256, st, args);
+    return launch(k, dim3((unsigned)(((long long)p.n * p.blocks * 4 + 255) / 256)), 256, st, args);
 }
 template <int KX, int KY>
-cudaError_t act_kind(const ActParams& p, int act, bool vec, unsigned grid, cudaStream_t st) {
-    if (act == PLORA_ACT_SILU) return act_go<KX, KY, PLORA_ACT_SILU>(p, vec, grid, st);
-    if (act == PLORA_ACT_GELU) return act_go<KX, KY, PLORA_ACT_GELU>(p, vec, grid, st);
-    return act_go<KX, KY, PLORA_ACT_NONE>(p, vec, grid, st);
+cudaError_t act_kind(const ActParams& p, int act, bool vec, cudaStream_t st) {
+    if (act == PLORA_ACT_SILU) return act_go<KX, KY, PLORA_ACT_SILU>(p, vec, st);
+    if (act == PLORA_ACT_GELU) return act_go<KX, KY, PLORA_ACT_GELU>(p, vec, st);
+    return act_go<KX, KY, PLORA_ACT_NONE>(p, vec, st);
 }
 template <int KX>
 cudaError_t weight_go(const WeightParams& p, bool vec, dim3 grid, cudaStream_t st) {
@@ -389,7 +536,7 @@ extern "C" PLORA_API plora_status plora_rms_norm(const plora_rms_norm_args* a, v
     if (!a->x || (!a->residual != !a->residual_out) || (!a->q != !a->scale) || (!a->y && !a->q && !a->residual)) return PLORA_ERR_INVALID_ARG;
     NormParams p{a->x, a->weight, a->residual, a->residual_out, a->y, static_cast<uint8_t*>(a->q), a->scale, a->x_stride, a->residual_stride,
                  a->residual_out_stride, a->y_stride, a->q_stride, a->n, a->d, (a->d + kBlock - 1) / kBlock, a->weight_type == kFp32,
-                 a->eps, a->offset};
+                 0, a->eps, a->offset};
     bool vec = a->d % 8 == 0;
     auto take = [&](const void* ptr, int kind, long long& stride) {
         if (!ptr) return true;
@@ -411,9 +558,9 @@ extern "C" PLORA_API plora_status plora_rms_norm(const plora_rms_norm_args* a, v
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (a->type == kBf16)
-        e = a->in_type == kFp32 ? norm_res<kFp32, kBf16>(p, a->residual_type, vec, dev.sms, st) : norm_res<kBf16, kBf16>(p, a->residual_type, vec, dev.sms, st);
+        e = a->in_type == kFp32 ? norm_res<kFp32, kBf16>(p, a->residual_type, vec, dev, st) : norm_res<kBf16, kBf16>(p, a->residual_type, vec, dev, st);
     else
-        e = a->in_type == kFp32 ? norm_res<kFp32, kFp16>(p, a->residual_type, vec, dev.sms, st) : norm_res<kFp16, kFp16>(p, a->residual_type, vec, dev.sms, st);
+        e = a->in_type == kFp32 ? norm_res<kFp32, kFp16>(p, a->residual_type, vec, dev, st) : norm_res<kFp16, kFp16>(p, a->residual_type, vec, dev, st);
     return e == cudaSuccess ? PLORA_OK : PLORA_ERR_CUDA;
 }
 
@@ -438,15 +585,13 @@ extern "C" PLORA_API plora_status plora_gated_act(const plora_gated_act_args* a,
         if (!p.q_stride) p.q_stride = up16(a->d);
         if (p.q_stride < a->d || p.q_stride % 16 || !aligned(a->q, 16) || !aligned(a->scale, 4)) return PLORA_ERR_INVALID_ARG;
     }
-    const long long lanes = (long long)p.n * p.blocks * 16;     // (the kernel counts blocks of 128 in 32 bits)
-    if (lanes / 16 > (1ll << 28)) return PLORA_ERR_UNSUPPORTED;
-    const unsigned grid = (unsigned)((lanes + 255) / 256);
+    if ((long long)p.n * p.blocks > (1ll << 29)) return PLORA_ERR_UNSUPPORTED;     // (the kernel counts its threads in 32 bits)
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (a->type == kBf16)
-        e = a->in_type == kFp32 ? act_kind<kFp32, kBf16>(p, a->act, vec, grid, st) : act_kind<kBf16, kBf16>(p, a->act, vec, grid, st);
+        e = a->in_type == kFp32 ? act_kind<kFp32, kBf16>(p, a->act, vec, st) : act_kind<kBf16, kBf16>(p, a->act, vec, st);
     else
-        e = a->in_type == kFp32 ? act_kind<kFp32, kFp16>(p, a->act, vec, grid, st) : act_kind<kFp16, kFp16>(p, a->act, vec, grid, st);
+        e = a->in_type == kFp32 ? act_kind<kFp32, kFp16>(p, a->act, vec, st) : act_kind<kFp16, kFp16>(p, a->act, vec, st);
     return e == cudaSuccess ? PLORA_OK : PLORA_ERR_CUDA;
 }
 
