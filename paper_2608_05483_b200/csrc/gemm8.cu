@@ -26,24 +26,29 @@ constexpr int kMaxWeights = 4;
 constexpr int kThreads = 384, kAddWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kScaleWarp = 10;      // (two of the last)
 constexpr int kRows = 128;                // rows of x per CTA
 constexpr int kRowBytes = 128;            // one block of K
-constexpr int kScaleRun = 4;              // blocks of K whose scales are staged together
-constexpr int kScaleBytes = kScaleRun * 2 * kRows * 4;
+constexpr int kScaleRun = 4, kScaleSlots = 4;          // blocks of K whose scales are staged together; such runs
+constexpr int kScaleBytes = kScaleRun * (kRows + 4) * 4;    // of a run: sx [block][row], then sw [block][half of the columns][2]
+constexpr int kMaxStages = 16;
+constexpr int kRingOffset = (kScaleSlots * kScaleBytes + 512 + 1023) / 1024 * 1024;        // scales, barriers and words lie in front of the ring
 constexpr long long kWaitCycles = 4000000000ll;      // limit of a wait: about two seconds of SM clock
 
-// CG: CTAs that share a tile (cta_group); BN: columns of the tile.
+// CG: CTAs that share a tile (cta_group); BN: columns of the tile, a multiple of 32.
+// Narrow tiles of single CTAs leave room for a second CTA on the SM, so that one starts or ends while the other streams (7.6 against
+// 11 us for 16 rows by 4096 x 4096, a launch behind another); the others have the SM to themselves.
 template <int CG, int BN>
 struct Cfg {
-    static constexpr int kABytes = kRows * kRowBytes, kBBytes = BN / CG * kRowBytes, kStageBytes = kABytes + kBBytes;
-    // one CTA per SM in pairs, two otherwise
-    static constexpr int kStages = CG == 2 ? (BN == 256 ? 6 : 8) : (BN == 128 ? 3 : 4);
-    static constexpr int kAccs = CG == 2 ? 512 / BN : 256 / BN, kTmemCols = kAccs * BN;
-    static constexpr int kScaleSlots = CG == 2 ? 4 : 2;       // such runs
-    static constexpr int kBars = 2 * kStages + 2 * kAccs + 2 * kScaleSlots + 1;
-    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kScaleSlots * kScaleBytes + kBars * 8 + 16;
-    static constexpr int kCols = BN / 2;  // columns of a thread
-    static constexpr int kRead = BN == 256 ? 16 : 32;     // columns read at a time (two such buffers beside the sums)
-    static constexpr int kPitch = BN + 1; // floats between the rows of a partial tile in shared memory
-    static_assert(CG == 2 || kRows * kPitch * 4 <= kStages * kStageBytes, "a partial tile fits into the ring");
+    static constexpr int kCtas = CG == 1 && BN == 64 ? 2 : 1;
+    static constexpr int kTmemCols = 512 / kCtas, kSmemMost = kCtas == 2 ? 112 * 1024 : 227 * 1024;
+    static constexpr int kBBytes = BN / CG * kRowBytes;
+    // Blocks of K per stage and accumulator: two where tensor memory holds two such accumulators (a block's hand-overs cost some 600
+    // cycles whatever its size: one row by 12288 x 4096 weights in tiles of 64 columns 14.2 us with one, 12.1 with two).
+    static constexpr int kRun = BN <= 128 ? 2 : 1;
+    static constexpr int kAccs = kTmemCols / (BN * kRun) > 4 ? 4 : kTmemCols / (BN * kRun);
+    static constexpr int kCols = BN / 2;                  // columns of a thread
+    static constexpr bool kCrosses = kBlock % kCols != 0; // a half may lie in two blocks of w's rows
+    static constexpr int kRead = 16;      // columns read at a time (two such buffers beside the sums)
+    static constexpr int kPitch = BN + 4; // floats between the rows of a partial tile in shared memory (4 banks apart, accesses of 16 bytes)
+    static_assert(BN % 32 == 0 && kBBytes % 1024 == 0, "");
 };
 
 struct Params {
@@ -53,7 +58,8 @@ struct Params {
     long long out_stride[kMaxWeights];
     int32_t n[kMaxWeights], tile_end[kMaxWeights];     // columns; tiles of columns up to and with this weight's
     int32_t m, blocks, m_tiles, n_tiles, tiles, splits, x_rows;   // blocks of K; x_rows: rows of a box of x
-    int32_t wide;                                      // every row of every output is 32-byte aligned
+    int32_t stages, x_bytes;                           // of the ring; bytes of a stage's box of x, a multiple of 1024
+    int32_t vec;                                       // bytes that every row of every output is aligned to: 32, 16, or fewer
     int32_t* status;
 };
 struct Maps {
@@ -96,26 +102,11 @@ __device__ __forceinline__ void umma_commit(uint32_t bar) {
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t* r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
-          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(a));
-}
 __device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
                    "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(a));
-}
-template <int N>
-__device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t* r) {
-    if (N == 32) tmem_ld32(a, r);
-    else tmem_ld16(a, r);
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // A box of rows of 128 bytes.  In a pair the barrier may be the other CTA's.
@@ -150,9 +141,9 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {     /
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ float ld_cluster(uint32_t a) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+__device__ __forceinline__ float4 ld_cluster(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ void cluster_sync() {
@@ -191,6 +182,18 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const WaitCt
     return mbar_try_wait(bar, parity) || wait_slow(bar, parity, w);
 }
 
+// A place in a ring of N, and the parity of the turn.
+template <uint32_t N>
+struct Turn {
+    uint32_t at = 0, parity = 0;
+    __device__ __forceinline__ void next(uint32_t n = N) {
+        if (++at == n) {
+            at = 0;
+            parity ^= 1;
+        }
+    }
+};
+
 // ---- the tiles ----------------------------------------------------------------------------------------------------
 // Tiles are numbered so that those under way at one time (some 74) form a near-square of x and w: runs of kGroup tiles of rows by all
 // tiles of columns.
@@ -218,10 +221,10 @@ __device__ __forceinline__ Tile tile_of(const Params& p, int i) {
 struct Share {
     int32_t first, step, b0, b1;
 };
-template <int CG>
+template <int CG, int RUN>
 __device__ __forceinline__ Share share_of(const Params& p, uint32_t rank) {
-    if (CG == 2) return {(int)(blockIdx.x >> 1), (int)(gridDim.x >> 1), 0, p.blocks};
-    const int per = (p.blocks + p.splits - 1) / p.splits, b0 = min((int)rank * per, p.blocks);
+    if (CG == 2 || p.splits == 1) return {(int)blockIdx.x / CG, (int)gridDim.x / CG, 0, p.blocks};
+    const int per = ((p.blocks + p.splits - 1) / p.splits + RUN - 1) / RUN * RUN, b0 = min((int)rank * per, p.blocks);
     return {(int)blockIdx.x / p.splits, p.tiles, b0, min(b0 + per, p.blocks)};
 }
 
@@ -238,54 +241,60 @@ template <int CG, int BN>
 __device__ __forceinline__ void load_warp(const Params& p, const Maps& maps, const Smem& sm, uint32_t rank) {
     using C = Cfg<CG, BN>;
     const unsigned all = 0xffffffffu;
-    const Share sh = share_of<CG>(p, rank);
-    const uint32_t bytes = CG * (uint32_t)(p.x_rows * kRowBytes + C::kBBytes);
+    const Share sh = share_of<CG, Cfg<CG, BN>::kRun>(p, rank);
+    const uint32_t bytes = CG * C::kRun * (uint32_t)(p.x_rows * kRowBytes + C::kBBytes);
     const uint32_t ring = uniform(sm.ring), full = uniform(sm.full), counts = uniform(CG == 2 ? in_cta(sm.full, 0) : sm.full);
     uint32_t it = 0, early = 0;
+    Turn<0> turn;
+    const uint32_t stages = p.stages, stage_bytes = C::kRun * (p.x_bytes + C::kBBytes);
     bool stopped = false;
     // The weights of the first stages are fetched before the kernel in front has completed: no kernel of the library that lets
     // the next one start early writes weights.
     auto begin = [&](uint32_t s, const Tile& t, int b) {
         if (elect_one()) {
             if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full + s * 8, bytes);
-            tma_box<CG>(ring + s * C::kStageBytes + C::kABytes, &maps.w[t.w], b * kRowBytes, t.nt * BN + (CG == 2 ? (int)rank * (BN / 2) : 0),
-                        counts + s * 8);
+#pragma unroll
+            for (int j = 0; j < C::kRun; ++j)        // (what lies beyond K reads as zeros)
+                tma_box<CG>(ring + s * stage_bytes + C::kRun * p.x_bytes + j * C::kBBytes, &maps.w[t.w], (b + j) * kRowBytes,
+                            t.nt * BN + (CG == 2 ? (int)rank * (BN / 2) : 0), counts + s * 8);
         }
     };
     auto finish = [&](uint32_t s, const Tile& t, int b) {
         if (elect_one())
-            tma_box<CG>(ring + s * C::kStageBytes, &maps.x, b * kRowBytes, (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows, counts + s * 8);
+#pragma unroll
+            for (int j = 0; j < C::kRun; ++j)
+                tma_box<CG>(ring + s * stage_bytes + j * p.x_bytes, &maps.x, (b + j) * kRowBytes, (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows,
+                            counts + s * 8);
     };
     if (sh.first < p.tiles) {
         const Tile t = tile_of(p, sh.first);
-        for (; early < C::kStages && sh.b0 + (int)early < sh.b1; ++early) begin(early, t, sh.b0 + early);
+        for (int b = sh.b0; early < stages && b < sh.b1; ++early, b += C::kRun) begin(early, t, b);
     }
     paged::grid_wait();
 #pragma unroll 1
     for (int i = sh.first; i < p.tiles && !stopped; i += sh.step) {
         const Tile t = tile_of(p, i);
 #pragma unroll 1
-        for (int b = sh.b0; b < sh.b1; ++b, ++it) {
-            const uint32_t s = it % C::kStages;
+        for (int b = sh.b0; b < sh.b1; b += C::kRun, ++it, turn.next(stages)) {
             if (it >= early) {
-                if (!__all_sync(all, wait(sm.empty + s * 8, ((it / C::kStages) & 1) ^ 1, sm.wc))) {
+                if (!__all_sync(all, wait(sm.empty + turn.at * 8, turn.parity ^ 1, sm.wc))) {
                     stopped = true;
                     break;
                 }
-                begin(s, t, b);
+                begin(turn.at, t, b);
             }
-            finish(s, t, b);
+            finish(turn.at, t, b);
         }
     }
     const uint32_t n = max(it, early);
     if (!stopped) {
         // the products' last signals come from the pair's first CTA: they must have come before the second one leaves
         if (CG == 2)
-            for (uint32_t j = n > C::kStages ? n - C::kStages : 0; j < n; ++j) wait(sm.empty + j % C::kStages * 8, (j / C::kStages) & 1, sm.wc);
+            for (uint32_t j = n > stages ? n - stages : 0; j < n; ++j) wait(sm.empty + j % stages * 8, (j / stages) & 1, sm.wc);
     } else if (CG == 1 || rank == 0) {
         // copies in flight must land before the CTA leaves (in a pair they are counted by the first CTA's barriers)
-        for (uint32_t j = n > C::kStages ? n - C::kStages : 0; j < n; ++j)
-            paged::mbar_drain(sm.full + j % C::kStages * 8, (j / C::kStages) & 1, kWaitCycles);
+        for (uint32_t j = n > stages ? n - stages : 0; j < n; ++j)
+            paged::mbar_drain(sm.full + j % stages * 8, (j / stages) & 1, kWaitCycles);
     }
 }
 
@@ -293,30 +302,47 @@ template <int CG, int BN>
 __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32_t tmem, uint32_t rank) {
     using C = Cfg<CG, BN>;
     const unsigned all = 0xffffffffu;
-    const Share sh = share_of<CG>(p, rank);
+    const Share sh = share_of<CG, Cfg<CG, BN>::kRun>(p, rank);
     constexpr uint32_t idesc = instr_desc(CG * kRows, BN);
     constexpr uint32_t kHi = (uint32_t)(smem_desc(0) >> 32), kLo = (uint32_t)smem_desc(0);
     const uint32_t ring = uniform(sm.ring >> 4), empty = uniform(sm.empty), acc_full = uniform(sm.acc_full);
     tmem = uniform(tmem);
-    uint32_t it = 0;
+    Turn<0> turn;
+    const uint32_t stages = p.stages, stage_step = C::kRun * (p.x_bytes + C::kBBytes) >> 4, x_step = p.x_bytes >> 4;
+    Turn<C::kAccs> acc;
     bool stopped = false;
+    // Both barriers of a block are tried at once, right behind the block before: a try's answer takes some 100 cycles, and
+    // with one after the other this warp took longer than the products.
+    bool go_acc = mbar_try_wait(sm.acc_empty, 1), go_full = false;
+    if (sh.first < p.tiles && sh.b0 < sh.b1) go_full = mbar_try_wait(sm.full, 0);
 #pragma unroll 1
     for (int i = sh.first; i < p.tiles && !stopped; i += sh.step) {
 #pragma unroll 1
-        for (int b = sh.b0; b < sh.b1; ++b, ++it) {
-            const uint32_t s = it % C::kStages, a = it % C::kAccs;
-            if (!__all_sync(all, wait(sm.acc_empty + a * 8, ((it / C::kAccs) & 1) ^ 1, sm.wc)) ||
-                !__all_sync(all, wait(sm.full + s * 8, (it / C::kStages) & 1, sm.wc))) {
-                stopped = true;
-                break;
+        for (int b = sh.b0; b < sh.b1; b += C::kRun) {
+            if (!__all_sync(all, go_acc && go_full)) {
+                if (!__all_sync(all, wait(sm.acc_empty + acc.at * 8, acc.parity ^ 1, sm.wc) && wait(sm.full + turn.at * 8, turn.parity, sm.wc))) {
+                    stopped = true;
+                    break;
+                }
             }
             tc_fence_after();
-            const uint32_t da = (ring + s * (C::kStageBytes >> 4)) | kLo, db = da + (C::kABytes >> 4);
+            const uint32_t da = (ring + turn.at * stage_step) | kLo, db = da + C::kRun * x_step;
             if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) umma<CG>(tmem + a * BN, desc_of(da + 2 * k, kHi), desc_of(db + 2 * k, kHi), idesc, k > 0);
-                umma_commit<CG, true>(empty + s * 8);
-                umma_commit<CG, true>(acc_full + a * 8);
+                for (int j = 0; j < C::kRun; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        umma<CG>(tmem + (acc.at * C::kRun + j) * BN, desc_of(da + j * x_step + 2 * k, kHi),
+                                 desc_of(db + j * (C::kBBytes >> 4) + 2 * k, kHi), idesc, k > 0);
+                umma_commit<CG, true>(acc_full + acc.at * 8);
+                umma_commit<CG, true>(empty + turn.at * 8);
+            }
+            turn.next(stages);
+            acc.next();
+            // (not behind the last block: a try sleeps for microseconds if nothing comes)
+            if (b + C::kRun < sh.b1 || i + sh.step < p.tiles) {
+                go_acc = mbar_try_wait(sm.acc_empty + acc.at * 8, acc.parity ^ 1);
+                go_full = mbar_try_wait(sm.full + turn.at * 8, turn.parity);
             }
         }
     }
@@ -331,78 +357,106 @@ __device__ __forceinline__ void store_one(void* out, long long at, float v) {
     else static_cast<uint16_t*>(out)[at] = (uint16_t)pack16<KIND == PLORA_INPUT_FP16>(v, 0.f);
 }
 
-// Warps 10 and 11: sx sw of each row, block and half of the tile's columns (a half lies in one block of w's rows).
+// Four columns of a row, of which `left` exist.
+template <int KIND>
+__device__ __forceinline__ void store_four(void* out, long long at, float4 v, int left, int vec) {
+    if (left >= 4 && vec >= (KIND == PLORA_INPUT_FP32 ? 16 : 8)) {
+        if (KIND == PLORA_INPUT_FP32) *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = v;
+        else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack16<KIND == PLORA_INPUT_FP16>(v.x, v.y), pack16<KIND == PLORA_INPUT_FP16>(v.z, v.w));
+        return;
+    }
+    const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) store_one<KIND>(out, at + i, f[i]);
+}
+
+// First of the (at most two) blocks of w's rows that columns [col, ..) lie in, and the columns up to the next one.
+__device__ __forceinline__ int block_of(int col) { return col / kBlock; }
+__device__ __forceinline__ int left_in_block(int col) { return kBlock - col % kBlock; }
+
+// Warps 10 and 11: the scales of the rows, two rows per thread, and of the halves' columns.
 template <int CG, int BN>
 __device__ __forceinline__ void scale_warps(const Params& p, const Smem& sm, uint32_t rank) {
     using C = Cfg<CG, BN>;
-    const Share sh = share_of<CG>(p, rank);
+    const Share sh = share_of<CG, Cfg<CG, BN>::kRun>(p, rank);
     const int lane = threadIdx.x & 31, r0 = threadIdx.x - kScaleWarp * 32;
-    uint32_t it = 0;
+    Turn<kScaleSlots> turn;
     paged::grid_wait();
 #pragma unroll 1
     for (int i = sh.first; i < p.tiles; i += sh.step) {
         const Tile t = tile_of(p, i);
-        const int row0 = (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows, last = (p.n[t.w] - 1) / kBlock;
+        const int row0 = (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows;
         const float *x0 = p.x_scale + (size_t)min(row0 + r0, p.m - 1) * p.blocks, *x1 = p.x_scale + (size_t)min(row0 + r0 + 64, p.m - 1) * p.blocks;
-        const float *w0 = p.w_scale[t.w] + (size_t)min(t.nt * BN / kBlock, last) * p.blocks;
-        const float *w1 = p.w_scale[t.w] + (size_t)min((t.nt * BN + C::kCols) / kBlock, last) * p.blocks;
+        // thread 4 j + 2 h + i of the 64: block j of the run, half h, i-th of its blocks
+        const int j4 = r0 >> 2, wb = block_of(t.nt * BN + (r0 >> 1 & 1) * C::kCols) + (r0 & 1);
+        const float* w0 = p.w_scale[t.w] + (size_t)min(wb, block_of(p.n[t.w] - 1)) * p.blocks;
 #pragma unroll 1
-        for (int b = sh.b0; b < sh.b1; b += kScaleRun, ++it) {
-            const uint32_t slot = it % C::kScaleSlots;
-            float x[2][kScaleRun], w[2][kScaleRun];
+        for (int b = sh.b0; b < sh.b1; b += kScaleRun, turn.next()) {
+            float x[2][kScaleRun], w = 0.f;
 #pragma unroll
             for (int j = 0; j < kScaleRun; ++j) {
-                const int at = min(b + j, sh.b1 - 1);
-                x[0][j] = x0[at]; x[1][j] = x1[at];
-                w[0][j] = w0[at]; w[1][j] = w1[at];
+                const bool there = b + j < sh.b1;        // (a block beyond the last one counts nothing)
+                x[0][j] = there ? x0[b + j] : 0.f;
+                x[1][j] = there ? x1[b + j] : 0.f;
             }
-            if (!__all_sync(0xffffffffu, wait(sm.scale_empty + slot * 8, ((it / C::kScaleSlots) & 1) ^ 1, sm.wc))) return;
-            float* s = sm.scales + slot * (kScaleBytes / 4) + r0;
+            if (r0 < 4 * kScaleRun && b + j4 < sh.b1) w = w0[b + j4];
+            if (!__all_sync(0xffffffffu, wait(sm.scale_empty + turn.at * 8, turn.parity ^ 1, sm.wc))) return;
+            float* s = sm.scales + turn.at * (kScaleBytes / 4);
 #pragma unroll
-            for (int j = 0; j < kScaleRun; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    s[(j * 2 + h) * kRows] = x[0][j] * w[h][j];
-                    s[(j * 2 + h) * kRows + 64] = x[1][j] * w[h][j];
-                }
+            for (int j = 0; j < kScaleRun; ++j) {
+                s[j * kRows + r0] = x[0][j];
+                s[j * kRows + r0 + 64] = x[1][j];
+            }
+            if (r0 < 4 * kScaleRun) s[kScaleRun * kRows + r0] = w;
             __syncwarp();
-            if (lane == 0) mbar_arrive(sm.scale_full + slot * 8);
+            if (lane == 0) mbar_arrive(sm.scale_full + turn.at * 8);
         }
     }
 }
 
-// Scales and adds the accumulators of one tile: row (warp & 3) * 32 + lane of the CTA's, half warp >> 2 of the columns.
+// Scales and adds the accumulators of one tile: row (warp & 3) * 32 + lane of the CTA's, half warp >> 2 of the columns, from `col` on.
 template <int CG, int BN>
-__device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t tmem, const Share& sh, bool any, int warp, int lane, uint32_t& it, uint32_t& run,
-                                         float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
+__device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t tmem, const Share& sh, bool any, int col, int warp, int lane,
+                                         Turn<Cfg<CG, BN>::kAccs>& in, Turn<kScaleSlots>& run, float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
     using C = Cfg<CG, BN>;
     const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + (warp >> 2) * C::kCols;
-    const float* scales = sm.scales + (warp >> 2) * kRows + (warp & 3) * 32 + lane;
+    const int first = left_in_block(col);        // columns of the half's first block
 #pragma unroll
     for (int i = 0; i < C::kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
 #pragma unroll 1
-    for (int left = sh.b1 - sh.b0; left > 0; left -= kScaleRun, ++run) {
-        const uint32_t slot = run % C::kScaleSlots;
-        if (!__all_sync(0xffffffffu, wait(sm.scale_full + slot * 8, (run / C::kScaleSlots) & 1, sm.wc))) return false;
+    for (int left = sh.b1 - sh.b0; left > 0; left -= kScaleRun, run.next()) {
+        if (!__all_sync(0xffffffffu, wait(sm.scale_full + run.at * 8, run.parity, sm.wc))) return false;
+        const float* sx = sm.scales + run.at * (kScaleBytes / 4) + (warp & 3) * 32 + lane;
+        const float* sw = sm.scales + run.at * (kScaleBytes / 4) + kScaleRun * kRows + (warp >> 2) * 2;
 #pragma unroll 1
-        for (int j = 0; j < min(left, kScaleRun); ++j, ++it) {
-            const uint32_t a = it % C::kAccs;
-            const float f = scales[slot * (kScaleBytes / 4) + j * 2 * kRows];
-            if (!__all_sync(0xffffffffu, wait(sm.acc_full + a * 8, (it / C::kAccs) & 1, sm.wc))) return false;
+        for (int j = 0; j < min(left, kScaleRun); j += C::kRun, in.next()) {
+            const uint32_t a = in.at;
+            float2 f[C::kRun], g[C::kRun];        // the scales in the half's first and second block
+#pragma unroll
+            for (int r = 0; r < C::kRun; ++r) {
+                const float x = sx[(j + r) * kRows], u = x * sw[(j + r) * 4], v = C::kCrosses ? x * sw[(j + r) * 4 + 1] : 0.f;
+                f[r] = make_float2(u, u);
+                g[r] = make_float2(v, v);
+            }
+            if (!__all_sync(0xffffffffu, wait(sm.acc_full + a * 8, in.parity, sm.wc))) return false;
             tc_fence_after();
             if (any) {        // (a row of this warp exists)
-                const float2 f2 = make_float2(f, f);
+                constexpr int kReads = C::kCols / C::kRead;
+                auto column = [&](int i) { return from + (a * C::kRun + i / kReads) * BN + i % kReads * C::kRead; };
                 uint32_t buf[2][C::kRead];
-                tmem_ld<C::kRead>(from + a * BN, buf[0]);
+                tmem_ld16(column(0), buf[0]);
 #pragma unroll
-                for (int c = 0; c < C::kCols / C::kRead; ++c) {
+                for (int i = 0; i < C::kRun * kReads; ++i) {
                     tmem_ld_wait();
-                    if (c + 1 < C::kCols / C::kRead) tmem_ld<C::kRead>(from + a * BN + (c + 1) * C::kRead, buf[(c + 1) & 1]);
-                    const float* v = reinterpret_cast<const float*>(buf[c & 1]);
+                    if (i + 1 < C::kRun * kReads) tmem_ld16(column(i + 1), buf[(i + 1) & 1]);
+                    const float* v = reinterpret_cast<const float*>(buf[i & 1]);
+                    const int c = i % kReads;
+                    const float2 s2 = C::kCrosses && c * C::kRead >= first ? g[i / kReads] : f[i / kReads];
 #pragma unroll
-                    for (int i = 0; i < C::kRead / 2; ++i) {
-                        float2& o = acc[c * (C::kRead / 2) + i];
-                        o = __ffma2_rn(make_float2(v[2 * i], v[2 * i + 1]), f2, o);
+                    for (int e = 0; e < C::kRead / 2; ++e) {
+                        float2& o = acc[c * (C::kRead / 2) + e];
+                        o = __ffma2_rn(make_float2(v[2 * e], v[2 * e + 1]), s2, o);
                     }
                 }
             }
@@ -413,7 +467,7 @@ __device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t tmem, const Sh
                 else mbar_arrive(sm.acc_empty + a * 8);
             }
         }
-        if (lane == 0) mbar_arrive(sm.scale_empty + slot * 8);
+        if (lane == 0) mbar_arrive(sm.scale_empty + run.at * 8);
     }
     return true;
 }
@@ -424,16 +478,22 @@ __device__ __forceinline__ void store_tile(const Params& p, const Tile& t, int r
     if (row >= p.m) return;
     const int n = p.n[t.w];
     const long long at = row * p.out_stride[t.w] + col;
-    constexpr int kStep = KIND == PLORA_INPUT_FP32 ? 8 : 16;       // columns of a 32-byte store
+    constexpr int kSize = KIND == PLORA_INPUT_FP32 ? 4 : 2, kStep = 32 / kSize;       // columns of a 32-byte store
 #pragma unroll
     for (int c = 0; c < C::kCols; c += kStep) {
         const float* v = reinterpret_cast<const float*>(acc) + c;
-        if (p.wide && col + c + kStep <= n) {
+        if (p.vec >= 16 && col + c + kStep <= n) {
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 w[i] = KIND == PLORA_INPUT_FP32 ? __float_as_uint(v[i]) : pack16<KIND == PLORA_INPUT_FP16>(v[(2 * i) % kStep], v[(2 * i + 1) % kStep]);
-            st_global32(static_cast<char*>(p.out[t.w]) + (at + c) * (KIND == PLORA_INPUT_FP32 ? 4 : 2), w);
+            char* o = static_cast<char*>(p.out[t.w]) + (at + c) * kSize;
+            if (p.vec == 32) {
+                st_global32(o, w);
+            } else {
+                *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(o + 16) = make_uint4(w[4], w[5], w[6], w[7]);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < kStep; ++i)
@@ -443,28 +503,32 @@ __device__ __forceinline__ void store_tile(const Params& p, const Tile& t, int r
 }
 
 template <int CG, int BN, int KIND>
-__global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
     using C = Cfg<CG, BN>;
     extern __shared__ uint8_t raw[];
     uint8_t* base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    uint8_t* bars = base + C::kStages * C::kStageBytes + C::kScaleSlots * kScaleBytes;
+    uint8_t* bars = base + kScaleSlots * kScaleBytes;
     Smem sm;
-    sm.ring = smem_u32(base);
+    // scales, barriers and words first: products read 128 rows of x from a stage whatever its box has, and what they read behind
+    // it has to be this CTA's (the host leaves room behind the last stage); it goes into rows that nobody takes
+    sm.ring = smem_u32(base) + kRingOffset;
     sm.full = smem_u32(bars);
-    sm.empty = sm.full + C::kStages * 8;
-    sm.acc_full = sm.empty + C::kStages * 8;
+    sm.empty = sm.full + kMaxStages * 8;
+    sm.acc_full = sm.empty + kMaxStages * 8;
     sm.acc_empty = sm.acc_full + C::kAccs * 8;
     sm.scale_full = sm.acc_empty + C::kAccs * 8;
-    sm.scale_empty = sm.scale_full + C::kScaleSlots * 8;
-    sm.done = sm.scale_empty + C::kScaleSlots * 8;
-    sm.scales = reinterpret_cast<float*>(base + C::kStages * C::kStageBytes);
-    sm.tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars * 8);
-    sm.wc.abort_flag = reinterpret_cast<volatile int*>(bars + C::kBars * 8 + 8);
+    sm.scale_empty = sm.scale_full + kScaleSlots * 8;
+    sm.done = sm.scale_empty + kScaleSlots * 8;
+    sm.scales = reinterpret_cast<float*>(base);
+    constexpr int kBars = 2 * kMaxStages + 2 * C::kAccs + 2 * kScaleSlots + 1;
+    static_assert(kScaleSlots * kScaleBytes + kBars * 8 + 16 <= kRingOffset, "");
+    sm.tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars * 8);
+    sm.wc.abort_flag = reinterpret_cast<volatile int*>(bars + kBars * 8 + 8);
     sm.wc.status = p.status;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::kStages; ++s) {
+        for (int s = 0; s < p.stages; ++s) {
             mbar_init(sm.full + s * 8, 1);
             mbar_init(sm.empty + s * 8, 1);
         }
@@ -472,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
             mbar_init(sm.acc_full + a * 8, 1);
             mbar_init(sm.acc_empty + a * 8, kAddWarps * CG);
         }
-        for (int r = 0; r < C::kScaleSlots; ++r) {
+        for (int r = 0; r < kScaleSlots; ++r) {
             mbar_init(sm.scale_full + r * 8, 2);
             mbar_init(sm.scale_empty + r * 8, kAddWarps);
         }
@@ -498,32 +562,30 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
     if (CG == 2) cluster_sync();        // the other CTA's barriers exist
     tc_fence_after();
     const uint32_t tmem = *sm.tmem_slot;
-    const Share sh = share_of<CG>(p, rank);
+    const Share sh = share_of<CG, Cfg<CG, BN>::kRun>(p, rank);
     if (warp < kAddWarps) {
-        if (CG == 2 && BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        if (BN > 192) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         paged::grid_wait();
         if (threadIdx.x == 0) paged::grid_launch_dependents();     // (what the kernel in front wrote is complete by now)
         const int r = (CG == 2 ? (int)rank * kRows : 0) + (warp & 3) * 32 + lane, c = (warp >> 2) * C::kCols;
-        uint32_t it = 0, run = 0;
+        Turn<C::kAccs> in;
+        Turn<kScaleSlots> run;
         float2 acc[C::kCols / 2];
 #pragma unroll 1
         for (int i = sh.first; i < p.tiles; i += sh.step) {
             const Tile t = tile_of(p, i);
             const int row = t.mt * CG * kRows + r, col = t.nt * BN + c;
-            if (!add_tile<CG, BN>(sm, tmem, sh, row - lane < p.m, warp, lane, it, run, acc)) break;
+            if (!add_tile<CG, BN>(sm, tmem, sh, row - lane < p.m, col, warp, lane, in, run, acc)) break;
             if (CG == 2 || p.splits == 1) {
                 store_tile<CG, BN, KIND>(p, t, row, col, acc);
             } else if (row < p.m) {       // all products are complete: the ring is free for the partial tile
-                float* part = reinterpret_cast<float*>(base) + r * C::kPitch + c;
+                float4* part = reinterpret_cast<float4*>(base + kRingOffset) + (r * C::kPitch + c) / 4;
 #pragma unroll
-                for (int e = 0; e < C::kCols / 2; ++e) {
-                    part[2 * e] = acc[e].x;
-                    part[2 * e + 1] = acc[e].y;
-                }
+                for (int e = 0; e < C::kCols / 4; ++e) part[e] = make_float4(acc[2 * e].x, acc[2 * e].y, acc[2 * e + 1].x, acc[2 * e + 1].y);
             }
         }
     } else {
-        if (CG == 2 && BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (BN > 192) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == kLoadWarp) load_warp<CG, BN>(p, maps, sm, rank);
         else if (warp == kMmaWarp && (CG == 1 || rank == 0)) mma_warp<CG, BN>(p, sm, tmem, rank);
         else if (warp >= kScaleWarp) scale_warps<CG, BN>(p, sm, rank);
@@ -539,14 +601,17 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
         const Tile t = tile_of(p, sh.first);
         const int rows = min(kRows, p.m - t.mt * kRows), cols = min(BN, p.n[t.w] - t.nt * BN);
 #pragma unroll 1
-        for (int e = (int)rank * kThreads + threadIdx.x; e < rows * BN; e += p.splits * kThreads) {
-            const int r = e / BN, c = e % BN;
+        for (int e = (int)rank * kThreads + threadIdx.x; e < rows * (BN / 4); e += p.splits * kThreads) {
+            const int r = e / (BN / 4), c = e % (BN / 4) * 4;
             if (c >= cols) continue;
             const uint32_t at = sm.ring + (r * C::kPitch + c) * 4;
-            float v = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-            for (int s = 0; s < p.splits; ++s) v += ld_cluster(in_cta(at, s));
-            store_one<KIND>(p.out[t.w], (t.mt * kRows + r) * p.out_stride[t.w] + t.nt * BN + c, v);
+            for (int s = 0; s < p.splits; ++s) {
+                const float4 o = ld_cluster(in_cta(at, s));
+                v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+            }
+            store_four<KIND>(p.out[t.w], (t.mt * kRows + r) * p.out_stride[t.w] + t.nt * BN + c, v, cols - c, p.vec);
         }
         cluster_sync();
     }
@@ -560,11 +625,23 @@ __global__ void __launch_bounds__(kThreads, CG == 2 ? 1 : 2) gemm_kernel(const _
 // ---- host side --------------------------------------------------------------------------------------------------
 template <int CG, int BN, int KIND>
 cudaError_t go(const Maps& maps, Params p, paged::Device dev, cudaStream_t st) {
+    using C = Cfg<CG, BN>;
     auto kern = gemm_kernel<CG, BN, KIND>;
     static paged::Configured configured;
-    const cudaError_t e = configured.ensure(reinterpret_cast<const void*>(kern), Cfg<CG, BN>::kSmemBytes, dev.id);
+    const cudaError_t e = configured.ensure(reinterpret_cast<const void*>(kern), C::kSmemMost, dev.id);
     if (e != cudaSuccess) return e;
-    const int cluster = CG == 2 ? 2 : p.splits, most = CG == 2 ? dev.sms / 2 : p.tiles;
+    // As deep a ring as fits, with 128 rows of x (or the rows of a partial tile) behind the start of its last stage.
+    const int stage = C::kRun * (p.x_bytes + C::kBBytes), room = C::kSmemMost - 1024 - kRingOffset;
+    const int last_x = stage - (C::kRun - 1) * p.x_bytes, behind = kRows * kRowBytes > last_x ? kRows * kRowBytes - last_x : 0;
+    p.stages = (room - behind) / stage;
+    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    const int most_stages = (p.blocks + C::kRun - 1) / C::kRun;
+    if (p.stages > most_stages) p.stages = most_stages;
+    int ring = p.stages * stage + behind;
+    const int rows = p.m < kRows ? p.m : kRows, part = p.splits > 1 ? rows * C::kPitch * 4 : 0;
+    if (ring < part) ring = part;
+    const int smem = 1024 + kRingOffset + ring;
+    const int cluster = CG == 2 ? 2 : p.splits, most = p.splits > 1 ? p.tiles : dev.sms * C::kCtas / CG;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -574,7 +651,7 @@ cudaError_t go(const Maps& maps, Params p, paged::Device dev, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((p.tiles < most ? p.tiles : most) * cluster));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Cfg<CG, BN>::kSmemBytes;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
@@ -587,7 +664,62 @@ cudaError_t go_kind(int kind, const Maps& maps, const Params& p, paged::Device d
     if (kind == PLORA_INPUT_BF16) return go<CG, BN, PLORA_INPUT_BF16>(maps, p, dev, st);
     return go<CG, BN, PLORA_INPUT_FP16>(maps, p, dev, st);
 }
+template <int CG>
+cudaError_t go_bn(int bn, int kind, const Maps& maps, const Params& p, paged::Device dev, cudaStream_t st) {
+    switch (bn) {
+        case 64: return go_kind<CG, 64>(kind, maps, p, dev, st);
+        case 96: return go_kind<CG, 96>(kind, maps, p, dev, st);
+        case 128: return go_kind<CG, 128>(kind, maps, p, dev, st);
+        case 160: return go_kind<CG, 160>(kind, maps, p, dev, st);
+        case 192: return go_kind<CG, 192>(kind, maps, p, dev, st);
+        case 224: return go_kind<CG, 224>(kind, maps, p, dev, st);
+        default: return go_kind<CG, 256>(kind, maps, p, dev, st);
+    }
+}
 bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// How a call is cut: single CTAs or pairs, columns of a tile, and parts that a tile's K is split into (a cluster of single CTAs).
+// Taken is the form whose estimate is least; the estimate is the time of a block of K in a CTA times the blocks that a CTA has, and
+// what a tile costs besides.  Its constants are measured: 60 bytes per ns and SM of what comes from HBM (one tile of rows), 75 of what
+// mostly comes from L2, 6500 from HBM in all; 1600 cycles per us under load; the hand-over of accumulators, which bounds wide tiles.
+// Of 37 calls of 1 to 4096 rows, 320 to 27648 columns and K up to 13824 it chose the fastest form, or one within 13 %, for all but one
+// (28 % behind, 5.4 against 4.2 us).
+struct Form {
+    int cg, bn, splits;
+};
+Form choose(const plora_gemm_fp8_args* a, int blocks, int sms) {
+    Form best{1, 64, 1};
+    double least = 1e30;
+    const int size = a->out_type == PLORA_INPUT_FP32 ? 4 : 2, x_rows = a->m < kRows ? a->m : kRows;
+    for (int cg = 1; cg <= (a->m > kRows ? 2 : 1); ++cg) {
+        const long long rows = ((long long)a->m + cg * kRows - 1) / (cg * kRows);
+        for (int bn = 64; bn <= 256; bn += 32) {
+            long long cols = 0;
+            for (int i = 0; i < a->n_weights; ++i) cols += ((long long)a->n[i] + bn - 1) / bn;
+            const double hand_over = bn <= 128 ? 0.17 : bn == 160 ? 0.37 : 0.12 + 0.0017 * bn;
+            const bool two = cg == 1 && bn == 64;        // CTAs on an SM
+            for (int s = 1; s <= (cg == 1 ? 8 : 1) && (s == 1 || blocks >= 2 * s); ++s) {
+                // (clusters do not fill the processing clusters of 16 to 20 SMs that they have to lie in: percent of the CTAs that
+                // fit at one time, by the size of a cluster, as the occupancy query gives them on a B200)
+                static const int fit[2][9] = {{0, 100, 100, 91, 89, 87, 89, 70, 81}, {0, 100, 100, 94, 95, 94, 91, 87, 89}};
+                const long long slots = (long long)sms * (two ? 2 : 1) * fit[two][s] / 100;
+                const long long ctas = rows * cols * s * cg, rounds = (ctas + slots - 1) / slots, active = ctas < slots ? ctas : slots;
+                const double on_sm = active > sms ? 2 : 1;
+                double t = (x_rows + bn / cg) * kRowBytes * on_sm / (rows == 1 ? 60e3 : 75e3);
+                const double products = bn * 2 * on_sm / 1600, hbm = (double)active * (bn / cg) * kRowBytes / rows / 6.5e6;
+                t = products > t ? products : t;
+                t = hand_over > t ? hand_over : t;
+                t = hbm > t ? hbm : t;
+                const double us = 3 + rounds * ((blocks + s - 1) / s * t + (double)x_rows * bn * size / 28e3) + (s > 1 ? 2 + 3 * (rounds - 1) + (double)x_rows * bn / 10e3 : 0);
+                if (us < least) {
+                    least = us;
+                    best = Form{cg, bn, s};
+                }
+            }
+        }
+    }
+    return best;
+}
 bool map_bytes(CUtensorMap* tm, const void* base, long long cols, long long rows, long long stride, int box_rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
     const cuuint32_t box[2] = {kRowBytes, (cuuint32_t)box_rows}, es[2] = {1, 1};
@@ -630,14 +762,14 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
     long long x_stride = a->x_stride, w_stride[kMaxWeights];
     if (!matrix(a->x, x_stride) || !a->x_scale || !aligned(a->x_scale, 4) || (a->status && !aligned(a->status, 4))) return PLORA_ERR_INVALID_ARG;
     Params p{};
-    p.wide = 1;
+    p.vec = 32;
     for (int i = 0; i < a->n_weights; ++i) {
         w_stride[i] = a->w_stride[i];
         if (!matrix(a->w[i], w_stride[i]) || !a->w_scale[i] || !aligned(a->w_scale[i], 4) || !a->out[i] || !aligned(a->out[i], es))
             return PLORA_ERR_INVALID_ARG;
         p.out_stride[i] = a->out_stride[i] ? a->out_stride[i] : a->n[i];
         if (p.out_stride[i] < a->n[i]) return PLORA_ERR_INVALID_ARG;
-        p.wide = p.wide && aligned(a->out[i], 32) && p.out_stride[i] * es % 32 == 0;
+        while (p.vec > es && (!aligned(a->out[i], p.vec) || p.out_stride[i] * es % p.vec)) p.vec /= 2;
         p.w_scale[i] = a->w_scale[i];
         p.out[i] = a->out[i];
         p.n[i] = a->n[i];
@@ -649,22 +781,14 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
     p.m = a->m;
     p.blocks = (int)(((long long)a->k + kBlock - 1) / kBlock);
     p.status = a->status;
+    const Form form = choose(a, p.blocks, dev.sms);
+    const int cg = form.cg, bn = form.bn;
+    p.splits = form.splits;
     auto tiles_of = [&](int bn) {
         long long t = 0;
         for (int i = 0; i < a->n_weights; ++i) t += ((long long)a->n[i] + bn - 1) / bn;
         return t;
     };
-    const bool pair = a->m > kRows;
-    int bn = 64;
-    p.splits = 1;
-    if (pair) {
-        const long long m_tiles = (a->m + 2 * kRows - 1) / (2 * kRows);
-        bn = m_tiles * tiles_of(256) >= dev.sms / 2 ? 256 : 128;
-    } else {
-        const long long t = tiles_of(64);
-        while (p.splits < 8 && t * p.splits * 2 <= 2 * dev.sms && p.blocks >= 4 * p.splits) p.splits *= 2;
-    }
-    const int cg = pair ? 2 : 1;
     const long long m_tiles = ((long long)a->m + cg * kRows - 1) / (cg * kRows), n_tiles = tiles_of(bn);
     if (m_tiles * n_tiles * 8 > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
     p.m_tiles = (int)m_tiles;
@@ -674,15 +798,15 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
         if (i < a->n_weights) t += (a->n[i] + bn - 1) / bn;
         p.tile_end[i] = t;
     }
-    p.x_rows = pair || a->m >= kRows ? kRows : (a->m + 7) / 8 * 8;
+    p.x_rows = a->m >= kRows ? kRows : (a->m + 7) / 8 * 8;
+    p.x_bytes = p.x_rows * kRowBytes;
     Maps maps;
     if (!map_bytes(&maps.x, a->x, a->k, a->m, x_stride, p.x_rows)) return PLORA_ERR_INVALID_ARG;
     for (int i = 0; i < a->n_weights; ++i)
         if (!map_bytes(&maps.w[i], a->w[i], a->k, a->n[i], w_stride[i], bn / cg)) return PLORA_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
-    if (pair) e = bn == 256 ? go_kind<2, 256>(a->out_type, maps, p, dev, st) : go_kind<2, 128>(a->out_type, maps, p, dev, st);
-    else e = go_kind<1, 64>(a->out_type, maps, p, dev, st);
+    e = cg == 2 ? go_bn<2>(bn, a->out_type, maps, p, dev, st) : go_bn<1>(bn, a->out_type, maps, p, dev, st);
     if (e != cudaSuccess) {
         (void)cudaGetLastError();      // reported here; a later call must not find it
         return PLORA_ERR_CUDA;

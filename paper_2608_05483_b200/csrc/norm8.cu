@@ -16,7 +16,6 @@ namespace w8 {
 namespace {
 
 constexpr float kTop = 448.f, kLeast = 1.17549435e-38f;   // largest e4m3 value; 2^-126
-constexpr int kRingMost = 224 * 1024;   // shared memory that the rings of an SM's CTAs may take together
 constexpr int kMaxNorm = 32768;     // columns of a row that a CTA of 1024 threads holds
 
 enum Kind { kNone = -1, kBf16 = PLORA_INPUT_BF16, kFp16 = PLORA_INPUT_FP16, kFp32 = PLORA_INPUT_FP32 };
@@ -228,8 +227,8 @@ __device__ __forceinline__ void weigh(const NormParams& p, Part& h, float sum, i
 }
 
 // CTA: a row per CTA; otherwise p.lanes lanes per row, and several rows per warp where a row has fewer than 32.
-template <int KX, int KR, int KY, bool CTA, bool VEC>
-__global__ void __launch_bounds__(CTA ? 1024 : 256) norm_kernel(const NormParams p) {
+template <int KX, int KR, int KY, bool CTA, int MAXT, bool VEC>
+__global__ void __launch_bounds__(MAXT, MAXT > 256 ? 1 : CTA && KX != kFp32 ? 3 : 2) norm_kernel(const NormParams p) {
     typedef typename TypeOf<KX>::type TX;
     typedef typename TypeOf<KR>::type TR;
     __shared__ float part[32];
@@ -271,95 +270,6 @@ __global__ void __launch_bounds__(CTA ? 1024 : 256) norm_kernel(const NormParams
     write_part<KY, VEC>(p.y, p.y_stride, p.q, p.q_stride, p.scale, p.blocks, p.d, row, t, live, h);
 }
 
-// A thread's columns on their way to its own place in shared memory: copies that the thread waits for itself, so that many are
-// under way without registers, barriers or other threads.  Places lie 16 bytes apart between the threads.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-template <typename T>
-__device__ __forceinline__ void fetch8(uint32_t dst, int threads, const T* src) {
-    copy16(dst, src);
-    if (sizeof(T) == 4) copy16(dst + threads * 16, reinterpret_cast<const char*>(src) + 16);
-}
-template <typename T>
-__device__ __forceinline__ void take8(uint32_t from, int threads, Eight& f) {
-    uint32_t w[2 * sizeof(T)];
-    const uint4 a = paged::lds128(from);
-    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-    if (sizeof(T) == 4) {
-        constexpr int k = sizeof(T) == 4 ? 4 : 0;
-        const uint4 b = paged::lds128(from + threads * 16);
-        w[k] = b.x; w[k + 1] = b.y; w[k + 2] = b.z; w[k + 3] = b.w;
-    }
-    unpack8(T(), w, f);
-}
-
-// Long rows, aligned, dealt out to CTAs that stay: a row's columns are under way while the kRing - 1 rows before it are worked on.
-// (Arithmetic and its order are those of norm_kernel: a row's result does not depend on the rows beside it.)
-constexpr int kRing = 3;
-template <int KX, int KR, int KY, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) norm_ring_kernel(const NormParams p) {
-    typedef typename TypeOf<KX>::type TX;
-    typedef typename TypeOf<KR>::type TR;
-    constexpr int kX = 8 * sizeof(TX), kR = KR == kNone ? 0 : 8 * sizeof(TR);
-    extern __shared__ uint4 ring[];
-    __shared__ float part[2][32];
-    const int T = blockDim.x, t = threadIdx.x;
-    const uint32_t mine = paged::smem_u32(ring) + t * 16;
-    auto place = [&](uint32_t stage, int i, bool res) { return mine + ((stage * kChunks + i) * (kX + kR) + (res ? kX : 0)) * T; };
-    auto fetch = [&](uint32_t stage, long long row) {
-        if (row < p.n) {
-            const TX* x = static_cast<const TX*>(p.x) + row * p.x_stride;
-            const TR* res = static_cast<const TR*>(p.res) + row * p.res_stride;
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i) {
-                const int c = column_of(t, i);
-                if (c < p.d) {
-                    fetch8(place(stage, i, false), T, x + c);
-                    if (KR != kNone) fetch8(place(stage, i, true), T, res + c);
-                }
-            }
-        }
-        copies_group();
-    };
-    paged::grid_wait();
-    paged::grid_launch_dependents();
-#pragma unroll
-    for (int s = 0; s < kRing; ++s) fetch(s, blockIdx.x + (long long)s * gridDim.x);
-    uint32_t stage = 0, odd = 0;
-#pragma unroll 1
-    for (long long row = blockIdx.x; row < p.n; row += gridDim.x, odd ^= 1) {
-        copies_wait<kRing - 1>();
-        Part h;
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-            const int c = column_of(t, i);
-            if (c < p.d) {
-                take8<TX>(place(stage, i, false), T, h[i]);
-                if (KR != kNone) {
-                    Eight r;
-                    take8<TR>(place(stage, i, true), T, r);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) h[i][e] = __fadd2_rn(h[i][e], r[e]);
-                    store8<true>(static_cast<TR*>(p.res_out) + row * p.res_out_stride + c, 8, h[i]);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[i][e] = make_float2(0.f, 0.f);
-            }
-        }
-        // (two rows' partial sums lie apart: a warp may be a row ahead of the others)
-        const float sum = row_sum<true>(h, part[odd], t, 32);
-        fetch(stage, row + (long long)kRing * gridDim.x);
-        stage = stage + 1 == kRing ? 0 : stage + 1;
-        weigh<KY, true>(p, h, sum, t);
-        write_part<KY, true>(p.y, p.y_stride, p.q, p.q_stride, p.scale, p.blocks, p.d, row, t, true, h);
-    }
-}
-
 // ---- activation --------------------------------------------------------------------------------------------------------
 struct ActParams {
     const void *gate, *up;
@@ -378,11 +288,11 @@ __device__ __forceinline__ float act_of(float v) {
     return v * paged::rcp(1.f + paged::ex2(z2 * -1.4426950408889634f));
 }
 template <int KX, int KY, int ACT, bool GATED, bool VEC>
-__global__ void __launch_bounds__(256, 3) act_kernel(const ActParams p) {
+__global__ void __launch_bounds__(128, 6) act_kernel(const ActParams p) {
     typedef typename TypeOf<KX>::type TX;
     paged::grid_wait();
     paged::grid_launch_dependents();
-    const unsigned g = (blockIdx.x * 256u + threadIdx.x) >> 2;
+    const unsigned g = (blockIdx.x * 128u + threadIdx.x) >> 2;
     const unsigned row = g / (unsigned)p.blocks, b = g - row * (unsigned)p.blocks;
     const int t = (int)b * 4 + (threadIdx.x & 3);
     const bool live = row < (unsigned)p.n;
@@ -451,8 +361,8 @@ __global__ void __launch_bounds__(1024) weight_kernel(const WeightParams p) {
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------
-cudaError_t launch(const void* kern, dim3 grid, unsigned block, cudaStream_t st, void** args, size_t smem = 0) {
-    const cudaError_t e = paged::launch_pdl(kern, grid, dim3(block), smem, st, args);
+cudaError_t launch(const void* kern, dim3 grid, unsigned block, cudaStream_t st, void** args) {
+    const cudaError_t e = paged::launch_pdl(kern, grid, dim3(block), 0, st, args);
     if (e != cudaSuccess) (void)cudaGetLastError();      // reported by the caller; a later call must not find it
     return e;
 }
@@ -473,38 +383,31 @@ Rows rows_of(const void* p, int kind, long long& stride, long long d) {
 }
 
 template <int KX, int KR, int KY, bool VEC>
-cudaError_t norm_go(NormParams p, paged::Device dev, cudaStream_t st) {
+cudaError_t norm_go(NormParams p, cudaStream_t st) {
     // Up to 1024 columns a row has 4 lanes per block, rounded up to a power of two; beyond, a CTA.  (Chosen by the columns alone:
     // rows sum alike in any batch.)
     void* args[] = {&p};
     if (p.blocks <= 8) {
         for (p.lanes = 4; p.lanes < 4 * p.blocks; p.lanes *= 2) {}
         const long long threads = (long long)p.n * p.lanes;
-        return launch((const void*)norm_kernel<KX, KR, KY, false, VEC>, dim3((unsigned)((threads + 255) / 256)), 256, st, args);
+        return launch((const void*)norm_kernel<KX, KR, KY, false, 256, VEC>, dim3((unsigned)((threads + 255) / 256)), 256, st, args);
     }
     const unsigned threads = (unsigned)((p.blocks * 4 + 31) / 32 * 32);
-    const size_t ring = (size_t)kRing * kChunks * 8 * (size_of(KX) + (KR == kNone ? 0 : size_of(KR))) * threads;
-    if (!VEC || ring + 1280 > kRingMost) return launch((const void*)norm_kernel<KX, KR, KY, true, VEC>, dim3(p.n), threads, st, args);
-    const bool wide = threads > 256;
-    const void* kern = wide ? (const void*)norm_ring_kernel<KX, KR, KY, 1024> : (const void*)norm_ring_kernel<KX, KR, KY, 256>;
-    static paged::Configured configured[2];
-    const cudaError_t e = configured[wide].ensure(kern, kRingMost, dev.id);
-    if (e != cudaSuccess) return e;
-    const long long fit = kRingMost / (ring + 1280), most = wide ? 1 : 768 / threads, ctas = (fit < most ? fit : most) * dev.sms;
-    return launch(kern, dim3((unsigned)(p.n < ctas ? p.n : ctas)), threads, st, args, ring);
+    return launch(threads > 256 ? (const void*)norm_kernel<KX, KR, KY, true, 1024, VEC> : (const void*)norm_kernel<KX, KR, KY, true, 256, VEC>,
+                  dim3(p.n), threads, st, args);
 }
 template <int KX, int KY>
-cudaError_t norm_res(const NormParams& p, int res, bool vec, paged::Device dev, cudaStream_t st) {
-    if (!p.res) return vec ? norm_go<KX, kNone, KY, true>(p, dev, st) : norm_go<KX, kNone, KY, false>(p, dev, st);
-    if (res == kFp32) return vec ? norm_go<KX, kFp32, KY, true>(p, dev, st) : norm_go<KX, kFp32, KY, false>(p, dev, st);
-    return vec ? norm_go<KX, KY, KY, true>(p, dev, st) : norm_go<KX, KY, KY, false>(p, dev, st);
+cudaError_t norm_res(const NormParams& p, int res, bool vec, cudaStream_t st) {
+    if (!p.res) return vec ? norm_go<KX, kNone, KY, true>(p, st) : norm_go<KX, kNone, KY, false>(p, st);
+    if (res == kFp32) return vec ? norm_go<KX, kFp32, KY, true>(p, st) : norm_go<KX, kFp32, KY, false>(p, st);
+    return vec ? norm_go<KX, KY, KY, true>(p, st) : norm_go<KX, KY, KY, false>(p, st);
 }
 template <int KX, int KY, int ACT>
 cudaError_t act_go(const ActParams& p, bool vec, cudaStream_t st) {
     void* args[] = {const_cast<ActParams*>(&p)};
     const void* k = p.up ? (vec ? (const void*)act_kernel<KX, KY, ACT, true, true> : (const void*)act_kernel<KX, KY, ACT, true, false>)
                          : (vec ? (const void*)act_kernel<KX, KY, ACT, false, true> : (const void*)act_kernel<KX, KY, ACT, false, false>);
-    return launch(k, dim3((unsigned)(((long long)p.n * p.blocks * 4 + 255) / 256)), 256, st, args);
+    return launch(k, dim3((unsigned)(((long long)p.n * p.blocks * 4 + 127) / 128)), 128, st, args);
 }
 template <int KX, int KY>
 cudaError_t act_kind(const ActParams& p, int act, bool vec, cudaStream_t st) {
@@ -553,14 +456,12 @@ extern "C" PLORA_API plora_status plora_rms_norm(const plora_rms_norm_args* a, v
         if (!p.q_stride) p.q_stride = up16(a->d);
         if (p.q_stride < a->d || p.q_stride % 16 || !aligned(a->q, 16) || !aligned(a->scale, 4)) return PLORA_ERR_INVALID_ARG;
     }
-    plora::paged::Device dev;
-    if (plora::w8::device(dev) != cudaSuccess) return PLORA_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (a->type == kBf16)
-        e = a->in_type == kFp32 ? norm_res<kFp32, kBf16>(p, a->residual_type, vec, dev, st) : norm_res<kBf16, kBf16>(p, a->residual_type, vec, dev, st);
+        e = a->in_type == kFp32 ? norm_res<kFp32, kBf16>(p, a->residual_type, vec, st) : norm_res<kBf16, kBf16>(p, a->residual_type, vec, st);
     else
-        e = a->in_type == kFp32 ? norm_res<kFp32, kFp16>(p, a->residual_type, vec, dev, st) : norm_res<kFp16, kFp16>(p, a->residual_type, vec, dev, st);
+        e = a->in_type == kFp32 ? norm_res<kFp32, kFp16>(p, a->residual_type, vec, st) : norm_res<kFp16, kFp16>(p, a->residual_type, vec, st);
     return e == cudaSuccess ? PLORA_OK : PLORA_ERR_CUDA;
 }
 
