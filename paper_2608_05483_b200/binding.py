@@ -560,27 +560,30 @@ _ACT_PACK = struct.Struct("@5i4x4q5P")
 _GEMM_PACK = struct.Struct("@8i9q15P")
 
 
+_kinds = {}       # type codes by torch type, filled when the torch layer is first used
+
+
 def _type_of(name, t) -> int:
-    if t.dtype is torch.bfloat16:
-        return INPUT_BF16
-    if t.dtype is torch.float32:
-        return INPUT_FP32
-    if t.dtype is torch.float16:
-        return INPUT_FP16
-    _bad(f"{name}: float32, bfloat16 or float16 expected, got {t.dtype}")
+    kind = _kinds.get(t.dtype)
+    if kind is None:
+        if not _kinds:
+            _kinds.update({torch.bfloat16: INPUT_BF16, torch.float16: INPUT_FP16, torch.float32: INPUT_FP32})
+            return _type_of(name, t)
+        _bad(f"{name}: float32, bfloat16 or float16 expected, got {t.dtype}")
+    return kind
 
 
 def _rows(name, t, n: int, d: int, dev: int) -> int:
-    """Elements between the rows of a CUDA tensor [n, d] whose rows are packed."""
-    if t.shape != (n, d) or not t.is_cuda or t.get_device() != dev:
+    """Elements between the rows of a CUDA tensor [n, d] whose rows are packed (dev: the inputs' device, at least 0)."""
+    if t.shape != (n, d) or t.get_device() != dev:
         _bad(f"{name}: CUDA tensor [{n}, {d}] on the inputs' device expected, got {list(t.shape)} on {t.device}")
     st, one = t.stride()
     if one != 1 and d > 1:
         _bad(f"{name}: packed rows expected")
-    if n < 2:
-        return d
     if st < d:       # (the C structures read 0 as packed; rows that overlap are not rows)
-        _bad(f"{name}: a tensor that is expanded along its rows is not supported")
+        if n > 1:
+            _bad(f"{name}: a tensor that is expanded along its rows is not supported")
+        return d
     return st
 
 
@@ -589,17 +592,24 @@ def _q_rows(name, q, n: int, d: int, dev: int) -> int:
     if q.dtype is not torch.float8_e4m3fn:
         _bad(f"{name}: float8_e4m3fn expected, got {q.dtype}")
     st = _rows(name, q, n, d, dev)
-    if n < 2:
-        return -(-d // 16) * 16
     if st % 16:
-        _bad(f"{name}: rows have to lie a multiple of 16 bytes apart")
+        if n > 1:
+            _bad(f"{name}: rows have to lie a multiple of 16 bytes apart")
+        return -(-d // 16) * 16
     return st
 
 
 def _scales(name, t, rows: int, cols: int, dev: int) -> int:
-    if t.dtype is not torch.float32 or t.shape != (rows, cols) or not t.is_cuda or not t.is_contiguous() or t.get_device() != dev:
+    if t.dtype is not torch.float32 or t.shape != (rows, cols) or not t.is_contiguous() or t.get_device() != dev:
         _bad(f"{name}: packed float32 CUDA tensor {[rows, cols]} on the inputs' device expected, got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
+
+
+def _device_of(name, t) -> int:
+    dev = t.get_device()
+    if dev < 0:
+        _bad(f"{name}: CUDA tensor expected, got one on {t.device}")
+    return dev
 
 
 def _q_empty(stream, n: int, d: int, device):
@@ -610,31 +620,22 @@ def _q_empty(stream, n: int, d: int, device):
     return (q if width == d else q[:, :d]), scale
 
 
-def _call_on(dev: int, fn, args, stream, t) -> int:
+def _call_on(name: str, dev: int, args, stream):
     """Makes the call with the inputs' device as the current one."""
-    if dev == torch.cuda.current_device():
-        return fn(args, _raw_stream(stream, t))
-    with torch.cuda.device(dev):
-        return fn(args, _raw_stream(stream, t))
+    fn = getattr(_lib or load(), name)
+    if dev == torch._C._cuda_getDevice():
+        rc = fn(args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if rc != OK:
+        raise PloraError(rc, name)
 
 
-def _outputs(n, d, dev, like, type16, out_type, fp8, y, q, scale, stream):
-    """(y, q, scale, the type of y, its code): the caller's buffers, or new ones where they are asked for."""
-    if (q is None) != (scale is None):
-        _bad("q and scale go together")
-    if y is not None:
-        out_type = y.dtype
-    elif out_type is not None:
-        y = _new_on(stream, torch.empty, (n, d), dtype=out_type, device=like.device)
-    if q is None and fp8:
-        q, scale = _q_empty(stream, n, d, like.device)
-    if out_type is None:
-        out_type = type16 or torch.bfloat16
-    if out_type is not torch.bfloat16 and out_type is not torch.float16:
-        _bad(f"y: bfloat16 or float16 expected, got {out_type}")
-    if type16 is not None and out_type is not type16:
-        _bad(f"y: the inputs' type, {type16}, expected, got {out_type}")
-    return y, q, scale, INPUT_BF16 if out_type is torch.bfloat16 else INPUT_FP16
+def _output_type(name, kind) -> int:
+    if kind == INPUT_FP32:
+        _bad(f"{name}: bfloat16 or float16 expected")
+    return kind
 
 
 def rms_norm(x, weight=None, eps: float = 1e-5, residual=None, residual_out=None, offset: float = 0.0, out_type=None, fp8: bool = False,
@@ -643,29 +644,25 @@ def rms_norm(x, weight=None, eps: float = 1e-5, residual=None, residual_out=None
     residual_out (None: to residual itself).  x is fp32, or of the 16-bit type; weight [d] of either.
     Outputs: y in 16 bits (out_type=torch.bfloat16 / float16, or a buffer) and an 8-bit matrix (fp8=True, or buffers q and scale)."""
     n, d = x.shape
-    dev = x.get_device()
-    in_type = _type_of("x", x)
-    type16 = None if in_type == INPUT_FP32 else x.dtype
-    for t in (weight, residual):
-        if type16 is None and t is not None and t.dtype is not torch.float32:
-            type16 = t.dtype
-    if type16 is None and y is None and out_type is None and q is None and not fp8 and residual is None:
-        _bad("nothing to write: neither y, q nor a residual")
-    y, q, scale, kind = _outputs(n, d, dev, x, type16, out_type, fp8, y, q, scale, stream)
-    wt = rt = kind
-    w_at = 0
+    dev = _device_of("x", x)
+    in_type = kind = _type_of("x", x)
+    if y is None and out_type is not None:
+        y = _new_on(stream, torch.empty, (n, d), dtype=out_type, device=x.device)
+    if fp8 and q is None and scale is None:
+        q, scale = _q_empty(stream, n, d, x.device)
+    xs = _rows("x", x, n, d, dev)
+    wt = rt = -1
+    w_at = rs = ros = r_at = ro_at = ys = y_at = qs = q_at = s_at = 0
+    if y is not None:
+        kind = _output_type("y", _type_of("y", y))
+        ys, y_at = _rows("y", y, n, d, dev), y.data_ptr()
     if weight is not None:
         wt = _type_of("weight", weight)
-        if weight.shape != (d,) or not weight.is_cuda or not weight.is_contiguous() or weight.get_device() != dev:
+        if weight.shape != (d,) or not weight.is_contiguous() or weight.get_device() != dev:
             _bad(f"weight: packed CUDA tensor [{d}] on x's device expected")
-        if wt != kind and wt != INPUT_FP32:
-            _bad("weight: float32 or the 16-bit type of the other tensors expected")
         w_at = weight.data_ptr()
-    rs = ros = r_at = ro_at = 0
     if residual is not None:
         rt = _type_of("residual", residual)
-        if rt != kind and rt != INPUT_FP32:
-            _bad("residual: float32 or the 16-bit type of the other tensors expected")
         if residual_out is None:
             residual_out = residual
         elif residual_out.dtype is not residual.dtype:
@@ -674,12 +671,22 @@ def rms_norm(x, weight=None, eps: float = 1e-5, residual=None, residual_out=None
         r_at, ro_at = residual.data_ptr(), residual_out.data_ptr()
     elif residual_out is not None:
         _bad("residual_out without a residual")
-    a = _NORM_PACK.pack(in_type, kind, wt, rt, n, d, _rows("x", x, n, d, dev), rs, ros, 0 if y is None else _rows("y", y, n, d, dev),
-                        0 if q is None else _q_rows("q", q, n, d, dev), x.data_ptr(), w_at, r_at, ro_at, 0 if y is None else y.data_ptr(),
-                        0 if q is None else q.data_ptr(), 0 if q is None else _scales("scale", scale, n, -(-d // 128), dev), eps, offset)
-    rc = _call_on(dev, load().plora_rms_norm, a, stream, x)
-    if rc != OK:
-        raise PloraError(rc, "plora_rms_norm")
+    if q is not None and scale is not None:
+        qs, q_at, s_at = _q_rows("q", q, n, d, dev), q.data_ptr(), _scales("scale", scale, n, (d + 127) // 128, dev)
+    elif q is not None or scale is not None:
+        _bad("q and scale go together")
+    elif y is None and residual is None:
+        _bad("nothing to write: neither y, q nor a residual")
+    # one 16-bit type: y's, or that of whichever of the others is not fp32 (bf16 where all are)
+    for t in (in_type, wt, rt):
+        if t >= 0 and t != INPUT_FP32 and t != kind:
+            if kind != INPUT_FP32:
+                _bad("x, weight, residual, y: float32 or one 16-bit type expected")
+            kind = t
+    if kind == INPUT_FP32:
+        kind = INPUT_BF16
+    _call_on("plora_rms_norm", dev, _NORM_PACK.pack(in_type, kind, kind if wt < 0 else wt, kind if rt < 0 else rt, n, d, xs, rs, ros, ys, qs,
+                                                    x.data_ptr(), w_at, r_at, ro_at, y_at, q_at, s_at, eps, offset), stream)
     return Act8(y, q, scale, residual_out)
 
 
@@ -689,23 +696,36 @@ _ACTS = {"none": ACT_NONE, "silu": ACT_SILU, "gelu": ACT_GELU}
 def gated_act(gate, up=None, act: str = "silu", out_type=None, fp8: bool = False, y=None, q=None, scale=None, stream=None) -> Act8:
     """act(gate) * up, or act(gate), for gate and up [n, d] (plora_gated_act); outputs as of rms_norm.  act: "silu", "gelu" (tanh form) or
     "none": with up=None the 8-bit form of a matrix."""
-    if act not in _ACTS:
+    code = _ACTS.get(act)
+    if code is None:
         _bad(f"act: one of {sorted(_ACTS)} expected, got {act!r}")
     n, d = gate.shape
-    dev = gate.get_device()
-    in_type = _type_of("gate", gate)
-    if up is not None and up.dtype is not gate.dtype:
-        _bad("gate and up: one type expected")
-    y, q, scale, kind = _outputs(n, d, dev, gate, None if in_type == INPUT_FP32 else gate.dtype, out_type, fp8, y, q, scale, stream)
-    if y is None and q is None:
+    dev = _device_of("gate", gate)
+    in_type = kind = _type_of("gate", gate)
+    if y is None and out_type is not None:
+        y = _new_on(stream, torch.empty, (n, d), dtype=out_type, device=gate.device)
+    if fp8 and q is None and scale is None:
+        q, scale = _q_empty(stream, n, d, gate.device)
+    us = u_at = ys = y_at = qs = q_at = s_at = 0
+    if up is not None:
+        if up.dtype is not gate.dtype:
+            _bad("gate and up: one type expected")
+        us, u_at = _rows("up", up, n, d, dev), up.data_ptr()
+    if y is not None:
+        kind = _output_type("y", _type_of("y", y))
+        if in_type != INPUT_FP32 and in_type != kind:
+            _bad("gate, up, y: float32 or one 16-bit type expected")
+        ys, y_at = _rows("y", y, n, d, dev), y.data_ptr()
+    if q is not None and scale is not None:
+        qs, q_at, s_at = _q_rows("q", q, n, d, dev), q.data_ptr(), _scales("scale", scale, n, (d + 127) // 128, dev)
+    elif q is not None or scale is not None:
+        _bad("q and scale go together")
+    elif y is None:
         _bad("nothing to write: neither y nor q")
-    a = _ACT_PACK.pack(in_type, kind, _ACTS[act], n, d, _rows("gate", gate, n, d, dev), 0 if up is None else _rows("up", up, n, d, dev),
-                       0 if y is None else _rows("y", y, n, d, dev), 0 if q is None else _q_rows("q", q, n, d, dev), gate.data_ptr(),
-                       0 if up is None else up.data_ptr(), 0 if y is None else y.data_ptr(), 0 if q is None else q.data_ptr(),
-                       0 if q is None else _scales("scale", scale, n, -(-d // 128), dev))
-    rc = _call_on(dev, load().plora_gated_act, a, stream, gate)
-    if rc != OK:
-        raise PloraError(rc, "plora_gated_act")
+    if kind == INPUT_FP32:
+        kind = INPUT_BF16
+    _call_on("plora_gated_act", dev, _ACT_PACK.pack(in_type, kind, code, n, d, _rows("gate", gate, n, d, dev), us, ys, qs, gate.data_ptr(),
+                                                    u_at, y_at, q_at, s_at), stream)
     return Act8(y, q, scale)
 
 
@@ -713,7 +733,7 @@ def quant_weight(w, stream=None):
     """A weight [n, k] (n: outputs, k: inputs) as an 8-bit matrix (q [n, k] e4m3, scale [ceil(n / 128), ceil(k / 128)]): a set-up call
     (plora_quant_weight)."""
     n, k = w.shape
-    dev = w.get_device()
+    dev = _device_of("w", w)
     kind, st = _type_of("w", w), _rows("w", w, n, k, dev)
     width = -(-k // 16) * 16
     q = _new_on(stream, torch.empty, (n, width), dtype=torch.float8_e4m3fn, device=w.device)[:, :k]
@@ -733,8 +753,8 @@ def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, strea
     if count < 1 or count > 4 or len(scales) != count:
         _bad("w, w_scale: one to four weights, each with its scales, expected")
     m, k = x.shape
-    dev = x.get_device()
-    blocks = -(-k // 128)
+    dev = _device_of("x", x)
+    blocks = (k + 127) // 128
     if out is None:
         kind = out_type or torch.float32
         outs = [_new_on(stream, torch.empty, (m, t.shape[0]), dtype=kind, device=x.device) for t in ws]
@@ -749,12 +769,15 @@ def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, strea
         if o.dtype is not kind:
             _bad("out: one type expected")
         ns[i], strides[i], out_strides[i] = n, _q_rows("w", t, n, k, dev), _rows("out", o, m, n, dev)
-        at[i], s_at[i], o_at[i] = t.data_ptr(), _scales("w_scale", s, -(-n // 128), blocks, dev), o.data_ptr()
-    a = _GEMM_PACK.pack(_type_of("out", outs[0]), m, k, count, *ns, _q_rows("x", x, m, k, dev), *strides, *out_strides, x.data_ptr(),
-                        _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, _opt_ints("status", status, (1,)))
-    rc = _call_on(dev, load().plora_gemm_fp8, a, stream, x)
-    if rc != OK:
-        raise PloraError(rc, "plora_gemm_fp8")
+        at[i], s_at[i], o_at[i] = t.data_ptr(), _scales("w_scale", s, (n + 127) // 128, blocks, dev), o.data_ptr()
+    status_at = 0
+    if status is not None:
+        status_at = _ints("status", status, (1,))
+        if status.get_device() != dev:
+            _bad("status: on the inputs' device expected")
+    _call_on("plora_gemm_fp8", dev, _GEMM_PACK.pack(_type_of("out", outs[0]), m, k, count, *ns, _q_rows("x", x, m, k, dev), *strides, *out_strides,
+                                                    x.data_ptr(), _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, status_at),
+             stream)
     return list(outs) if many else outs[0]
 
 
