@@ -26,7 +26,7 @@ constexpr int kMaxWeights = 4;
 constexpr int kThreads = 384, kAddWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kScaleWarp = 10;      // (two of the last)
 constexpr int kRows = 128;                // rows of x per CTA
 constexpr int kRowBytes = 128;            // one block of K
-constexpr int kScaleRun = 4, kScaleSlots = 4;          // blocks of K whose scales are staged together; such runs
+constexpr int kScaleRun = 8, kScaleSlots = 2;          // blocks of K whose scales are staged together; such runs
 constexpr int kScaleBytes = kScaleRun * (kRows + 4) * 4;    // of a run: sx [block][row], then sw [block][half of the columns][2]
 constexpr int kMaxStages = 16;
 constexpr int kRingOffset = (kScaleSlots * kScaleBytes + 512 + 1023) / 1024 * 1024;        // scales, barriers and words lie in front of the ring
@@ -46,7 +46,9 @@ struct Cfg {
     static constexpr int kAccs = kTmemCols / (BN * kRun) > 4 ? 4 : kTmemCols / (BN * kRun);
     static constexpr int kCols = BN / 2;                  // columns of a thread
     static constexpr bool kCrosses = kBlock % kCols != 0; // a half may lie in two blocks of w's rows
-    static constexpr int kRead = 16;      // columns read at a time (two such buffers beside the sums)
+    // Columns read from tensor memory at a time: 32 (4 % faster in tiles of 160 columns), but 16 where the halves are multiples of 32,
+    // for reads of 32 take far longer there (tiles of 256 columns 359 against 294 us for 4096 x 8192 x 8192, of 128 367 against 329).
+    static constexpr int kRead = kCols % 32 == 0 ? 16 : 32;
     static constexpr int kPitch = BN + 4; // floats between the rows of a partial tile in shared memory (4 banks apart, accesses of 16 bytes)
     static_assert(BN % 32 == 0 && kBBytes % 1024 == 0, "");
 };
@@ -102,11 +104,36 @@ __device__ __forceinline__ void umma_commit(uint32_t bar) {
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(a));
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
                    "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(a));
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t* r) {
+    if (N == 32) tmem_ld32(a, r);
+    else tmem_ld16(a, r);
+}
+__device__ __forceinline__ float lds32(uint32_t a) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ float2 lds64(uint32_t a) {
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
+    return v;
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // A box of rows of 128 bytes.  In a pair the barrier may be the other CTA's.
@@ -126,6 +153,10 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* tm, int
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
 }
+__device__ __forceinline__ int opaque(int v) {     // the same value, but the compiler does not know
+    asm volatile("" : "+r"(v));
+    return v;
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -136,10 +167,18 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {     /
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-// (Hands nothing over in memory, only the right to tensor memory, whose reads are complete: a release at cluster scope cost the
-// warps that add some 800 cycles per block of K.)
-__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// An arrival by the lanes that say so, without a branch.  REMOTE: at a barrier of the cluster; it hands nothing over in memory, only the
+// right to tensor memory, whose reads are complete (a release at cluster scope cost the warps that add some 800 cycles per block of K).
+template <bool REMOTE>
+__device__ __forceinline__ void arrive_if(uint32_t bar, bool yes) {
+    if (REMOTE)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n\t}" ::"r"(bar),
+            "r"((uint32_t)yes)
+            : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"((uint32_t)yes)
+                     : "memory");
 }
 __device__ __forceinline__ float4 ld_cluster(uint32_t a) {
     float4 v;
@@ -388,7 +427,7 @@ __device__ __forceinline__ void scale_warps(const Params& p, const Smem& sm, uin
         const Tile t = tile_of(p, i);
         const int row0 = (t.mt * CG + (CG == 2 ? (int)rank : 0)) * kRows;
         const float *x0 = p.x_scale + (size_t)min(row0 + r0, p.m - 1) * p.blocks, *x1 = p.x_scale + (size_t)min(row0 + r0 + 64, p.m - 1) * p.blocks;
-        // thread 4 j + 2 h + i of the 64: block j of the run, half h, i-th of its blocks
+        // thread 4 j + 2 h + i of the first 32: block j of the run, half h, i-th of its blocks
         const int j4 = r0 >> 2, wb = block_of(t.nt * BN + (r0 >> 1 & 1) * C::kCols) + (r0 & 1);
         const float* w0 = p.w_scale[t.w] + (size_t)min(wb, block_of(p.n[t.w] - 1)) * p.blocks;
 #pragma unroll 1
@@ -415,63 +454,83 @@ __device__ __forceinline__ void scale_warps(const Params& p, const Smem& sm, uin
     }
 }
 
-// Scales and adds the accumulators of one tile: row (warp & 3) * 32 + lane of the CTA's, half warp >> 2 of the columns, from `col` on.
+// Scales and adds the accumulators of one tile: row (warp & 3) * 32 + lane of the CTA's, half warp >> 2 of the columns, of which the
+// first `first` lie in the half's first block.  These warps bound the kernel (a block took them 1010 cycles in tiles of 256 columns, 520
+// of them to read and add), so a block's scales are fetched while the one before it is read, and places and addresses are kept.
 template <int CG, int BN>
-__device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t tmem, const Share& sh, bool any, int col, int warp, int lane,
-                                         Turn<Cfg<CG, BN>::kAccs>& in, Turn<kScaleSlots>& run, float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
+__device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t from, uint32_t hand_back, int blocks, bool any, int first, Turn<Cfg<CG, BN>::kAccs>& in,
+                                         Turn<kScaleSlots>& run, float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
     using C = Cfg<CG, BN>;
-    const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + (warp >> 2) * C::kCols;
-    const int first = left_in_block(col);        // columns of the half's first block
+    const unsigned all = 0xffffffffu;
+    const int lane = threadIdx.x & 31;
+    const uint32_t sx = smem_u32(sm.scales) + (threadIdx.x & 127) * 4, sw = smem_u32(sm.scales) + kScaleRun * kRows * 4 + (threadIdx.x >> 7) * 8;
 #pragma unroll
     for (int i = 0; i < C::kCols / 2; ++i) acc[i] = make_float2(0.f, 0.f);
 #pragma unroll 1
-    for (int left = sh.b1 - sh.b0; left > 0; left -= kScaleRun, run.next()) {
-        if (!__all_sync(0xffffffffu, wait(sm.scale_full + run.at * 8, run.parity, sm.wc))) return false;
-        const float* sx = sm.scales + run.at * (kScaleBytes / 4) + (warp & 3) * 32 + lane;
-        const float* sw = sm.scales + run.at * (kScaleBytes / 4) + kScaleRun * kRows + (warp >> 2) * 2;
-#pragma unroll 1
-        for (int j = 0; j < min(left, kScaleRun); j += C::kRun, in.next()) {
-            const uint32_t a = in.at;
-            float2 f[C::kRun], g[C::kRun];        // the scales in the half's first and second block
+    for (; blocks > 0; blocks -= kScaleRun, run.next()) {
+        if (!__all_sync(all, wait(sm.scale_full + run.at * 8, run.parity, sm.wc))) return false;
+        float x[C::kRun];
+        float2 w[C::kRun];
+        auto fetch = [&](int j) {
 #pragma unroll
             for (int r = 0; r < C::kRun; ++r) {
-                const float x = sx[(j + r) * kRows], u = x * sw[(j + r) * 4], v = C::kCrosses ? x * sw[(j + r) * 4 + 1] : 0.f;
-                f[r] = make_float2(u, u);
-                g[r] = make_float2(v, v);
+                x[r] = lds32(sx + run.at * kScaleBytes + (j + r) * kRows * 4);
+                w[r] = lds64(sw + run.at * kScaleBytes + (j + r) * 16);
             }
-            if (!__all_sync(0xffffffffu, wait(sm.acc_full + a * 8, in.parity, sm.wc))) return false;
+        };
+        fetch(0);
+        const int here = min(blocks, kScaleRun);
+#pragma unroll 1
+        for (int j = 0; j < here; j += C::kRun, in.next()) {
+            const uint32_t a = in.at;
+            if (!__all_sync(all, wait(sm.acc_full + a * 8, in.parity, sm.wc))) return false;
             tc_fence_after();
             if (any) {        // (a row of this warp exists)
-                constexpr int kReads = C::kCols / C::kRead;
-                auto column = [&](int i) { return from + (a * C::kRun + i / kReads) * BN + i % kReads * C::kRead; };
-                uint32_t buf[2][C::kRead];
-                tmem_ld16(column(0), buf[0]);
+                uint32_t buf[C::kRead];
+                tmem_ld<C::kRead>(from + a * C::kRun * BN, buf);
+                float2 f[C::kRun], g[C::kRun];        // the scales in the half's first and second block
 #pragma unroll
-                for (int i = 0; i < C::kRun * kReads; ++i) {
-                    tmem_ld_wait();
-                    if (i + 1 < C::kRun * kReads) tmem_ld16(column(i + 1), buf[(i + 1) & 1]);
-                    const float* v = reinterpret_cast<const float*>(buf[i & 1]);
-                    const int c = i % kReads;
-                    const float2 s2 = C::kCrosses && c * C::kRead >= first ? g[i / kReads] : f[i / kReads];
-#pragma unroll
-                    for (int e = 0; e < C::kRead / 2; ++e) {
-                        float2& o = acc[c * (C::kRead / 2) + e];
-                        o = __ffma2_rn(make_float2(v[2 * e], v[2 * e + 1]), s2, o);
-                    }
+                for (int r = 0; r < C::kRun; ++r) {
+                    f[r] = make_float2(x[r] * w[r].x, x[r] * w[r].x);
+                    g[r] = C::kCrosses ? make_float2(x[r] * w[r].y, x[r] * w[r].y) : f[r];
                 }
+                if (j + C::kRun < here) fetch(j + C::kRun);
+#pragma unroll
+                for (int r = 0; r < C::kRun; ++r)
+#pragma unroll
+                    for (int c = 0; c < C::kCols; c += C::kRead) {
+                        const bool whole = c + C::kRead <= C::kCols;        // (or the last 16 columns)
+                        if (r > 0 || c > 0) {
+                            if (whole) tmem_ld<C::kRead>(from + (a * C::kRun + r) * BN + c, buf);
+                            else tmem_ld<16>(from + (a * C::kRun + r) * BN + c, buf);
+                        }
+                        tmem_ld_wait();
+                        const float* v = reinterpret_cast<const float*>(buf);
+#pragma unroll
+                        for (int e = 0; e < (whole ? C::kRead / 2 : 8); ++e) {
+                            float2& o = acc[c / 2 + e];
+                            o = __ffma2_rn(make_float2(v[2 * e], v[2 * e + 1]), C::kCrosses && c + e / 8 * 16 >= first ? g[r] : f[r], o);
+                        }
+                    }
             }
             tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (CG == 2) arrive_cluster(in_cta(sm.acc_empty + a * 8, 0));
-                else mbar_arrive(sm.acc_empty + a * 8);
-            }
+            arrive_if<CG == 2>(hand_back + a * 8, lane == 0);        // (the warp's reads are complete: it reads as one)
         }
-        if (lane == 0) mbar_arrive(sm.scale_empty + run.at * 8);
+        __syncwarp();
+        arrive_if<false>(sm.scale_empty + run.at * 8, lane == 0);
     }
     return true;
 }
 
+// 32 bytes of a row.
+template <int KIND>
+__device__ __forceinline__ void words_of(const float* v, uint32_t (&w)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        w[i] = KIND == PLORA_INPUT_FP32 ? __float_as_uint(v[i]) : pack16<KIND == PLORA_INPUT_FP16>(v[KIND == PLORA_INPUT_FP32 ? 0 : 2 * i], v[KIND == PLORA_INPUT_FP32 ? 0 : 2 * i + 1]);
+}
+// Row `row` of the tile's half, kCols columns from `col` on: each lane writes its row in pieces of 32 bytes.  (Four lanes to a piece of 64
+// bytes through shared memory took as long: what a tile's end waits for is the write itself, 128 KB per CTA.)
 template <int CG, int BN, int KIND>
 __device__ __forceinline__ void store_tile(const Params& p, const Tile& t, int row, int col, const float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
     using C = Cfg<CG, BN>;
@@ -484,9 +543,7 @@ __device__ __forceinline__ void store_tile(const Params& p, const Tile& t, int r
         const float* v = reinterpret_cast<const float*>(acc) + c;
         if (p.vec >= 16 && col + c + kStep <= n) {
             uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                w[i] = KIND == PLORA_INPUT_FP32 ? __float_as_uint(v[i]) : pack16<KIND == PLORA_INPUT_FP16>(v[(2 * i) % kStep], v[(2 * i + 1) % kStep]);
+            words_of<KIND>(v, w);
             char* o = static_cast<char*>(p.out[t.w]) + (at + c) * kSize;
             if (p.vec == 32) {
                 st_global32(o, w);
@@ -564,18 +621,20 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
     const uint32_t tmem = *sm.tmem_slot;
     const Share sh = share_of<CG, Cfg<CG, BN>::kRun>(p, rank);
     if (warp < kAddWarps) {
-        if (BN > 192) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        if (BN > 192) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         paged::grid_wait();
         if (threadIdx.x == 0) paged::grid_launch_dependents();     // (what the kernel in front wrote is complete by now)
         const int r = (CG == 2 ? (int)rank * kRows : 0) + (warp & 3) * 32 + lane, c = (warp >> 2) * C::kCols;
+        const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + c, hand_back = CG == 2 ? in_cta(sm.acc_empty, 0) : sm.acc_empty;
         Turn<C::kAccs> in;
         Turn<kScaleSlots> run;
         float2 acc[C::kCols / 2];
 #pragma unroll 1
         for (int i = sh.first; i < p.tiles; i += sh.step) {
-            const Tile t = tile_of(p, i);
+            const Tile u = tile_of(p, i);
+            if (!add_tile<CG, BN>(sm, from, hand_back, sh.b1 - sh.b0, u.mt * CG * kRows + r - lane < p.m, left_in_block(u.nt * BN + c), in, run, acc)) break;
+            const Tile t = tile_of(p, opaque(i));       // (made again rather than kept beside the sums)
             const int row = t.mt * CG * kRows + r, col = t.nt * BN + c;
-            if (!add_tile<CG, BN>(sm, tmem, sh, row - lane < p.m, col, warp, lane, in, run, acc)) break;
             if (CG == 2 || p.splits == 1) {
                 store_tile<CG, BN, KIND>(p, t, row, col, acc);
             } else if (row < p.m) {       // all products are complete: the ring is free for the partial tile
