@@ -12,7 +12,14 @@ The first step takes the prompts; the later ones generate a token per request.  
 same tokens (its system prompt): their pages are shared from the second request on, and the single-token steps read
 them once per adapter, the requests being sorted by adapter.
 
-    python examples/serve_layer.py [--steps N]
+With --block the layer is a whole decoder block with its base weights in 8 bits and adapters on all seven projections:
+
+    norm      x to 16 bits (the adapters' input) and to 8 bits    rms_norm (the second one adds the residual)
+    product   the base projections, fp32 y                        gemm_fp8 (q, k, v in one call; up and gate in one)
+    delta, rotary, attention                                      as above
+    to 8 bits what the next product reads                         gated_act (silu(gate) * up; the attention's output as it is)
+
+    python examples/serve_layer.py [--steps N] [--block]
 """
 import argparse
 import sys
@@ -60,6 +67,47 @@ class Layer:
         y = (o @ self.W[3]).float()
         self.ctx.lora_delta(o, ids, 0, 3, y)
         return y
+
+
+class Block(Layer):
+    """A decoder block: norm, attention layer, norm with the residual, gated FFN.  Projections q k v o up gate down."""
+
+    def __init__(self, ffn=1024, n_adapters=3, rank=16, seed=0, **kw):
+        super().__init__(n_adapters=n_adapters, rank=rank, seed=seed, **kw)
+        g = torch.Generator(device="cuda").manual_seed(seed + 1)
+        rnd = lambda *s, std=1.0: (torch.randn(*s, generator=g, device="cuda") * std).bfloat16()
+        ins, widths = [self.hidden, self.hidden, ffn], [ffn, ffn, self.hidden]
+        self.W += [rnd(i, o, std=i ** -0.5) for i, o in zip(ins, widths)]
+        self.A += [[rnd(i, rank, std=i ** -0.5) for _ in range(n_adapters)] for i in ins]
+        self.B += [[rnd(rank, o, std=rank ** -0.5) for _ in range(n_adapters)] for o in widths]
+        for proj in range(4, 7):
+            self.ctx.register_pool(0, proj, ins[proj - 4], widths[proj - 4], [rank] * n_adapters, [0.5] * n_adapters, self.A[proj], self.B[proj])
+        self.gain = [rnd(self.hidden, std=0.2) + 1.0 for _ in range(2)]
+        self.W8 = [P.quant_weight(w.t().contiguous()) for w in self.W]           # once: [d_out, d_in], a scale per 128 x 128
+
+    def project(self, a, x, ids, projs):
+        """y = x W + s (x A) B of projections that share their input: a its 8-bit form, x the 16-bit one.  fp32."""
+        ys = P.gemm_fp8(a.q, a.scale, [self.W8[p][0] for p in projs], [self.W8[p][1] for p in projs])
+        self.ctx.lora_delta_group([x] * len(projs), ids, [0] * len(projs), projs, ys)
+        return ys
+
+    def step(self, x, ids, plan, block_table, **attn):
+        """x [n_tok, hidden] bf16: the residual stream.  Returns it with the block's sum, fp32."""
+        n, res = x.shape[0], x.clone()
+        self.ctx.bucket(ids, self.n_adapters)
+        heads = lambda y, h: y.view(n, h, self.d)
+        a = P.rms_norm(res, self.gain[0], out_type=torch.bfloat16, fp8=True)
+        q, k, v = self.project(a, a.y, ids, [0, 1, 2])
+        q = P.rope_cache(heads(q, self.n_q), heads(k, self.n_kv), heads(v, self.n_kv), plan.positions[:n], plan.slots[:n], self.table,
+                         self.k_cache, self.v_cache)
+        o, _ = P.attn_paged(q, self.k_cache, self.v_cache, block_table, plan.kv_len, self.d ** -0.5, **attn)
+        o = o.view(n, -1)
+        y, = self.project(P.gated_act(o, act="none", fp8=True), o, ids, [3])
+        a = P.rms_norm(y, self.gain[1], residual=res, out_type=torch.bfloat16, fp8=True)     # res += y
+        up, gate = self.project(a, a.y, ids, [4, 5])
+        b = P.gated_act(gate, up, out_type=torch.bfloat16, fp8=True)
+        y, = self.project(b, b.y, ids, [6])
+        return res.float() + y
 
 
 def serve(layer, system, prompts, adapters, new_tokens):
@@ -110,8 +158,13 @@ def serve(layer, system, prompts, adapters, new_tokens):
 def reference(layer, x, adapter):
     """The same layer over one request's whole sequence, in 64 bits."""
     W = [w.double() + 0.5 * (a[adapter].double() @ b[adapter].double()) for w, a, b in zip(layer.W, layer.A, layer.B)]
+    return attention(layer, x.double(), W)
+
+
+def attention(layer, x, W):
+    """Attention of a whole sequence through q, k, v and o, in 64 bits."""
     n, d = x.shape[0], layer.d
-    q, k, v = (x.double() @ w for w in W[:3])
+    q, k, v = (x @ w for w in W[:3])
     pos = torch.arange(n, device=x.device)
     cs = layer.table[pos].double()
 
@@ -128,8 +181,19 @@ def reference(layer, x, adapter):
     return torch.einsum("htk,khd->thd", torch.softmax(s, -1), v).reshape(n, -1) @ W[3]
 
 
-def main(steps=4):
-    layer = Layer()
+def reference_block(block, x, adapter):
+    """The block over one request's whole sequence, in 64 bits, from its 16-bit weights."""
+    W = [w.double() + 0.5 * (a[adapter].double() @ b[adapter].double()) for w, a, b in zip(block.W, block.A, block.B)]
+    norm = lambda h, gain: h / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-5) * gain.double()
+    h = x.double()
+    h = h + attention(block, norm(h, block.gain[0]), W)
+    y = norm(h, block.gain[1])
+    gate = y @ W[5]
+    return h + (gate * torch.sigmoid(gate) * (y @ W[4])) @ W[6]
+
+
+def main(steps=4, block=False):
+    layer = Block() if block else Layer()
     g = torch.Generator(device="cuda").manual_seed(1)
     rnd = lambda n: torch.randn(n, layer.hidden, generator=g, device="cuda").bfloat16()
     system = [rnd(n) for n in (70, 16, 5)]
@@ -140,9 +204,9 @@ def main(steps=4):
     worst = 0.0
     for r, a in enumerate(adapters):
         x = torch.cat([system[a], prompts[r], *[t[r:r + 1] for t in new]])
-        want = reference(layer, x, a)
+        want = reference_block(layer, x, a) if block else reference(layer, x, a)
         worst = max(worst, float((outs[r].double() - want).abs().max() / want.abs().max()))
-    print(f"serve_layer: {len(prompts)} requests, {steps} single-token steps, worst error {worst:.2e} of the largest output")
+    print(f"serve_{'block' if block else 'layer'}: {len(prompts)} requests, {steps} single-token steps, worst error {worst:.2e} of the largest output")
     layer.ctx.close()
     return worst
 
@@ -150,4 +214,6 @@ def main(steps=4):
 if __name__ == "__main__":
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=4)
-    main(ap.parse_args().steps)
+    ap.add_argument("--block", action="store_true")
+    args = ap.parse_args()
+    main(args.steps, args.block)

@@ -574,7 +574,7 @@ PLORA_API plora_status plora_attn_paged(const plora_paged_attn *args, void *stre
  *   weights      q [n][k], scale [ceil(n / 128)][ceil(k / 128)]: one per 128 x 128; n is d_out, k is d_in
  * q is 16-byte aligned, its stride a multiple of 16 (0: cols rounded up to 16); bytes between the columns' end and the stride
  * are neither read as values nor written.  Scales are packed.  The calls below that make 8-bit matrices take
- * s = max(max|v| / 448, 2^-126) over the block and round v / s to nearest even (v / s is good to a few 2^-24; a NaN or an infinity
+ * s = max(max|v| / 448, 2^-126) over the block and round v / s to nearest even (v / s is good to a few 2^-23; a NaN or an infinity
  * in a block makes its scale one).
  *
  * plora_rms_norm:  h = x + residual;  v = h * rsqrt(mean(h^2) + eps) * (weight + offset)  per row of d columns, in fp32.
@@ -586,7 +586,7 @@ PLORA_API plora_status plora_attn_paged(const plora_paged_attn *args, void *stre
  *   q, scale                v as an 8-bit matrix, or both NULL
  * At least one of y, q, residual_out.  d <= 32768.  Strides count elements (q's: bytes); 0 means packed.  Any strides and
  * alignments of whole elements work (q excepted); where all rows are 16-byte aligned (fp32: 32) and d is a multiple of 8
- * the accesses are wide.  The first 16 rows or 16000 give the same bits for a row. */
+ * the accesses are wide.  A row's result does not depend on the rows beside it, to the bit. */
 typedef struct {
     int32_t in_type, type, weight_type, residual_type, n, d;
     int64_t x_stride, residual_stride, residual_out_stride, y_stride, q_stride;
@@ -621,8 +621,8 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
  * gate and up), in one launch:
  *     out[r][c] = sum_b x_scale[r][b] w_scale[c / 128][b] sum_{k in block b} x[r][k] w[c][k]
  * Sums in fp32, rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
- * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; 32-byte aligned
- * rows are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1.
+ * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; rows aligned to
+ * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1.
  * The weights are read before the kernel in front has completed if that kernel is one of this library's: they have to be complete
  * before it begins (weights made by plora_quant_weight, copies or any other library's kernels always are).
  * The kernel takes up to all 512 tensor-memory columns of an SM; as with plora_lora_delta's tensor-core path, do not run it
