@@ -6,8 +6,17 @@
 // next accumulator.  (The tensor cores' sum over a block of 128 is exact to fp32 rounding here: measured error 0 against 64 bits.)
 //
 // Roles: warps 0-7 scale and add, a row per thread and half of the tile's columns per warpgroup; warp 8 loads (a box of x and one
-// of w per block of K, 128-byte rows, swizzled); warp 9 issues the products; warps 10 and 11 stage the scales' products, some blocks ahead (loaded
-// by the adding warps themselves, a line per row, they cost those 140 of 870 cycles per block).
+// of w per block of K, 128-byte rows, swizzled); warp 9 issues the products; warps 10 and 11 stage the scales, some blocks ahead
+// (loaded by the adding warps themselves, a line per row, they cost those 140 of 870 cycles per block).
+//
+// Forms: pairs of CTAs share tiles of 256 rows (cta_group::2: each holds half of w's rows, so that a tile needs two thirds of the copies);
+// single CTAs take tiles of 128 rows, and clusters of them split K where tiles are few, each leaving its sums in shared memory for
+// the others to add in the order of K.  Tiles have 64 to 256 columns; choose() estimates what is fastest.
+//
+// What bounds it.  Few rows: HBM (64 rows by 27648 x 5120 27.3 us, 5.5 TB/s), a launch's start and the first copies (12288 x 4096 by one
+// row 12.0 us, of which 7.7 are the weights).  Many rows: 4096 x 8192 x 8192 takes 300 us, 1.8 PFLOP/s at the power limit of 1000 W and
+// 1.5 to 1.6 GHz.  Without its reads and additions it takes 241, with the reads alone 262: tensor memory serves the products and the
+// reads, and energy goes into both.  (The library's product of the same operands with one scale for all takes 228 for long, 185 in a burst.)
 #include "w8.cuh"
 
 namespace plora {
@@ -268,8 +277,8 @@ __device__ __forceinline__ Share share_of(const Params& p, uint32_t rank) {
 }
 
 struct Smem {
-    uint32_t ring, full, empty, acc_full, acc_empty, scale_full, scale_empty, done;
-    float* scales;       // [run][block][half of the columns][row]
+    uint32_t ring, full, empty, acc_full, acc_empty, scale_full, scale_empty, done, peer;
+    float* scales;       // [run]: sx [block][row], then sw [block][half of the columns][2]
     uint32_t* tmem_slot;
     WaitCtl wc;
 };
@@ -576,8 +585,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
     sm.scale_full = sm.acc_empty + C::kAccs * 8;
     sm.scale_empty = sm.scale_full + kScaleSlots * 8;
     sm.done = sm.scale_empty + kScaleSlots * 8;
+    sm.peer = sm.done + 8;
     sm.scales = reinterpret_cast<float*>(base);
-    constexpr int kBars = 2 * kMaxStages + 2 * C::kAccs + 2 * kScaleSlots + 1;
+    constexpr int kBars = 2 * kMaxStages + 2 * C::kAccs + 2 * kScaleSlots + 2;
     static_assert(kScaleSlots * kScaleBytes + kBars * 8 + 16 <= kRingOffset, "");
     sm.tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars * 8);
     sm.wc.abort_flag = reinterpret_cast<volatile int*>(bars + kBars * 8 + 8);
@@ -598,6 +608,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
             mbar_init(sm.scale_empty + r * 8, kAddWarps);
         }
         mbar_init(sm.done, 1);
+        mbar_init(sm.peer, 1);
         sm.wc.abort_flag[0] = 0;
         mbar_init_fence();
     }
@@ -605,25 +616,22 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
         prefetch_map(&maps.x);
         prefetch_map(&maps.w[0]);
     }
-    if (warp == kMmaWarp) {
-        if (CG == 2) {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(sm.tmem_slot)), "n"(C::kTmemCols) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(sm.tmem_slot)), "n"(C::kTmemCols) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        }
-        tc_fence_before();
-    }
     __syncthreads();
     if (CG == 2) cluster_sync();        // the other CTA's barriers exist
-    tc_fence_after();
-    const uint32_t tmem = *sm.tmem_slot;
+    // Tensor memory is taken when the kernel in front has completed, not before: it may have let this one start before it took
+    // its own.  (The loads of weights do not wait for that.)  The next kernel may start when this one has its tensor memory.
+    uint32_t tmem = 0;
+    auto tmem_taken = [&] {
+        asm volatile("bar.sync 1, %0;" ::"n"((kAddWarps + 1) * 32) : "memory");
+        tc_fence_after();
+        tmem = *sm.tmem_slot;
+    };
     const Share sh = share_of<CG, Cfg<CG, BN>::kRun>(p, rank);
     if (warp < kAddWarps) {
         if (BN > 192) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         paged::grid_wait();
-        if (threadIdx.x == 0) paged::grid_launch_dependents();     // (what the kernel in front wrote is complete by now)
+        tmem_taken();
+        if (threadIdx.x == 0) paged::grid_launch_dependents();
         const int r = (CG == 2 ? (int)rank * kRows : 0) + (warp & 3) * 32 + lane, c = (warp >> 2) * C::kCols;
         const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + c, hand_back = CG == 2 ? in_cta(sm.acc_empty, 0) : sm.acc_empty;
         Turn<C::kAccs> in;
@@ -646,8 +654,21 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
     } else {
         if (BN > 192) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == kLoadWarp) load_warp<CG, BN>(p, maps, sm, rank);
-        else if (warp == kMmaWarp && (CG == 1 || rank == 0)) mma_warp<CG, BN>(p, sm, tmem, rank);
-        else if (warp >= kScaleWarp) scale_warps<CG, BN>(p, sm, rank);
+        if (warp == kMmaWarp) {
+            paged::grid_wait();
+            if (CG == 2) {
+                asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(sm.tmem_slot)), "n"(C::kTmemCols) : "memory");
+                asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+            } else {
+                asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(sm.tmem_slot)), "n"(C::kTmemCols) : "memory");
+                asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+            }
+            tc_fence_before();
+            tmem_taken();
+            if (CG == 2 && rank == 1) arrive_if<true>(in_cta(sm.peer, 0), lane == 0);        // products write into this CTA's, too
+            else if (CG == 1 || __all_sync(0xffffffffu, wait(sm.peer, 0, sm.wc))) mma_warp<CG, BN>(p, sm, tmem, rank);
+        }
+        if (warp >= kScaleWarp) scale_warps<CG, BN>(p, sm, rank);
         __syncwarp();
     }
     tc_fence_before();
@@ -689,18 +710,18 @@ cudaError_t go(const Maps& maps, Params p, paged::Device dev, cudaStream_t st) {
     static paged::Configured configured;
     const cudaError_t e = configured.ensure(reinterpret_cast<const void*>(kern), C::kSmemMost, dev.id);
     if (e != cudaSuccess) return e;
+    const int cluster = CG == 2 ? 2 : p.splits, most = p.splits > 1 ? p.tiles : dev.sms * C::kCtas / CG;
     // As deep a ring as fits, with 128 rows of x (or the rows of a partial tile) behind the start of its last stage.
     const int stage = C::kRun * (p.x_bytes + C::kBBytes), room = C::kSmemMost - 1024 - kRingOffset;
     const int last_x = stage - (C::kRun - 1) * p.x_bytes, behind = kRows * kRowBytes > last_x ? kRows * kRowBytes - last_x : 0;
     p.stages = (room - behind) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
-    const int most_stages = (p.blocks + C::kRun - 1) / C::kRun;
-    if (p.stages > most_stages) p.stages = most_stages;
+    const int stages_of_k = (p.blocks + C::kRun - 1) / C::kRun;
+    if (p.tiles <= most && p.stages > stages_of_k) p.stages = stages_of_k;        // (a CTA has one tile)
     int ring = p.stages * stage + behind;
     const int rows = p.m < kRows ? p.m : kRows, part = p.splits > 1 ? rows * C::kPitch * 4 : 0;
     if (ring < part) ring = part;
     const int smem = 1024 + kRingOffset + ring;
-    const int cluster = CG == 2 ? 2 : p.splits, most = p.splits > 1 ? p.tiles : dev.sms * C::kCtas / CG;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
