@@ -622,7 +622,7 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
  *     out[r][c] = sum_b x_scale[r][b] w_scale[c / 128][b] sum_{k in block b} x[r][k] w[c][k]
  * Sums in fp32, rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
  * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; rows aligned to
- * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1.
+ * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1 up to 2^30.
  * The weights are read before the kernel in front has completed if that kernel is one of this library's: they have to be complete
  * before it begins (weights made by plora_quant_weight, copies or any other library's kernels always are).
  * The kernel takes up to all 512 tensor-memory columns of an SM; as with plora_lora_delta's tensor-core path, do not run it

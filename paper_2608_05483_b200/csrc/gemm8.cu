@@ -779,6 +779,7 @@ Form choose(const plora_gemm_fp8_args* a, int blocks, int sms) {
             const double hand_over = bn <= 128 ? 0.17 : bn == 160 ? 0.37 : 0.12 + 0.0017 * bn;
             const bool two = cg == 1 && bn == 64;        // CTAs on an SM
             for (int s = 1; s <= (cg == 1 ? 8 : 1) && (s == 1 || blocks >= 2 * s); ++s) {
+                if (s > 1 && rows * cols * (s - 1) >= sms * (two ? 2 : 1)) break;        // (one part less fills the SMs already)
                 // (clusters do not fill the processing clusters of 16 to 20 SMs that they have to lie in: percent of the CTAs that
                 // fit at one time, by the size of a cluster, as the occupancy query gives them on a B200)
                 static const int fit[2][9] = {{0, 100, 100, 91, 89, 87, 89, 70, 81}, {0, 100, 100, 94, 95, 94, 91, 87, 89}};
@@ -854,6 +855,11 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
         p.out[i] = a->out[i];
         p.n[i] = a->n[i];
     }
+    // (rows, columns and their products with tile numbers are counted in 32 bits)
+    constexpr int kMost = 1 << 30;
+    if (a->m > kMost || a->k > kMost) return PLORA_ERR_UNSUPPORTED;
+    for (int i = 0; i < a->n_weights; ++i)
+        if (a->n[i] > kMost) return PLORA_ERR_UNSUPPORTED;
     plora::paged::Device dev;
     if (device(dev) != cudaSuccess) return PLORA_ERR_CUDA;
     if (!plora::paged::encode_tiled()) return PLORA_ERR_UNSUPPORTED;

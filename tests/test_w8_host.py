@@ -90,6 +90,7 @@ def test_more_refusals():
     assert lib.plora_rms_norm(None, 0) == lib.plora_gated_act(None, 0) == lib.plora_gemm_fp8(None, 0) == P.ERR_INVALID_ARG
     assert _norm(d=32769) == P.ERR_UNSUPPORTED
     assert _act(n=1 << 24, d=1 << 14) == P.ERR_UNSUPPORTED
+    assert _gemm(m=(1 << 30) + 1) == _gemm(n=(0, (1 << 30) + 1), out_stride=(0, 1 << 31)) == _gemm(k=(1 << 30) + 1) == P.ERR_UNSUPPORTED
     q = P.plora_quant_weight
     for bad in ((None, 0, 4, 64, 0, AT, 0, AT), (AT, 3, 4, 64, 0, AT, 0, AT), (AT, 0, -1, 64, 0, AT, 0, AT), (AT, 0, 4, 0, 0, AT, 0, AT),
                 (AT, 0, 4, 64, 32, AT, 0, AT), (AT, 0, 4, 64, 0, AT + 8, 0, AT), (AT, 0, 4, 64, 0, AT, 72, AT), (AT, 0, 4, 64, 0, AT, 0, None),
