@@ -573,6 +573,8 @@ def _type_of(name, t) -> int:
     return kind
 
 
+# (The calls look at the usual layout in place, one line per tensor, and leave what is not usual to these helpers, which refuse what has
+# to be refused: a helper call per tensor cost 0.6 us of the 8 that a small norm takes.)
 def _rows(name, t, n: int, d: int, dev: int) -> int:
     """Elements between the rows of a CUDA tensor [n, d] whose rows are packed (dev: the inputs' device, at least 0)."""
     if t.shape != (n, d) or t.get_device() != dev:
@@ -643,19 +645,25 @@ def rms_norm(x, weight=None, eps: float = 1e-5, residual=None, residual_out=None
     """Root-mean-square norm of the rows of x [n, d] (plora_rms_norm), x + residual first if there is a residual: the sum goes to
     residual_out (None: to residual itself).  x is fp32, or of the 16-bit type; weight [d] of either.
     Outputs: y in 16 bits (out_type=torch.bfloat16 / float16, or a buffer) and an 8-bit matrix (fp8=True, or buffers q and scale)."""
-    n, d = x.shape
+    shape = x.shape
+    n, d = shape
     dev = _device_of("x", x)
     in_type = kind = _type_of("x", x)
     if y is None and out_type is not None:
         y = _new_on(stream, torch.empty, (n, d), dtype=out_type, device=x.device)
     if fp8 and q is None and scale is None:
         q, scale = _q_empty(stream, n, d, x.device)
-    xs = _rows("x", x, n, d, dev)
+    xs, one = x.stride()
+    if one != 1 or xs < d:
+        xs = _rows("x", x, n, d, dev)
     wt = rt = -1
     w_at = rs = ros = r_at = ro_at = ys = y_at = qs = q_at = s_at = 0
     if y is not None:
         kind = _output_type("y", _type_of("y", y))
-        ys, y_at = _rows("y", y, n, d, dev), y.data_ptr()
+        ys, one = y.stride()
+        if y.shape != shape or one != 1 or ys < d or y.get_device() != dev:
+            ys = _rows("y", y, n, d, dev)
+        y_at = y.data_ptr()
     if weight is not None:
         wt = _type_of("weight", weight)
         if weight.shape != (d,) or not weight.is_contiguous() or weight.get_device() != dev:
@@ -663,16 +671,26 @@ def rms_norm(x, weight=None, eps: float = 1e-5, residual=None, residual_out=None
         w_at = weight.data_ptr()
     if residual is not None:
         rt = _type_of("residual", residual)
+        rs, one = residual.stride()
+        if residual.shape != shape or one != 1 or rs < d or residual.get_device() != dev:
+            rs = _rows("residual", residual, n, d, dev)
+        r_at = residual.data_ptr()
         if residual_out is None:
-            residual_out = residual
-        elif residual_out.dtype is not residual.dtype:
-            _bad("residual_out: residual's type expected")
-        rs, ros = _rows("residual", residual, n, d, dev), _rows("residual_out", residual_out, n, d, dev)
-        r_at, ro_at = residual.data_ptr(), residual_out.data_ptr()
+            residual_out, ros, ro_at = residual, rs, r_at
+        else:
+            if residual_out.dtype is not residual.dtype:
+                _bad("residual_out: residual's type expected")
+            ros, one = residual_out.stride()
+            if residual_out.shape != shape or one != 1 or ros < d or residual_out.get_device() != dev:
+                ros = _rows("residual_out", residual_out, n, d, dev)
+            ro_at = residual_out.data_ptr()
     elif residual_out is not None:
         _bad("residual_out without a residual")
     if q is not None and scale is not None:
-        qs, q_at, s_at = _q_rows("q", q, n, d, dev), q.data_ptr(), _scales("scale", scale, n, (d + 127) // 128, dev)
+        qs, one = q.stride()
+        if q.shape != shape or one != 1 or qs < d or qs % 16 or q.dtype is not torch.float8_e4m3fn or q.get_device() != dev:
+            qs = _q_rows("q", q, n, d, dev)
+        q_at, s_at = q.data_ptr(), _scales("scale", scale, n, (d + 127) // 128, dev)
     elif q is not None or scale is not None:
         _bad("q and scale go together")
     elif y is None and residual is None:
@@ -699,32 +717,45 @@ def gated_act(gate, up=None, act: str = "silu", out_type=None, fp8: bool = False
     code = _ACTS.get(act)
     if code is None:
         _bad(f"act: one of {sorted(_ACTS)} expected, got {act!r}")
-    n, d = gate.shape
+    shape = gate.shape
+    n, d = shape
     dev = _device_of("gate", gate)
     in_type = kind = _type_of("gate", gate)
     if y is None and out_type is not None:
         y = _new_on(stream, torch.empty, (n, d), dtype=out_type, device=gate.device)
     if fp8 and q is None and scale is None:
         q, scale = _q_empty(stream, n, d, gate.device)
+    gs, one = gate.stride()
+    if one != 1 or gs < d:
+        gs = _rows("gate", gate, n, d, dev)
     us = u_at = ys = y_at = qs = q_at = s_at = 0
     if up is not None:
         if up.dtype is not gate.dtype:
             _bad("gate and up: one type expected")
-        us, u_at = _rows("up", up, n, d, dev), up.data_ptr()
+        us, one = up.stride()
+        if up.shape != shape or one != 1 or us < d or up.get_device() != dev:
+            us = _rows("up", up, n, d, dev)
+        u_at = up.data_ptr()
     if y is not None:
         kind = _output_type("y", _type_of("y", y))
         if in_type != INPUT_FP32 and in_type != kind:
             _bad("gate, up, y: float32 or one 16-bit type expected")
-        ys, y_at = _rows("y", y, n, d, dev), y.data_ptr()
+        ys, one = y.stride()
+        if y.shape != shape or one != 1 or ys < d or y.get_device() != dev:
+            ys = _rows("y", y, n, d, dev)
+        y_at = y.data_ptr()
     if q is not None and scale is not None:
-        qs, q_at, s_at = _q_rows("q", q, n, d, dev), q.data_ptr(), _scales("scale", scale, n, (d + 127) // 128, dev)
+        qs, one = q.stride()
+        if q.shape != shape or one != 1 or qs < d or qs % 16 or q.dtype is not torch.float8_e4m3fn or q.get_device() != dev:
+            qs = _q_rows("q", q, n, d, dev)
+        q_at, s_at = q.data_ptr(), _scales("scale", scale, n, (d + 127) // 128, dev)
     elif q is not None or scale is not None:
         _bad("q and scale go together")
     elif y is None:
         _bad("nothing to write: neither y nor q")
     if kind == INPUT_FP32:
         kind = INPUT_BF16
-    _call_on("plora_gated_act", dev, _ACT_PACK.pack(in_type, kind, code, n, d, _rows("gate", gate, n, d, dev), us, ys, qs, gate.data_ptr(),
+    _call_on("plora_gated_act", dev, _ACT_PACK.pack(in_type, kind, code, n, d, gs, us, ys, qs, gate.data_ptr(),
                                                     u_at, y_at, q_at, s_at), stream)
     return Act8(y, q, scale)
 
@@ -763,21 +794,29 @@ def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, strea
         if len(outs) != count:
             _bad("out: a buffer for each weight expected")
     ns, strides, out_strides, at, s_at, o_at = [0] * 4, [0] * 4, [0] * 4, [0] * 4, [0] * 4, [0] * 4
-    kind = outs[0].dtype
+    kind, f8 = outs[0].dtype, torch.float8_e4m3fn
     for i, (t, s, o) in enumerate(zip(ws, scales, outs)):
-        n = t.shape[0]
+        n, tk = t.shape
         if o.dtype is not kind:
             _bad("out: one type expected")
-        ns[i], strides[i], out_strides[i] = n, _q_rows("w", t, n, k, dev), _rows("out", o, m, n, dev)
+        st, one = t.stride()
+        if tk != k or one != 1 or st < k or st % 16 or t.dtype is not f8 or t.get_device() != dev:
+            st = _q_rows("w", t, n, k, dev)
+        ost, one = o.stride()
+        if o.shape != (m, n) or one != 1 or ost < n or o.get_device() != dev:
+            ost = _rows("out", o, m, n, dev)
+        ns[i], strides[i], out_strides[i] = n, st, ost
         at[i], s_at[i], o_at[i] = t.data_ptr(), _scales("w_scale", s, (n + 127) // 128, blocks, dev), o.data_ptr()
+    xs, one = x.stride()
+    if one != 1 or xs < k or xs % 16 or x.dtype is not f8:
+        xs = _q_rows("x", x, m, k, dev)
     status_at = 0
     if status is not None:
         status_at = _ints("status", status, (1,))
         if status.get_device() != dev:
             _bad("status: on the inputs' device expected")
-    _call_on("plora_gemm_fp8", dev, _GEMM_PACK.pack(_type_of("out", outs[0]), m, k, count, *ns, _q_rows("x", x, m, k, dev), *strides, *out_strides,
-                                                    x.data_ptr(), _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, status_at),
-             stream)
+    _call_on("plora_gemm_fp8", dev, _GEMM_PACK.pack(_type_of("out", outs[0]), m, k, count, *ns, xs, *strides, *out_strides, x.data_ptr(),
+                                                    _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, status_at), stream)
     return list(outs) if many else outs[0]
 
 
