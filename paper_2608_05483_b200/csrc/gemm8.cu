@@ -37,7 +37,7 @@ constexpr int kRows = 128;                // rows of x per CTA
 constexpr int kRowBytes = 128;            // one block of K
 constexpr int kScaleRun = 8, kScaleSlots = 2;          // blocks of K whose scales are staged together; such runs
 constexpr int kScaleBytes = kScaleRun * (kRows + 4) * 4;    // of a run: sx [block][row], then sw [block][half of the columns][2]
-constexpr int kMaxStages = 16;
+constexpr int kMaxStages = 16, kPairBytes = 200 * 1024;
 constexpr int kRingOffset = (kScaleSlots * kScaleBytes + 512 + 1023) / 1024 * 1024;        // scales, barriers and words lie in front of the ring
 constexpr long long kWaitCycles = 4000000000ll;      // limit of a wait: about two seconds of SM clock
 
@@ -721,7 +721,10 @@ cudaError_t go(const Maps& maps, Params p, paged::Device dev, cudaStream_t st) {
     int ring = p.stages * stage + behind;
     const int rows = p.m < kRows ? p.m : kRows, part = p.splits > 1 ? rows * C::kPitch * 4 : 0;
     if (ring < part) ring = part;
-    const int smem = 1024 + kRingOffset + ring;
+    // (A pair takes tensor memory on two SMs: it has both to itself, so that it never holds one half while a kernel of another stream
+    // that holds the other waits for a CTA of its own.)
+    int smem = 1024 + kRingOffset + ring;
+    if (CG == 2 && smem < kPairBytes) smem = kPairBytes;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
