@@ -247,10 +247,10 @@ __device__ __forceinline__ void weigh(const NormParams& p, Part& h, float sum, i
 }
 
 // CTA: a row per CTA; otherwise p.lanes lanes per row, and several rows per warp where a row has fewer than 32.
-// (CTAs per SM: three where x has 16 bits; fp32 chunks and short rows are faster with more registers, 16384 x 4096 fp32 108 us with two,
-// 114 with three.)
-template <int KX, int KR, int KY, bool CTA, int MAXT, bool VEC>
-__global__ void __launch_bounds__(MAXT, MAXT > 256 ? 1 : CTA && KX != kFp32 ? 3 : 2) norm_kernel(const NormParams p) {
+// (CTAs of MAXT threads per SM: three where x has 16 bits; fp32 chunks and short rows are faster with more registers, 16384 x 4096 fp32
+// 108 us with two, 114 with three.  TIGHT: four.)
+template <int KX, int KR, int KY, bool CTA, int MAXT, bool VEC, bool TIGHT = false>
+__global__ void __launch_bounds__(MAXT, MAXT > 256 ? 1 : TIGHT ? 4 : CTA && KX != kFp32 ? 3 : 2) norm_kernel(const NormParams p) {
     typedef typename TypeOf<KX>::type TX;
     typedef typename TypeOf<KR>::type TR;
     __shared__ float part[32];
@@ -419,8 +419,17 @@ Rows rows_of(const void* p, int kind, long long& stride, long long d) {
     return {stride >= d && aligned(p, es), stride % 8 == 0 && aligned(p, 8 * es)};
 }
 
+// CTAs of `warps` warps that fit on an SM's four parts, each with registers for 512 / regs warps.
+long long ctas_by_registers(int regs, int warps) { return 4 * (512 / ((regs + 7) / 8 * 8)) / warps; }
+int registers_of(const void* kern) {
+    cudaFuncAttributes a;
+    if (cudaFuncGetAttributes(&a, kern) == cudaSuccess) return a.numRegs;
+    (void)cudaGetLastError();
+    return 64;
+}
+
 template <int KX, int KR, int KY, bool VEC>
-cudaError_t norm_go(NormParams p, cudaStream_t st) {
+cudaError_t norm_go(NormParams p, int sms, cudaStream_t st) {
     // Up to 1024 columns a row has 4 lanes per block, rounded up to a power of two; beyond, a CTA.  (Chosen by the columns alone:
     // rows sum alike in any batch.)
     void* args[] = {&p};
@@ -430,14 +439,23 @@ cudaError_t norm_go(NormParams p, cudaStream_t st) {
         return launch((const void*)norm_kernel<KX, KR, KY, false, 256, VEC>, dim3((unsigned)((threads + 255) / 256)), 256, st, args);
     }
     const unsigned threads = (unsigned)((p.blocks * 4 + 31) / 32 * 32);
-    return launch(threads > 256 ? (const void*)norm_kernel<KX, KR, KY, true, 1024, VEC> : (const void*)norm_kernel<KX, KR, KY, true, 256, VEC>,
-                  dim3(p.n), threads, st, args);
+    const void* kern = threads > 256 ? (const void*)norm_kernel<KX, KR, KY, true, 1024, VEC> : (const void*)norm_kernel<KX, KR, KY, true, 256, VEC>;
+    if constexpr (VEC && (KX == kFp32 || KR == kFp32)) {
+        // fp32 rows take more than 64 registers a thread.  With 64 more of them fit at one time, which pays if all then do: 777 x 4168,
+        // half with an fp32 residual, 9.2 us against 11.7; 1000 x 4096, fp32, 9.3 against 11.4.  With one round or several either way
+        // it does not (512 x 4168 7.5 against 5.8, 1200 x 4168 14.9 against 14.2).
+        static const int regs = registers_of((const void*)norm_kernel<KX, KR, KY, true, 256, VEC>);
+        const int warps = (int)threads / 32;
+        if (threads <= 256 && p.n > ctas_by_registers(regs, warps) * sms && p.n <= ctas_by_registers(64, warps) * sms)
+            kern = (const void*)norm_kernel<KX, KR, KY, true, 256, VEC, true>;
+    }
+    return launch(kern, dim3(p.n), threads, st, args);
 }
 template <int KX, int KY>
-cudaError_t norm_res(const NormParams& p, int res, bool vec, cudaStream_t st) {
-    if (!p.res) return vec ? norm_go<KX, kNone, KY, true>(p, st) : norm_go<KX, kNone, KY, false>(p, st);
-    if (res == kFp32) return vec ? norm_go<KX, kFp32, KY, true>(p, st) : norm_go<KX, kFp32, KY, false>(p, st);
-    return vec ? norm_go<KX, KY, KY, true>(p, st) : norm_go<KX, KY, KY, false>(p, st);
+cudaError_t norm_res(const NormParams& p, int res, bool vec, int sms, cudaStream_t st) {
+    if (!p.res) return vec ? norm_go<KX, kNone, KY, true>(p, sms, st) : norm_go<KX, kNone, KY, false>(p, sms, st);
+    if (res == kFp32) return vec ? norm_go<KX, kFp32, KY, true>(p, sms, st) : norm_go<KX, kFp32, KY, false>(p, sms, st);
+    return vec ? norm_go<KX, KY, KY, true>(p, sms, st) : norm_go<KX, KY, KY, false>(p, sms, st);
 }
 template <int KX, int KY, int ACT>
 cudaError_t act_go(const ActParams& p, bool vec, cudaStream_t st) {
@@ -493,12 +511,14 @@ extern "C" PLORA_API plora_status plora_rms_norm(const plora_rms_norm_args* a, v
         if (!p.q_stride) p.q_stride = up16(a->d);
         if (p.q_stride < a->d || p.q_stride % 16 || !aligned(a->q, 16) || !aligned(a->scale, 4)) return PLORA_ERR_INVALID_ARG;
     }
+    plora::paged::Device dev;
+    if (device(dev) != cudaSuccess) return PLORA_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (a->type == kBf16)
-        e = a->in_type == kFp32 ? norm_res<kFp32, kBf16>(p, a->residual_type, vec, st) : norm_res<kBf16, kBf16>(p, a->residual_type, vec, st);
+        e = a->in_type == kFp32 ? norm_res<kFp32, kBf16>(p, a->residual_type, vec, dev.sms, st) : norm_res<kBf16, kBf16>(p, a->residual_type, vec, dev.sms, st);
     else
-        e = a->in_type == kFp32 ? norm_res<kFp32, kFp16>(p, a->residual_type, vec, st) : norm_res<kFp16, kFp16>(p, a->residual_type, vec, st);
+        e = a->in_type == kFp32 ? norm_res<kFp32, kFp16>(p, a->residual_type, vec, dev.sms, st) : norm_res<kFp16, kFp16>(p, a->residual_type, vec, dev.sms, st);
     return e == cudaSuccess ? PLORA_OK : PLORA_ERR_CUDA;
 }
 

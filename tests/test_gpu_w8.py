@@ -129,6 +129,18 @@ def test_norm_rows_do_not_depend_on_the_batch():
         assert torch.equal(a.y[5:6], b.y) and torch.equal(a.q[5:6].float(), b.q.float()) and torch.equal(a.scale[5:6], b.scale)
 
 
+def test_norm_rows_do_not_depend_on_the_round_they_fit_in():
+    """Batches of some 600 to 1200 fp32 rows take a form with fewer registers: the same bits."""
+    g = _gen(2)
+    for n, d, res_type in ((777, 5120, BF), (1000, 4096, BF), (640, 4168, F32)):
+        x, w, res = _randn(g, n, d), _randn(g, d).to(BF), _randn(g, n, d).to(res_type)
+        a = P.rms_norm(x, w, residual=res, residual_out=torch.empty_like(res), out_type=BF, fp8=True)
+        for rows in (slice(0, 3), slice(n - 2, n)):
+            b = P.rms_norm(x[rows], w, residual=res[rows], residual_out=torch.empty_like(res[rows]), out_type=BF, fp8=True)
+            assert torch.equal(a.y[rows], b.y) and torch.equal(a.q[rows].float(), b.q.float()) and torch.equal(a.scale[rows], b.scale)
+            assert torch.equal(a.residual[rows], b.residual)
+
+
 def test_norm_of_zeros_infinities_and_nan():
     x = torch.randn((6, 384), device=DEV)
     x[0] = 0.0
