@@ -70,6 +70,7 @@ struct Params {
     int32_t n[kMaxWeights], tile_end[kMaxWeights];     // columns; tiles of columns up to and with this weight's
     int32_t m, blocks, m_tiles, n_tiles, tiles, splits, x_rows;   // blocks of K; x_rows: rows of a box of x
     int32_t stages, x_bytes;                           // of the ring; bytes of a stage's box of x, a multiple of 1024
+    int32_t quads;                                     // groups of 32 rows of a tile that have rows (4 if any tile is full)
     int32_t vec;                                       // bytes that every row of every output is aligned to: 32, 16, or fewer
     int32_t* status;
 };
@@ -601,11 +602,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
         }
         for (int a = 0; a < C::kAccs; ++a) {
             mbar_init(sm.acc_full + a * 8, 1);
-            mbar_init(sm.acc_empty + a * 8, kAddWarps * CG);
+            mbar_init(sm.acc_empty + a * 8, kAddWarps / 4 * p.quads * CG);
         }
         for (int r = 0; r < kScaleSlots; ++r) {
             mbar_init(sm.scale_full + r * 8, 2);
-            mbar_init(sm.scale_empty + r * 8, kAddWarps);
+            mbar_init(sm.scale_empty + r * 8, kAddWarps / 4 * p.quads);
         }
         mbar_init(sm.done, 1);
         mbar_init(sm.peer, 1);
@@ -637,8 +638,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
         Turn<C::kAccs> in;
         Turn<kScaleSlots> run;
         float2 acc[C::kCols / 2];
+        // (warps whose rows no tile has leave at once: one row by 12288 x 4096 11.5 -> 11.35 us)
 #pragma unroll 1
-        for (int i = sh.first; i < p.tiles; i += sh.step) {
+        for (int i = (warp & 3) < p.quads ? sh.first : p.tiles; i < p.tiles; i += sh.step) {
             const Tile u = tile_of(p, i);
             if (!add_tile<CG, BN>(sm, from, hand_back, sh.b1 - sh.b0, u.mt * CG * kRows + r - lane < p.m, left_in_block(u.nt * BN + c), in, run, acc)) break;
             const Tile t = tile_of(p, opaque(i));       // (made again rather than kept beside the sums)
@@ -889,6 +891,7 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
     }
     p.x_rows = a->m >= kRows ? kRows : (a->m + 7) / 8 * 8;
     p.x_bytes = p.x_rows * kRowBytes;
+    p.quads = a->m >= kRows ? 4 : (a->m + 31) / 32;
     Maps maps;
     if (!map_bytes(&maps.x, a->x, a->k, a->m, x_stride, p.x_rows)) return PLORA_ERR_INVALID_ARG;
     for (int i = 0; i < a->n_weights; ++i)
