@@ -84,10 +84,11 @@ class Block(Layer):
             self.ctx.register_pool(0, proj, ins[proj - 4], widths[proj - 4], [rank] * n_adapters, [0.5] * n_adapters, self.A[proj], self.B[proj])
         self.gain = [rnd(self.hidden, std=0.2) + 1.0 for _ in range(2)]
         self.W8 = [P.quant_weight(w.t().contiguous()) for w in self.W]           # once: [d_out, d_in], a scale per 128 x 128
+        torch.cuda.synchronize()                                                 # complete before any step begins: weights_ready
 
     def project(self, a, x, ids, projs):
         """y = x W + s (x A) B of projections that share their input: a its 8-bit form, x the 16-bit one.  fp32."""
-        ys = P.gemm_fp8(a.q, a.scale, [self.W8[p][0] for p in projs], [self.W8[p][1] for p in projs])
+        ys = P.gemm_fp8(a.q, a.scale, [self.W8[p][0] for p in projs], [self.W8[p][1] for p in projs], weights_ready=True)
         self.ctx.lora_delta_group([x] * len(projs), ids, [0] * len(projs), projs, ys)
         return ys
 

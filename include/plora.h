@@ -623,8 +623,10 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
  * Sums in fp32, rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
  * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; rows aligned to
  * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1 up to 2^30.
- * The weights are read before the kernel in front has completed if that kernel is one of this library's: they have to be complete
- * before it begins (weights made by plora_quant_weight, copies or any other library's kernels always are).
+ * weights_ready  1: the caller's word that every w_i was complete and visible to the whole device before the kernel in front of
+ *         this call on the stream began (weights laid out once, and the host or an event has waited for that since).  The first copies of
+ *         weights then start while that kernel drains.  0: they start behind it, whatever it is.  The results are the same to the bit;
+ *         wrong use is a data race on the weights, nothing else (x and all scales are read behind that kernel either way).
  * The kernel takes up to all 512 tensor-memory columns of an SM; as with plora_lora_delta's tensor-core path, do not run it
  * beside a kernel that holds tensor memory for its whole lifetime and itself waits for this call.
  * status  device int32 or NULL: a sticky word that gets PLORA_ERR_TIMEOUT if a bounded device-side wait ran out. */
@@ -638,6 +640,7 @@ typedef struct {
     const float *w_scale[4];
     void *out[4];
     int32_t *status;
+    int32_t weights_ready;
 } plora_gemm_fp8_args;
 PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args *args, void *stream);
 

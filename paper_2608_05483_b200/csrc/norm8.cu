@@ -363,8 +363,8 @@ struct WeightParams {
     long long w_stride, q_stride;
     int32_t n, k, blocks;
 };
-// A CTA of 1024 threads per 128 x 128 block: a thread has two chunks of 8 columns, 64 rows apart.  (A set-up call: it does not let
-// the next kernel start early, which is what allows the product to fetch weights before it has joined the stream's order.)
+// A CTA of 1024 threads per 128 x 128 block: a thread has two chunks of 8 columns, 64 rows apart.  (A set-up call: it lets
+// no kernel start early.)
 template <int KX, bool VEC>
 __global__ void __launch_bounds__(1024) weight_kernel(const WeightParams p) {
     typedef typename TypeOf<KX>::type TX;
