@@ -629,7 +629,12 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
  *         wrong use is a data race on the weights, nothing else (x and all scales are read behind that kernel either way).
  * The kernel takes up to all 512 tensor-memory columns of an SM; as with plora_lora_delta's tensor-core path, do not run it
  * beside a kernel that holds tensor memory for its whole lifetime and itself waits for this call.
- * status  device int32 or NULL: a sticky word that gets PLORA_ERR_TIMEOUT if a bounded device-side wait ran out. */
+ * status  device int32 or NULL: a sticky word that gets PLORA_ERR_TIMEOUT if a bounded device-side wait ran out.  The kernel then winds
+ *         down: copies and products under way are waited for (once more for at most the limit), tensor memory is freed, out may hold
+ *         anything.  Later calls are not affected.
+ * wait_cycles  limit of the waits in SM clock cycles; 0: 4e9, about two seconds.
+ * test_hook    for tests only: with PLORA_HOOK_WITHHOLD_RELEASE one warp of every CTA never hands an accumulator back, so that the
+ *         products' wait for one runs out (where a CTA has more than four blocks of K).  Needs 0 < wait_cycles <= PLORA_HOOK_MAX_CYCLES. */
 typedef struct {
     int32_t out_type, m, k, n_weights;
     int32_t n[4];
@@ -640,7 +645,8 @@ typedef struct {
     const float *w_scale[4];
     void *out[4];
     int32_t *status;
-    int32_t weights_ready;
+    int64_t wait_cycles;
+    int32_t weights_ready, test_hook;
 } plora_gemm_fp8_args;
 PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args *args, void *stream);
 

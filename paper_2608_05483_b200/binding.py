@@ -120,7 +120,8 @@ class GemmFp8Args(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("out_type", "m", "k", "n_weights")]
                 + [("n", ctypes.c_int32 * 4), ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64 * 4),
                    ("out_stride", ctypes.c_int64 * 4), ("x", ctypes.c_void_p), ("x_scale", ctypes.c_void_p), ("w", ctypes.c_void_p * 4),
-                   ("w_scale", ctypes.c_void_p * 4), ("out", ctypes.c_void_p * 4), ("status", ctypes.c_void_p), ("weights_ready", ctypes.c_int32)])
+                   ("w_scale", ctypes.c_void_p * 4), ("out", ctypes.c_void_p * 4), ("status", ctypes.c_void_p), ("wait_cycles", ctypes.c_int64),
+                   ("weights_ready", ctypes.c_int32), ("test_hook", ctypes.c_int32)])
 
 
 class PloraError(RuntimeError):
@@ -557,7 +558,7 @@ class Act8(NamedTuple):
 # (packed as RmsNormArgs, GatedActArgs and GemmFp8Args are laid out)
 _NORM_PACK = struct.Struct("@6i5q7P2f")
 _ACT_PACK = struct.Struct("@5i4x4q5P")
-_GEMM_PACK = struct.Struct("@8i9q15Pi4x")
+_GEMM_PACK = struct.Struct("@8i9q15Pq2i")
 
 
 _kinds = {}       # type codes by torch type, filled when the torch layer is first used
@@ -775,11 +776,13 @@ def quant_weight(w, stream=None):
     return q, scale
 
 
-def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, stream=None, weights_ready: bool = False):
+def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, stream=None, weights_ready: bool = False,
+             wait_cycles: int = 0):
     """x w^T for an 8-bit matrix x [m, k] with x_scale and an 8-bit weight w [n, k] with w_scale, or up to four of them (lists) that
     share x, in one launch (plora_gemm_fp8).  Returns [m, n] (a list of them for lists): fp32, or out_type, or the buffers `out`.
     weights_ready: the caller's word that the weights were complete before the kernel in front of this call on the stream began (laid out
-    once, and waited for since); their first copies then start while that kernel drains."""
+    once, and waited for since); their first copies then start while that kernel drains.
+    wait_cycles: limit of the kernel's waits in SM clock cycles, 0: about two seconds."""
     many = isinstance(w, (list, tuple))
     ws, scales = (w, w_scale) if many else ((w,), (w_scale,))
     count = len(ws)
@@ -818,8 +821,8 @@ def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, strea
         if status.get_device() != dev:
             _bad("status: on the inputs' device expected")
     _call_on("plora_gemm_fp8", dev, _GEMM_PACK.pack(_type_of("out", outs[0]), m, k, count, *ns, xs, *strides, *out_strides, x.data_ptr(),
-                                                    _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, status_at, 1 if weights_ready else 0),
-             stream)
+                                                    _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, status_at, wait_cycles,
+                                                      1 if weights_ready else 0, HOOK_NONE), stream)
     return list(outs) if many else outs[0]
 
 

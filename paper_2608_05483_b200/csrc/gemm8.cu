@@ -39,7 +39,7 @@ constexpr int kScaleRun = 8, kScaleSlots = 2;          // blocks of K whose scal
 constexpr int kScaleBytes = kScaleRun * (kRows + 4) * 4;    // of a run: sx [block][row], then sw [block][half of the columns][2]
 constexpr int kMaxStages = 16, kPairBytes = 200 * 1024;
 constexpr int kRingOffset = (kScaleSlots * kScaleBytes + 512 + 1023) / 1024 * 1024;        // scales, barriers and words lie in front of the ring
-constexpr long long kWaitCycles = 4000000000ll;      // limit of a wait: about two seconds of SM clock
+constexpr long long kWaitCycles = 4000000000ll;      // limit of a wait unless the caller sets one: about two seconds of SM clock
 
 // CG: CTAs that share a tile (cta_group); BN: columns of the tile, a multiple of 32.
 // Narrow tiles of single CTAs leave room for a second CTA on the SM, so that one starts or ends while the other streams (7.6 against
@@ -71,6 +71,8 @@ struct Params {
     int32_t m, blocks, m_tiles, n_tiles, tiles, splits, x_rows;   // blocks of K; x_rows: rows of a box of x
     int32_t stages, x_bytes;                           // of the ring; bytes of a stage's box of x, a multiple of 1024
     int32_t quads;                                     // groups of 32 rows of a tile that have rows (4 if any tile is full)
+    int32_t test_hook;                                 // PLORA_HOOK_*: tests make a wait run out with it
+    long long wait_cycles;                             // limit of a wait
     int32_t weights_ready;                             // the caller's word that w was complete before the kernel in front began
     int32_t vec;                                       // bytes that every row of every output is aligned to: 32, 16, or fewer
     int32_t* status;
@@ -216,13 +218,14 @@ __device__ __forceinline__ void st_global32(void* p, const uint32_t* w) {
 struct WaitCtl {
     volatile int* abort_flag;
     int32_t* status;
+    long long limit;
 };
 __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, WaitCtl w) {
     const long long t0 = clock64();
 #pragma unroll 1
     for (uint32_t n = 1;; ++n) {
         if (mbar_try_wait(bar, parity)) return true;
-        if ((n & 63) == 0 && (*w.abort_flag || clock64() - t0 > kWaitCycles)) break;
+        if ((n & 63) == 0 && (*w.abort_flag || clock64() - t0 > w.limit)) break;
     }
     if (!*w.abort_flag && w.status) atomicCAS(w.status, 0, PLORA_ERR_TIMEOUT);
     *w.abort_flag = 1;
@@ -344,9 +347,11 @@ __device__ __forceinline__ void load_warp(const Params& p, const Maps& maps, con
         if (CG == 2)
             for (uint32_t j = n > stages ? n - stages : 0; j < n; ++j) wait(sm.empty + j % stages * 8, (j / stages) & 1, sm.wc);
     } else if (CG == 1 || rank == 0) {
-        // copies in flight must land before the CTA leaves (in a pair they are counted by the first CTA's barriers)
+        // copies in flight must land before the CTA leaves (in a pair they are counted by the first CTA's barriers): one limit for all
+        // of them, for a stage that the pair's other CTA never asked for does not fill
+        const long long t0 = clock64();
         for (uint32_t j = n > stages ? n - stages : 0; j < n; ++j)
-            paged::mbar_drain(sm.full + j % stages * 8, (j / stages) & 1, kWaitCycles);
+            paged::mbar_drain(sm.full + j % stages * 8, (j / stages) & 1, sm.wc.limit - (clock64() - t0));
     }
 }
 
@@ -400,7 +405,7 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
     }
     // no product is under way when tensor memory is given back
     if (elect_one()) umma_commit<CG, false>(sm.done);
-    if (!paged::mbar_drain(sm.done, 0, kWaitCycles) && p.status) atomicCAS(p.status, 0, PLORA_ERR_TIMEOUT);
+    if (!paged::mbar_drain(sm.done, 0, sm.wc.limit) && sm.wc.status) atomicCAS(sm.wc.status, 0, PLORA_ERR_TIMEOUT);
 }
 
 template <int KIND>
@@ -471,7 +476,7 @@ __device__ __forceinline__ void scale_warps(const Params& p, const Smem& sm, uin
 // first `first` lie in the half's first block.  These warps bound the kernel (a block took them 1010 cycles in tiles of 256 columns, 520
 // of them to read and add), so a block's scales are fetched while the one before it is read, and places and addresses are kept.
 template <int CG, int BN>
-__device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t from, uint32_t hand_back, int blocks, bool any, int first, Turn<Cfg<CG, BN>::kAccs>& in,
+__device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t from, uint32_t hand_back, bool hands_back, int blocks, bool any, int first, Turn<Cfg<CG, BN>::kAccs>& in,
                                          Turn<kScaleSlots>& run, float2 (&acc)[Cfg<CG, BN>::kCols / 2]) {
     using C = Cfg<CG, BN>;
     const unsigned all = 0xffffffffu;
@@ -527,7 +532,7 @@ __device__ __forceinline__ bool add_tile(const Smem& sm, uint32_t from, uint32_t
                     }
             }
             tc_fence_before();
-            arrive_if<CG == 2>(hand_back + a * 8, lane == 0);        // (the warp's reads are complete: it reads as one)
+            arrive_if<CG == 2>(hand_back + a * 8, hands_back);        // (the warp's reads are complete: it reads as one)
         }
         __syncwarp();
         arrive_if<false>(sm.scale_empty + run.at * 8, lane == 0);
@@ -596,6 +601,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
     sm.tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars * 8);
     sm.wc.abort_flag = reinterpret_cast<volatile int*>(bars + kBars * 8 + 8);
     sm.wc.status = p.status;
+    sm.wc.limit = p.wait_cycles;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
@@ -638,6 +644,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
         if (threadIdx.x == 0) paged::grid_launch_dependents();
         const int r = (CG == 2 ? (int)rank * kRows : 0) + (warp & 3) * 32 + lane, c = (warp >> 2) * C::kCols;
         const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + c, hand_back = CG == 2 ? in_cta(sm.acc_empty, 0) : sm.acc_empty;
+        const bool hands_back = lane == 0 && !(p.test_hook == PLORA_HOOK_WITHHOLD_RELEASE && warp == 0);
         Turn<C::kAccs> in;
         Turn<kScaleSlots> run;
         float2 acc[C::kCols / 2];
@@ -645,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
 #pragma unroll 1
         for (int i = (warp & 3) < p.quads ? sh.first : p.tiles; i < p.tiles; i += sh.step) {
             const Tile u = tile_of(p, i);
-            if (!add_tile<CG, BN>(sm, from, hand_back, sh.b1 - sh.b0, u.mt * CG * kRows + r - lane < p.m, left_in_block(u.nt * BN + c), in, run, acc)) break;
+            if (!add_tile<CG, BN>(sm, from, hand_back, hands_back, sh.b1 - sh.b0, u.mt * CG * kRows + r - lane < p.m, left_in_block(u.nt * BN + c), in, run, acc)) break;
             const Tile t = tile_of(p, opaque(i));       // (made again rather than kept beside the sums)
             const int row = t.mt * CG * kRows + r, col = t.nt * BN + c;
             if (CG == 2 || p.splits == 1) {
@@ -843,6 +850,8 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
     for (int i = 0; i < a->n_weights; ++i)
         if (a->n[i] < 1) return PLORA_ERR_INVALID_ARG;
     if (a->weights_ready != 0 && a->weights_ready != 1) return PLORA_ERR_INVALID_ARG;
+    if (a->wait_cycles < 0 || (a->test_hook != PLORA_HOOK_NONE && a->test_hook != PLORA_HOOK_WITHHOLD_RELEASE)) return PLORA_ERR_INVALID_ARG;
+    if (a->test_hook != PLORA_HOOK_NONE && (a->wait_cycles < 1 || a->wait_cycles > PLORA_HOOK_MAX_CYCLES)) return PLORA_ERR_INVALID_ARG;
     if (a->m == 0) return PLORA_OK;
     const long long packed = ((long long)a->k + 15) & ~15ll, es = a->out_type == PLORA_INPUT_FP32 ? 4 : 2;
     auto matrix = [&](const void* p, long long& stride) {
@@ -877,6 +886,8 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
     p.blocks = (int)(((long long)a->k + kBlock - 1) / kBlock);
     p.status = a->status;
     p.weights_ready = a->weights_ready;
+    p.wait_cycles = a->wait_cycles ? a->wait_cycles : kWaitCycles;
+    p.test_hook = a->test_hook;
     const Form form = choose(a, p.blocks, dev.sms);
     const int cg = form.cg, bn = form.bn;
     p.splits = form.splits;

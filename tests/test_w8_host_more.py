@@ -9,3 +9,14 @@ from test_w8_host import _gemm
 def test_product_takes_weights_ready_as_a_truth_value(value):
     assert _gemm(weights_ready=value) == _gemm(weights_ready=value, m=0) == P.ERR_INVALID_ARG
     assert _gemm(weights_ready=1, m=0) == _gemm(weights_ready=0, m=0) == P.OK
+
+
+@pytest.mark.parametrize("kw", [dict(wait_cycles=-1), dict(test_hook=2), dict(test_hook=-1), dict(test_hook=P.HOOK_WITHHOLD_RELEASE),
+                                dict(test_hook=P.HOOK_WITHHOLD_RELEASE, wait_cycles=P.HOOK_MAX_CYCLES + 1)])
+def test_product_refuses_limits_and_hooks(kw):
+    assert _gemm(**kw) == _gemm(m=0, **kw) == P.ERR_INVALID_ARG
+
+
+def test_product_takes_limits_and_a_hook_with_a_short_one():
+    assert _gemm(m=0, wait_cycles=1) == _gemm(m=0, wait_cycles=1 << 40) == P.OK
+    assert _gemm(m=0, wait_cycles=P.HOOK_MAX_CYCLES, test_hook=P.HOOK_WITHHOLD_RELEASE) == P.OK
