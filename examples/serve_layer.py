@@ -208,6 +208,8 @@ def main(steps=4, block=False):
         want = reference_block(layer, x, a) if block else reference(layer, x, a)
         worst = max(worst, float((outs[r].double() - want).abs().max() / want.abs().max()))
     print(f"serve_{'block' if block else 'layer'}: {len(prompts)} requests, {steps} single-token steps, worst error {worst:.2e} of the largest output")
+    if block and P.gemm_fp8_status() != P.OK:
+        raise RuntimeError("a product's wait ran out")
     layer.ctx.close()
     return worst
 

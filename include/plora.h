@@ -629,7 +629,8 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
  *         wrong use is a data race on the weights, nothing else (x and all scales are read behind that kernel either way).
  * The kernel takes up to all 512 tensor-memory columns of an SM; as with plora_lora_delta's tensor-core path, do not run it
  * beside a kernel that holds tensor memory for its whole lifetime and itself waits for this call.
- * status  device int32 or NULL: a sticky word that gets PLORA_ERR_TIMEOUT if a bounded device-side wait ran out.  The kernel then winds
+ * status  device int32: a sticky word that gets PLORA_ERR_TIMEOUT if a bounded device-side wait ran out.  NULL: a word that the library
+ *         keeps on each device, which plora_gemm_fp8_status reads (waiting for `stream`) and clears.  The kernel then winds
  *         down: copies and products under way are waited for (once more for at most the limit), tensor memory is freed, out may hold
  *         anything.  Later calls are not affected.
  * wait_cycles  limit of the waits in SM clock cycles; 0: 4e9, about two seconds.
@@ -649,6 +650,7 @@ typedef struct {
     int32_t weights_ready, test_hook;
 } plora_gemm_fp8_args;
 PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args *args, void *stream);
+PLORA_API plora_status plora_gemm_fp8_status(void *stream, int32_t *host_out);
 
 #ifdef __cplusplus
 }

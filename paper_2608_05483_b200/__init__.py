@@ -14,6 +14,6 @@ from .binding import (  # noqa: F401
     INPUT_BF16, INPUT_FP16, INPUT_FP32, ROPE_BANDS, ROPE_HALF, ROPE_INTERLEAVED, ROPE_LINEAR, ROPE_NONE, ROPE_NTK, ROPE_RAMP,
     KvPlan, PagedAttn, RopeCacheArgs, RopeDesc, attn_paged, attn_paged_workspace, kv_plan, plora_attn_paged,
     plora_attn_paged_workspace_bytes, plora_kv_plan, plora_rope_cache, plora_rope_table, rope_cache, rope_table,
-    ACT_GELU, ACT_NONE, ACT_SILU, Act8, GatedActArgs, GemmFp8Args, RmsNormArgs, gated_act, gemm_fp8, plora_gated_act, plora_gemm_fp8,
-    plora_quant_weight, plora_rms_norm, quant_weight, rms_norm,
+    ACT_GELU, ACT_NONE, ACT_SILU, Act8, GatedActArgs, GemmFp8Args, RmsNormArgs, gated_act, gemm_fp8, gemm_fp8_status, plora_gated_act,
+    plora_gemm_fp8, plora_gemm_fp8_status, plora_quant_weight, plora_rms_norm, quant_weight, rms_norm,
 )

@@ -51,6 +51,7 @@ EXPORTS = (
     "plora_set_wait_limit", "plora_set_test_hook", "plora_set_inputs_resident", "plora_stream_read",
     "plora_kv_plan", "plora_rope_table", "plora_rope_cache", "plora_attn_paged_workspace_bytes", "plora_attn_paged",
     "plora_rms_norm", "plora_gated_act", "plora_quant_weight", "plora_gemm_fp8",
+    "plora_gemm_fp8_status",
 )
 
 INPUT_BF16, INPUT_FP16, INPUT_FP32 = 0, 1, 2
@@ -199,6 +200,7 @@ def load(build_if_missing: bool = True):
         "plora_gated_act": (i32, [vp, vp]),
         "plora_quant_weight": (i32, [vp, i32, i32, i32, i64, vp, i64, vp, vp]),
         "plora_gemm_fp8": (i32, [vp, vp]),
+        "plora_gemm_fp8_status": (i32, [vp, ctypes.POINTER(i32)]),
     }
     for name in EXPORTS:
         fn = getattr(lib, name)  # AttributeError here = the library does not export what the header declares
@@ -546,6 +548,12 @@ def plora_gemm_fp8(args: GemmFp8Args, stream=0):
     return load().plora_gemm_fp8(ctypes.byref(args), stream)
 
 
+def plora_gemm_fp8_status(stream=0):
+    v = ctypes.c_int32(0)
+    rc = load().plora_gemm_fp8_status(stream, ctypes.byref(v))
+    return rc, int(v.value)
+
+
 class Act8(NamedTuple):
     """What rms_norm and gated_act write: y [n, d] in 16 bits, q [n, d] e4m3 with scale [n, ceil(d / 128)], the residual sum (each
     None where it was not asked for)."""
@@ -782,7 +790,8 @@ def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, strea
     share x, in one launch (plora_gemm_fp8).  Returns [m, n] (a list of them for lists): fp32, or out_type, or the buffers `out`.
     weights_ready: the caller's word that the weights were complete before the kernel in front of this call on the stream began (laid out
     once, and waited for since); their first copies then start while that kernel drains.
-    wait_cycles: limit of the kernel's waits in SM clock cycles, 0: about two seconds."""
+    wait_cycles: limit of the kernel's waits in SM clock cycles, 0: about two seconds.  A wait that ran out leaves ERR_TIMEOUT in status
+    (int32 [1]), or without one in the word that gemm_fp8_status reads."""
     many = isinstance(w, (list, tuple))
     ws, scales = (w, w_scale) if many else ((w,), (w_scale,))
     count = len(ws)
@@ -824,6 +833,15 @@ def gemm_fp8(x, x_scale, w, w_scale, out_type=None, out=None, status=None, strea
                                                     _scales("x_scale", x_scale, m, blocks, dev), *at, *s_at, *o_at, status_at, wait_cycles,
                                                       1 if weights_ready else 0, HOOK_NONE), stream)
     return list(outs) if many else outs[0]
+
+
+def gemm_fp8_status(device=None, stream=None) -> int:
+    """The sticky status of the gemm_fp8 calls that were given no status word, on `device` (None: the current one); waits for the stream
+    and clears the word (plora_gemm_fp8_status)."""
+    with torch.cuda.device(device):
+        rc, status = plora_gemm_fp8_status(torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream)
+    _check(rc, "plora_gemm_fp8_status")
+    return status
 
 
 def plora_pool_slab_bytes(desc: PoolDesc) -> int:

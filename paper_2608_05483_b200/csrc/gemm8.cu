@@ -62,6 +62,9 @@ struct Cfg {
     static_assert(BN % 32 == 0 && kBBytes % 1024 == 0, "");
 };
 
+// The sticky status word of calls that bring none.
+__device__ int32_t default_status;
+
 struct Params {
     const float* x_scale;
     const float* w_scale[kMaxWeights];
@@ -75,7 +78,7 @@ struct Params {
     long long wait_cycles;                             // limit of a wait
     int32_t weights_ready;                             // the caller's word that w was complete before the kernel in front began
     int32_t vec;                                       // bytes that every row of every output is aligned to: 32, 16, or fewer
-    int32_t* status;
+    int32_t* status;                                   // nullptr: default_status
 };
 struct Maps {
     CUtensorMap x, w[kMaxWeights];
@@ -227,7 +230,7 @@ __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, WaitCtl
         if (mbar_try_wait(bar, parity)) return true;
         if ((n & 63) == 0 && (*w.abort_flag || clock64() - t0 > w.limit)) break;
     }
-    if (!*w.abort_flag && w.status) atomicCAS(w.status, 0, PLORA_ERR_TIMEOUT);
+    if (!*w.abort_flag) atomicCAS(w.status, 0, PLORA_ERR_TIMEOUT);
     *w.abort_flag = 1;
     return false;
 }
@@ -405,7 +408,7 @@ __device__ __forceinline__ void mma_warp(const Params& p, const Smem& sm, uint32
     }
     // no product is under way when tensor memory is given back
     if (elect_one()) umma_commit<CG, false>(sm.done);
-    if (!paged::mbar_drain(sm.done, 0, sm.wc.limit) && sm.wc.status) atomicCAS(sm.wc.status, 0, PLORA_ERR_TIMEOUT);
+    if (!paged::mbar_drain(sm.done, 0, sm.wc.limit)) atomicCAS(sm.wc.status, 0, PLORA_ERR_TIMEOUT);
 }
 
 template <int KIND>
@@ -600,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
     static_assert(kScaleSlots * kScaleBytes + kBars * 8 + 16 <= kRingOffset, "");
     sm.tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars * 8);
     sm.wc.abort_flag = reinterpret_cast<volatile int*>(bars + kBars * 8 + 8);
-    sm.wc.status = p.status;
+    sm.wc.status = p.status ? p.status : &default_status;
     sm.wc.limit = p.wait_cycles;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -920,4 +923,15 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
         return PLORA_ERR_CUDA;
     }
     return PLORA_OK;
+}
+
+extern "C" PLORA_API plora_status plora_gemm_fp8_status(void* stream, int32_t* host_out) {
+    if (!host_out) return PLORA_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    void* word = nullptr;
+    const bool done = cudaGetSymbolAddress(&word, default_status) == cudaSuccess &&
+                      cudaMemcpyAsync(host_out, word, 4, cudaMemcpyDeviceToHost, st) == cudaSuccess &&
+                      cudaMemsetAsync(word, 0, 4, st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
+    if (!done) (void)cudaGetLastError();      // reported here; a later call must not find it
+    return done ? PLORA_OK : PLORA_ERR_CUDA;
 }

@@ -80,3 +80,24 @@ def test_a_short_limit_alone_changes_nothing(m, k, ns):
     want = P.gemm_fp8(*args)
     torch.cuda.synchronize()
     assert int(status) == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_call_without_a_status_word_leaves_it_to_the_device():
+    g = _gen(6)
+    x, xs = _matrix8(g, 300, 8192, 1)
+    w, s = _matrix8(g, 1024, 8192, 128)
+    P.gemm_fp8_status()
+    assert P.gemm_fp8_status() == P.OK
+    out, intact = _guarded(300, 1024, torch.float32, 3)
+    _withheld(x, xs, w, s, out, None)
+    good = P.gemm_fp8(x, xs, w, s)                    # the word is sticky
+    assert P.gemm_fp8_status() == P.ERR_TIMEOUT
+    assert P.gemm_fp8_status(torch.device(DEV)) == P.OK
+    intact()
+    _check_product(good, x, xs, w, s)
+    # a call with a word of its own reports there and nowhere else
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    _withheld(x, xs, w, s, out, status)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    assert P.gemm_fp8_status(stream=side) == P.OK and int(status) == P.ERR_TIMEOUT

@@ -20,3 +20,7 @@ def test_product_refuses_limits_and_hooks(kw):
 def test_product_takes_limits_and_a_hook_with_a_short_one():
     assert _gemm(m=0, wait_cycles=1) == _gemm(m=0, wait_cycles=1 << 40) == P.OK
     assert _gemm(m=0, wait_cycles=P.HOOK_MAX_CYCLES, test_hook=P.HOOK_WITHHOLD_RELEASE) == P.OK
+
+
+def test_status_needs_a_place_to_go():
+    assert P.load().plora_gemm_fp8_status(0, None) == P.ERR_INVALID_ARG
