@@ -440,10 +440,11 @@ cudaError_t norm_go(NormParams p, int sms, cudaStream_t st) {
     }
     const unsigned threads = (unsigned)((p.blocks * 4 + 31) / 32 * 32);
     const void* kern = threads > 256 ? (const void*)norm_kernel<KX, KR, KY, true, 1024, VEC> : (const void*)norm_kernel<KX, KR, KY, true, 256, VEC>;
-    if constexpr (VEC && (KX == kFp32 || KR == kFp32)) {
+    if constexpr (VEC && (KX == kFp32) != (KR == kFp32)) {
         // fp32 rows take more than 64 registers a thread.  With 64 more of them fit at one time, which pays if all then do: 777 x 4168,
         // half with an fp32 residual, 9.2 us against 11.7; 1000 x 4096, fp32, 9.3 against 11.4.  With one round or several either way
-        // it does not (512 x 4168 7.5 against 5.8, 1200 x 4168 14.9 against 14.2).
+        // it does not (512 x 4168 7.5 against 5.8, 1200 x 4168 14.9 against 14.2), nor where x and the residual are both fp32, which spills
+        // 128 bytes a thread (777 x 4168 12.4 against 11.4, 1000 x 4096 14.0 against 12.3).
         static const int regs = registers_of((const void*)norm_kernel<KX, KR, KY, true, 256, VEC>);
         const int warps = (int)threads / 32;
         if (threads <= 256 && p.n > ctas_by_registers(regs, warps) * sms && p.n <= ctas_by_registers(64, warps) * sms)

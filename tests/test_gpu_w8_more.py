@@ -1,0 +1,25 @@
+"""More of the 8-bit calls on the GPU, against 64-bit references; tolerances as in test_gpu_w8.py unless said otherwise."""
+import pytest
+import torch
+
+import paper_2608_05483_b200 as P
+from test_gpu_w8 import _check8, _check16, _gen, _norm_ref, _randn
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, HALF, F32, F8 = torch.bfloat16, torch.float16, torch.float32, torch.float8_e4m3fn
+
+
+@pytest.mark.parametrize("n,d", [(640, 4168), (777, 5120), (1000, 4096), (600, 8192), (1300, 4096)])
+def test_norm_of_fp32_rows_and_an_fp32_residual(n, d):
+    """Batches about the number of rows that fit at one time: right, and a row's bits do not depend on the batch."""
+    g = _gen(n + d)
+    x, res, w = _randn(g, n, d), _randn(g, n, d) * 3.0, (_randn(g, d) * 0.3 + 1.0).to(BF)
+    a = P.rms_norm(x, w, residual=res, residual_out=torch.empty_like(res), out_type=BF, fp8=True)
+    h, v = _norm_ref(x, w, 1e-5, res, 0.0)
+    _check16(a.y, v)
+    _check8(a.q, a.scale, v)
+    assert torch.equal(a.residual, h.float())
+    for rows in (slice(0, 3), slice(n - 2, n)):
+        b = P.rms_norm(x[rows], w, residual=res[rows], residual_out=torch.empty_like(res[rows]), out_type=BF, fp8=True)
+        assert torch.equal(a.y[rows], b.y) and torch.equal(a.q[rows].float(), b.q.float()) and torch.equal(a.scale[rows], b.scale)
