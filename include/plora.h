@@ -613,7 +613,8 @@ typedef struct {
 } plora_gated_act_args;
 PLORA_API plora_status plora_gated_act(const plora_gated_act_args *args, void *stream);
 
-/* A weight [n][k] of type bf16, fp16 or fp32 (rows w_stride elements apart, 0: packed) as an 8-bit matrix: a set-up call. */
+/* A weight [n][k] of type bf16, fp16 or fp32 (rows w_stride elements apart, 0: packed) as an 8-bit matrix: a set-up call.
+ * n up to 65535 * 128; more is PLORA_ERR_UNSUPPORTED. */
 PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32_t n, int32_t k, int64_t w_stride, void *q_dev,
                                           int64_t q_stride, float *scale_dev, void *stream);
 
@@ -622,7 +623,8 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
  *     out[r][c] = sum_b x_scale[r][b] w_scale[c / 128][b] sum_{k in block b} x[r][k] w[c][k]
  * Sums in fp32, rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
  * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; rows aligned to
- * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1 up to 2^30.
+ * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1 up to 2^30, as long as
+ * ceil(m / 128) times the sum of ceil(n_i / 64) stays below 2^28; beyond either, PLORA_ERR_UNSUPPORTED.
  * weights_ready  1: the caller's word that every w_i was complete and visible to the whole device before the kernel in front of
  *         this call on the stream began (weights laid out once, and the host or an event has waited for that since).  The first copies of
  *         weights then start while that kernel drains.  0: they start behind it, whatever it is.  The results are the same to the bit;

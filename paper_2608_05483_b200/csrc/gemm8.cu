@@ -32,6 +32,7 @@ using paged::pack16;
 using paged::smem_u32;
 
 constexpr int kMaxWeights = 4;
+constexpr long long kMaxTiles = 1 << 28;  // of 128 rows and 64 columns (no form has more): tile numbers times kGroup are counted in 32 bits
 constexpr int kThreads = 384, kAddWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kScaleWarp = 10;      // (two of the last)
 constexpr int kRows = 128;                // rows of x per CTA
 constexpr int kRowBytes = 128;            // one block of K
@@ -254,6 +255,7 @@ struct Turn {
 // Tiles are numbered so that those under way at one time (some 74) form a near-square of x and w: runs of kGroup tiles of rows by all
 // tiles of columns.
 constexpr int kGroup = 8;
+static_assert(kMaxTiles * kGroup <= (1ll << 31), "");
 struct Tile {
     int32_t mt, w, nt;      // tile of rows; weight, and tile of its columns
 };
@@ -876,11 +878,17 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
         p.out[i] = a->out[i];
         p.n[i] = a->n[i];
     }
-    // (rows, columns and their products with tile numbers are counted in 32 bits)
+    // (rows and columns are counted in 32 bits, too)
     constexpr int kMost = 1 << 30;
     if (a->m > kMost || a->k > kMost) return PLORA_ERR_UNSUPPORTED;
+    auto tiles_of = [&](int bn) {
+        long long t = 0;
+        for (int i = 0; i < a->n_weights; ++i) t += ((long long)a->n[i] + bn - 1) / bn;
+        return t;
+    };
     for (int i = 0; i < a->n_weights; ++i)
         if (a->n[i] > kMost) return PLORA_ERR_UNSUPPORTED;
+    if (((long long)a->m + kRows - 1) / kRows * tiles_of(64) >= kMaxTiles) return PLORA_ERR_UNSUPPORTED;
     plora::paged::Device dev;
     if (device(dev) != cudaSuccess) return PLORA_ERR_CUDA;
     if (!plora::paged::encode_tiled()) return PLORA_ERR_UNSUPPORTED;
@@ -894,13 +902,7 @@ extern "C" PLORA_API plora_status plora_gemm_fp8(const plora_gemm_fp8_args* a, v
     const Form form = choose(a, p.blocks, dev.sms);
     const int cg = form.cg, bn = form.bn;
     p.splits = form.splits;
-    auto tiles_of = [&](int bn) {
-        long long t = 0;
-        for (int i = 0; i < a->n_weights; ++i) t += ((long long)a->n[i] + bn - 1) / bn;
-        return t;
-    };
     const long long m_tiles = ((long long)a->m + cg * kRows - 1) / (cg * kRows), n_tiles = tiles_of(bn);
-    if (m_tiles * n_tiles * 8 > INT32_MAX) return PLORA_ERR_UNSUPPORTED;
     p.m_tiles = (int)m_tiles;
     p.n_tiles = (int)n_tiles;
     p.tiles = (int)(m_tiles * n_tiles);

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2608_05483_b200 as P
-from test_gpu_w8 import _check8, _check16, _gen, _norm_ref, _randn
+from test_gpu_w8 import _check8, _check16, _check_product, _gen, _matrix8, _norm_ref, _randn
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -23,3 +23,22 @@ def test_norm_of_fp32_rows_and_an_fp32_residual(n, d):
     for rows in (slice(0, 3), slice(n - 2, n)):
         b = P.rms_norm(x[rows], w, residual=res[rows], residual_out=torch.empty_like(res[rows]), out_type=BF, fp8=True)
         assert torch.equal(a.y[rows], b.y) and torch.equal(a.q[rows].float(), b.q.float()) and torch.equal(a.scale[rows], b.scale)
+
+
+@pytest.mark.parametrize("m", [70, 300])
+def test_product_of_operands_beyond_32_bits(m):
+    """x and w whose rows lie so far apart that the last ones begin more than 2^32 bytes in."""
+    g = _gen(m)
+    k, n = 400, 200
+    x, xs = _matrix8(g, m, k, 1)
+    w, ws = _matrix8(g, n, k, 128)
+    far = {}
+    for name, t in (("x", x), ("w", w)):
+        stride = (1 << 32) // (t.shape[0] - 1) // 16 * 16 + 64
+        store = torch.empty((t.shape[0] - 1) * stride + k, dtype=torch.uint8, device=DEV)
+        assert (t.shape[0] - 1) * stride > 1 << 32
+        far[name] = store.view(F8).as_strided(t.shape, (stride, 1))
+        far[name].copy_(t)
+    out = P.gemm_fp8(far["x"], xs, far["w"], ws)
+    _check_product(out, x, xs, w, ws)
+    assert torch.equal(out, P.gemm_fp8(x, xs, w, ws))

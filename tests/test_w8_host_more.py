@@ -22,5 +22,13 @@ def test_product_takes_limits_and_a_hook_with_a_short_one():
     assert _gemm(m=0, wait_cycles=P.HOOK_MAX_CYCLES, test_hook=P.HOOK_WITHHOLD_RELEASE) == P.OK
 
 
+def test_product_refuses_more_tiles_than_it_can_number():
+    rows, cols = 128 << 14, 64 << 14                     # 2^28 tiles
+    kw = dict(m=rows, n=(0, cols), out_stride=(0, cols))
+    assert _gemm(n_weights=1, **kw) == P.ERR_UNSUPPORTED
+    assert _gemm(**kw) == P.ERR_UNSUPPORTED
+    assert _gemm(n_weights=1, m=1 << 30, n=(0, 1 << 30), out_stride=(0, 1 << 30)) == P.ERR_UNSUPPORTED
+
+
 def test_status_needs_a_place_to_go():
     assert P.load().plora_gemm_fp8_status(0, None) == P.ERR_INVALID_ARG
