@@ -621,7 +621,8 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
 /* out_i [m][n_i] = x w_i^T for the 8-bit activations x [m][k] and 1 to 4 8-bit weights w_i [n_i][k] that share them (q, k and v;
  * gate and up), in one launch:
  *     out[r][c] = sum_b x_scale[r][b] w_scale[c / 128][b] sum_{k in block b} x[r][k] w[c][k]
- * Sums in fp32, rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
+ * Sums in fp32 (within a block the tensor cores cut what lies more than some 24 bits below the largest of 32 products and the sum so
+ * far: a block's sum is off by at most 132 * 2^-24 of the largest of its products and partial sums), rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
  * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; rows aligned to
  * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1 up to 2^30, as long as
  * ceil(m / 128) times the sum of ceil(n_i / 64) stays below 2^28; beyond either, PLORA_ERR_UNSUPPORTED.

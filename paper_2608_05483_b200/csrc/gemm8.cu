@@ -3,7 +3,9 @@
 // The inner sums run on the fifth-generation tensor cores (tcgen05.mma, kind f8f6f4, e4m3 operands, fp32 accumulators in tensor
 // memory): a block of K is four instructions of 32.  The scales differ from block to block, so an accumulator holds
 // one block only; eight warps read it, multiply it by the two scales and add it to fp32 registers while the tensor cores fill the
-// next accumulator.  (The tensor cores' sum over a block of 128 is exact to fp32 rounding here: measured error 0 against 64 bits.)
+// next accumulator.  (The tensor cores align a sum's 32 products and the accumulator to the largest of them and cut what lies more
+// than some 24 bits below it.  Measured over single blocks of 128, against 64 bits: of normally distributed values 97 % are exact, the worst
+// off by 2^-24.5 of the sum of the magnitudes; of values of all exponents the worst by 2^-21.6 of that sum, 2^-19.6 of the largest product.)
 //
 // Roles: warps 0-7 scale and add, a row per thread and half of the tile's columns per warpgroup; warp 8 loads (a box of x and one
 // of w per block of K, 128-byte rows, swizzled); warp 9 issues the products; warps 10 and 11 stage the scales, some blocks ahead
