@@ -574,8 +574,8 @@ PLORA_API plora_status plora_attn_paged(const plora_paged_attn *args, void *stre
  *   weights      q [n][k], scale [ceil(n / 128)][ceil(k / 128)]: one per 128 x 128; n is d_out, k is d_in
  * q is 16-byte aligned, its stride a multiple of 16 (0: cols rounded up to 16); bytes between the columns' end and the stride
  * are neither read as values nor written.  Scales are packed.  The calls below that make 8-bit matrices take
- * s = max(max|v| / 448, 2^-126) over the block and round v / s to nearest even (v / s is good to a few 2^-23; a NaN or an infinity
- * in a block makes its scale one).
+ * s = max(max|v| / 448, 2^-126) over the block and round v / s to nearest even (v / s is good to a few 2^-23; a block with a NaN
+ * or an infinity has a NaN or an infinity as its scale).
  *
  * plora_rms_norm:  h = x + residual;  v = h * rsqrt(mean(h^2) + eps) * (weight + offset)  per row of d columns, in fp32.
  *   x                       in_type: PLORA_INPUT_FP32 (the deltas' y), or the same as type
@@ -621,7 +621,7 @@ PLORA_API plora_status plora_quant_weight(const void *w_dev, int32_t type, int32
 /* out_i [m][n_i] = x w_i^T for the 8-bit activations x [m][k] and 1 to 4 8-bit weights w_i [n_i][k] that share them (q, k and v;
  * gate and up), in one launch:
  *     out[r][c] = sum_b x_scale[r][b] w_scale[c / 128][b] sum_{k in block b} x[r][k] w[c][k]
- * Sums in fp32 (within a block the tensor cores cut what lies more than some 24 bits below the largest of 32 products and the sum so
+ * The two scales are multiplied first, in fp32.  Sums in fp32 (within a block the tensor cores cut what lies more than some 24 bits below the largest of 32 products and the sum so
  * far: a block's sum is off by at most 132 * 2^-24 of the largest of its products and partial sums), rounded once to out_type (fp32, bf16 or IEEE half); every element's sum is taken in an order that depends on the
  * sizes alone.  out is overwritten; rows out_stride elements apart (0: packed), any alignment of whole elements; rows aligned to
  * 16 bytes or more are fast.  x, w and their strides are 16-byte aligned; any m >= 0, n >= 1, k >= 1 up to 2^30, as long as

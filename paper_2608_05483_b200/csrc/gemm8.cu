@@ -15,8 +15,9 @@
 // single CTAs take tiles of 128 rows, and clusters of them split K where tiles are few, each leaving its sums in shared memory for
 // the others to add in the order of K.  Tiles have 64 to 256 columns; choose() estimates what is fastest.
 //
-// What bounds it.  Few rows: HBM (64 rows by 27648 x 5120 27.3 us, 5.5 TB/s), a launch's start and the first copies (12288 x 4096 by one
-// row 12.0 us, of which 7.7 are the weights).  Many rows: 4096 x 8192 x 8192 takes 300 us, 1.8 PFLOP/s at the power limit of 1000 W and
+// What bounds it (launches behind one another, graph replay).  Few rows: HBM (64 rows by 27648 x 5120 28.1 us, 5.3 TB/s, in a burst; 31.8 in
+// a long run at the power limit), a launch's start and the first copies (12288 x 4096 by one row 12.7 us, of which 7.7 are the weights;
+// 11.3 where the caller says that they are ready).  Many rows: 4096 x 8192 x 8192 takes 300 us, 1.8 PFLOP/s at the power limit of 1000 W and
 // 1.5 to 1.6 GHz.  Without its reads and additions it takes 241, with the reads alone 262: tensor memory serves the products and the
 // reads, and energy goes into both.  (The library's product of the same operands with one scale for all takes 228 for long, 185 in a burst.)
 #include "w8.cuh"
@@ -309,7 +310,7 @@ __device__ __forceinline__ void load_warp(const Params& p, const Maps& maps, con
     const uint32_t stages = p.stages, stage_bytes = C::kRun * (p.x_bytes + C::kBBytes);
     bool stopped = false;
     // Where the caller says that they were complete before the kernel in front began, the weights of the first stages are fetched
-    // before that kernel has completed (one row by 12288 x 4096 11.5 us so, 12.8 behind it).  Nothing here shows whether that kernel
+    // before that kernel has completed (one row by 12288 x 4096 11.3 us so, 12.7 behind it).  Nothing here shows whether that kernel
     // writes them: it may let this one start before it has, and even if it does not, its writes are visible only behind the wait.
     auto begin = [&](uint32_t s, const Tile& t, int b) {
         if (elect_one()) {
@@ -655,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<CG, BN>::kCtas) gemm_kernel(cons
         Turn<C::kAccs> in;
         Turn<kScaleSlots> run;
         float2 acc[C::kCols / 2];
-        // (warps whose rows no tile has leave at once: one row by 12288 x 4096 11.5 -> 11.35 us)
+        // (warps whose rows no tile has leave at once: one row by 12288 x 4096, weights ready, 11.5 -> 11.35 us)
 #pragma unroll 1
         for (int i = (warp & 3) < p.quads ? sh.first : p.tiles; i < p.tiles; i += sh.step) {
             const Tile u = tile_of(p, i);
